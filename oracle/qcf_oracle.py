@@ -370,3 +370,82 @@ class PlantOps:
     def shift_keys(self, shape, k_rows, delta):
         k, _ = rerope([k_rows], None, [delta], shape.rope_base, shape.rope_style)
         return k
+
+
+# --------------------------------------------------------------------------
+# decoding over a cache in pages
+# --------------------------------------------------------------------------
+
+def page_append(pools: Sequence[np.ndarray], table: np.ndarray, lens: Sequence[int], row_off: Sequence[int], k: np.ndarray,
+                v: np.ndarray, pos: Optional[np.ndarray], base: float, style: int = 0) -> Tuple[np.ndarray, ...]:
+    """Rows of k and v [M, H_kv, d] become tokens lens[b], lens[b] + 1, ... of their request, keys turned by pos.
+
+    pools (k, v [n_pages, page, H_kv, d], bounds [n_pages, H_kv, 2, d]) are copied, not changed; token t of request b is slot
+    t % page of page table[b, t // page], and is dropped where there is no such page.  bounds: least and largest key."""
+    kp, vp, bounds = (np.array(p, dtype=F64) for p in pools)
+    k = np.asarray(k, dtype=F64) if pos is None else rope_at(k, pos, base, style)
+    page = kp.shape[1]
+    for b in range(len(lens)):
+        for m in range(row_off[b], row_off[b + 1]):
+            t = lens[b] + m - row_off[b]
+            if t < 0 or t // page >= table.shape[1] or not 0 <= table[b, t // page] < kp.shape[0]:
+                continue
+            p, s = table[b, t // page], t % page
+            kp[p, s], vp[p, s] = k[m], v[m]
+            bounds[p, :, 0] = k[m] if s == 0 else np.minimum(bounds[p, :, 0], k[m])
+            bounds[p, :, 1] = k[m] if s == 0 else np.maximum(bounds[p, :, 1], k[m])
+    return kp, vp, bounds
+
+
+def page_scores(q: np.ndarray, bounds: np.ndarray, pages: np.ndarray) -> np.ndarray:
+    """Scores [H_kv, len(pages)] of pool pages for one row's queries q [H, d]: the largest product that a key within a page's
+    bounds can have with a query of the KV head's group; infinite where it is not a number, -inf for a page not in the pool."""
+    n_pages, n_kv = bounds.shape[:2]
+    group = q.shape[0] // n_kv
+    out = np.full((n_kv, len(pages)), -np.inf)
+    for j, p in enumerate(pages):
+        if not 0 <= p < n_pages:
+            continue
+        for g in range(n_kv):
+            x = np.asarray(q[g * group:(g + 1) * group], dtype=F64)
+            with np.errstate(invalid="ignore"):
+                s = (np.minimum(x, 0) * bounds[p, g, 0] + np.maximum(x, 0) * bounds[p, g, 1]).sum(-1)
+            out[g, j] = np.where(np.isfinite(s), s, np.inf).max()
+    return out
+
+
+def page_select(score: np.ndarray, n_keep: int, n_first: int, n_last: int) -> np.ndarray:
+    """Pages [H_kv, n_keep] of score [H_kv, P], ascending, -1 behind the last: the first and the last ones, then the largest
+    scores (as float32), ties to the lower page."""
+    n_kv, P = score.shape
+    out = np.full((n_kv, n_keep), -1, dtype=np.int64)
+    for g in range(n_kv):
+        with np.errstate(over="ignore"):
+            s = score[g].astype(np.float32)
+        always = [p for p in range(P) if p < n_first or p >= P - n_last]
+        rest = sorted((p for p in range(P) if p not in always), key=lambda p: -s[p])
+        kept = list(range(P)) if P <= n_keep else sorted(always + rest[:n_keep - len(always)])
+        out[g, :len(kept)] = kept
+    return out
+
+
+def page_attn(q: np.ndarray, k_pool: np.ndarray, v_pool: np.ndarray, table_row: np.ndarray, seen: int,
+              pages: Optional[np.ndarray] = None) -> Tuple[np.ndarray, np.ndarray]:
+    """One row's queries q [H, d] over tokens t < seen of its request (and of pages[g], [H_kv, n], where given): o [H, d], lse [H]."""
+    n_pages, page, n_kv, d = k_pool.shape
+    H = q.shape[0]
+    o, lse = np.zeros((H, d)), np.full(H, -np.inf)
+    for h in range(H):
+        g = h // (H // n_kv)
+        listed = range(len(table_row)) if pages is None else pages[g]
+        rows = [(table_row[p], t - p * page) for p in listed if 0 <= p < len(table_row) and 0 <= table_row[p] < n_pages
+                for t in range(p * page, min((p + 1) * page, seen))]
+        if not rows:
+            continue
+        at, slot = np.array(rows).T
+        logits = k_pool[at, slot, g].astype(F64) @ np.asarray(q[h], dtype=F64) / math.sqrt(d)
+        top = logits.max()
+        e = np.exp(logits - top)
+        o[h] = e @ v_pool[at, slot, g].astype(F64) / e.sum()
+        lse[h] = top + math.log(e.sum())
+    return o, lse

@@ -40,6 +40,10 @@ ANCHORS_EXPORTS = ["qcf_extract_anchors_workspace_bytes", "qcf_extract_anchors"]
 # declared in qcf_fuse.h
 FUSE_EXPORTS = ["qcf_fuse_layer"]
 
+# declared in qcf_pages.h
+PAGES_EXPORTS = ["qcf_page_append", "qcf_page_select_workspace_bytes", "qcf_page_select", "qcf_page_attn_workspace_bytes",
+                 "qcf_page_attn"]
+
 
 class QcfError(RuntimeError):
     pass
@@ -55,6 +59,12 @@ class ChunkDesc(C.Structure):
     _fields_ = [("k_src", C.c_void_p), ("v_src", C.c_void_p), ("len", C.c_int32),
                 ("src_pos0", C.c_int32), ("dst_row", C.c_int64), ("dst_pos0", C.c_int32),
                 ("reserved", C.c_int32)]
+
+
+class PageCacheDesc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("bounds", C.c_void_p), ("table", C.c_void_p),
+                ("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("max_pages", C.c_int32), ("reserved", C.c_int32)]
 
 
 _lib = None
@@ -133,6 +143,16 @@ def load_library() -> C.CDLL:
     lib.qcf_key_norm.argtypes = [dp, vp, i64, vp, vp]
     lib.qcf_gather.restype = C.c_int
     lib.qcf_gather.argtypes = [dp, vp, vp, vp, i64, i64, vp, vp, vp]
+    cp = C.POINTER(PageCacheDesc)
+    lib.qcf_page_append.restype = C.c_int
+    lib.qcf_page_append.argtypes = [dp, cp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]
+    for name in ("qcf_page_select_workspace_bytes", "qcf_page_attn_workspace_bytes"):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [dp, cp, i32, i32, i32]
+    lib.qcf_page_select.restype = C.c_int
+    lib.qcf_page_select.argtypes = [dp, cp, i32, i32, vp, vp, i32, i32, i32, vp, vp, sz, vp]
+    lib.qcf_page_attn.restype = C.c_int
+    lib.qcf_page_attn.argtypes = [dp, cp, i32, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -429,3 +449,78 @@ def qcf_gather(desc: LayerDesc, k_src: torch.Tensor, v_src: Optional[torch.Tenso
                total_rows: int, k_out: torch.Tensor, v_out: Optional[torch.Tensor]) -> None:
     _check(load_library().qcf_gather(C.byref(desc), _ptr(k_src), _ptr(v_src), _ptr(src_rows), M, total_rows,
                                      _ptr(k_out), _ptr(v_out), _stream()))
+
+
+class PageCache:
+    """A layer's cache in pages: the descriptor that the calls take, and the tensors that it points into."""
+
+    def __init__(self, desc: PageCacheDesc, tensors: tuple):
+        self.desc, self.tensors = desc, tensors
+        self.ref = C.byref(desc)
+
+
+def page_cache(k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor], table: torch.Tensor) -> PageCache:
+    """k and v [n_pages, page_size, H_kv, d] with equal strides and dense rows (any order of the other three, so views of a pool
+    that keeps the tokens of a head together are taken too); bounds [n_pages, H_kv, 2, d] or None; table [B, max_pages] int32."""
+    if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(3) != 1:
+        raise QcfError("k and v must have the shape [n_pages, page_size, H_kv, d], one type, equal strides and dense rows")
+    if not k.is_cuda or not v.is_cuda:
+        raise QcfError("tensors handed to the library must be CUDA tensors")
+    if table.dim() != 2 or table.dtype != torch.int32:
+        raise QcfError("table must be an int32 tensor [B, max_pages]")
+    n_pages, page_size, n_kv, d = k.shape
+    if bounds is not None and (bounds.shape != (n_pages, n_kv, 2, d) or bounds.dtype != k.dtype):
+        raise QcfError("bounds must have the shape [n_pages, H_kv, 2, d] and the type of the keys")
+    # (the stride of an axis of one entry says nothing: one that fits takes its place)
+    head = k.stride(2) if n_kv > 1 else d
+    slot = k.stride(1) if page_size > 1 else n_kv * d
+    page = k.stride(0) if n_pages > 1 else (page_size - 1) * slot + (n_kv - 1) * head + d
+    return PageCache(PageCacheDesc(k.data_ptr(), v.data_ptr(), _ptr(bounds), _ptr(table), page, slot, head, n_pages, page_size,
+                                   table.shape[1], 0), (k, v, bounds, table))
+
+
+def _rows(t: Optional[torch.Tensor]):
+    """Pointer and row stride of [rows, heads, d], dense but for the distance of its rows."""
+    if t is None:
+        return None, 0
+    dense = t.shape[1] * t.shape[2]
+    if not t.is_cuda or t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise QcfError("rows handed to the library must be CUDA tensors [rows, heads, d] with dense rows")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else dense
+
+
+def qcf_page_append(desc: LayerDesc, cache: PageCache, B: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                    row_off: torch.Tensor, total_rows: int, lens: torch.Tensor, pos: Optional[torch.Tensor],
+                    q_out: Optional[torch.Tensor]) -> None:
+    """Rows of k and v behind what their requests hold (lens), keys and queries turned by pos on the way."""
+    (qp, qs), (kp, ks), (vp, vs) = _rows(q), _rows(k), _rows(v)
+    _check(load_library().qcf_page_append(C.byref(desc), cache.ref, B, qp, qs, kp, ks, vp, vs, _ptr(row_off), total_rows,
+                                          _ptr(lens), _ptr(pos), _ptr(q_out), _stream()))
+
+
+def qcf_page_select_workspace_bytes(desc: LayerDesc, cache: PageCache, B: int, n_q: int, n_keep: int) -> int:
+    return int(load_library().qcf_page_select_workspace_bytes(C.byref(desc), cache.ref, B, n_q, n_keep))
+
+
+def qcf_page_select(desc: LayerDesc, cache: PageCache, B: int, n_q: int, q: torch.Tensor, seen: torch.Tensor, n_keep: int,
+                    n_first: int, n_last: int, pages: torch.Tensor, workspace: Optional[torch.Tensor] = None) -> None:
+    if workspace is None:
+        workspace = _workspace(qcf_page_select_workspace_bytes(desc, cache, B, n_q, n_keep), q.device)
+    wp, wn = _ws_args(workspace)
+    _check(load_library().qcf_page_select(C.byref(desc), cache.ref, B, n_q, _ptr(q), _ptr(seen), n_keep, n_first, n_last,
+                                          _ptr(pages), wp, wn, _stream()))
+
+
+def qcf_page_attn_workspace_bytes(desc: LayerDesc, cache: PageCache, B: int, n_q: int, n_keep: int) -> int:
+    return int(load_library().qcf_page_attn_workspace_bytes(C.byref(desc), cache.ref, B, n_q, n_keep))
+
+
+def qcf_page_attn(desc: LayerDesc, cache: PageCache, B: int, n_q: int, q: torch.Tensor, seen: torch.Tensor,
+                  pages: Optional[torch.Tensor], n_keep: int, o_out: torch.Tensor, lse_out: Optional[torch.Tensor],
+                  workspace: Optional[torch.Tensor] = None) -> None:
+    """Attention of n_q new rows of each request over all its pages, or over those that `pages` lists for each row and KV head."""
+    if workspace is None:
+        workspace = _workspace(qcf_page_attn_workspace_bytes(desc, cache, B, n_q, n_keep), q.device)
+    wp, wn = _ws_args(workspace)
+    _check(load_library().qcf_page_attn(C.byref(desc), cache.ref, B, n_q, _ptr(q), _ptr(seen), _ptr(pages), n_keep, _ptr(o_out),
+                                        _ptr(lse_out), wp, wn, _stream()))

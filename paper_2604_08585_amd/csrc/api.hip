@@ -581,4 +581,125 @@ qcf_status qcf_extract_anchors(const qcf_layer_desc* desc, const void* k, const 
   return launch_select_gather(*desc, norm, n_chunks, ctx_off, sel_off, k, v, rows, k_out, v_out, (hipStream_t)stream);
 }
 
+// ---- decoding over a cache in pages ------------------------------------------------
+static qcf_status check_page_cache(const qcf_layer_desc* desc, const qcf_page_cache* c) {
+  QCF_TRY(check_desc(desc));
+  if (!c) return fail(QCF_ERR_INVALID_ARG, "page cache is NULL");
+  if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1)))
+    return fail(QCF_ERR_UNSUPPORTED, "page_size %d (supported: 16, 32, 64, 128, 256)", c->page_size);
+  if (c->n_pages <= 0 || c->max_pages <= 0)
+    return fail(QCF_ERR_INVALID_ARG, "n_pages %d and max_pages %d must be positive", c->n_pages, c->max_pages);
+  if ((int64_t)c->max_pages * c->page_size > kMaxRows)
+    return fail(QCF_ERR_UNSUPPORTED, "max_pages %d of %d tokens: more than 2^30 tokens", c->max_pages, c->page_size);
+  if (c->reserved != 0) return fail(QCF_ERR_INVALID_ARG, "reserved must be 0");
+  const int64_t d = desc->head_dim, last_slot = c->page_size - 1, last_head = desc->n_kv_heads - 1, most = (int64_t)1 << 24;
+  if ((c->page_stride | c->slot_stride | c->head_stride) & 7)
+    return fail(QCF_ERR_INVALID_ARG, "page, slot and head strides must be multiples of 8");
+  if (c->slot_stride < d || c->head_stride < d || c->slot_stride > most || c->head_stride > most)
+    return fail(QCF_ERR_INVALID_ARG, "slot and head strides must be from head_dim to 2^24");
+  if (c->slot_stride < last_head * c->head_stride + d && c->head_stride < last_slot * c->slot_stride + d)
+    return fail(QCF_ERR_INVALID_ARG, "rows of a page overlap");
+  if (c->page_stride < last_slot * c->slot_stride + last_head * c->head_stride + d || c->page_stride > (int64_t)1 << 31)
+    return fail(QCF_ERR_INVALID_ARG, "page_stride %lld is less than what a page spans, or more than 2^31", (long long)c->page_stride);
+  return QCF_OK;
+}
+static qcf_status check_page_pointers(const qcf_page_cache* c, bool bounds) {
+  QCF_TRY(need_ptr(c->k, "cache k"));
+  QCF_TRY(need_ptr(c->v, "cache v"));
+  QCF_TRY(bounds ? need_ptr(c->bounds, "cache bounds") : opt_ptr(c->bounds, "cache bounds"));
+  return need_idx_ptr(c->table, "cache table");
+}
+static qcf_status check_row_stride(const char* name, int64_t stride, int64_t row) {
+  if (stride < row || (stride & 7) || stride > (int64_t)1 << 31)
+    return fail(QCF_ERR_INVALID_ARG, "%s_stride %lld (a multiple of 8 from %lld on)", name, (long long)stride, (long long)row);
+  return QCF_OK;
+}
+
+qcf_status qcf_page_append(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, const void* q, int64_t q_stride,
+                           const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int64_t* row_off_dev,
+                           int64_t total_rows, const int32_t* len_dev, const int32_t* pos_dev, void* q_out, void* stream) {
+  QCF_TRY(check_page_cache(desc, cache));
+  if (B < 0 || total_rows < 0) return fail(QCF_ERR_INVALID_ARG, "negative size");
+  if (B > 65535) return fail(QCF_ERR_UNSUPPORTED, "B %d > 65535", B);
+  if (total_rows > kMaxRows) return fail(QCF_ERR_UNSUPPORTED, "too many rows");
+  if (B == 0 || total_rows == 0) return QCF_OK;
+  QCF_TRY(check_page_pointers(cache, false));
+  QCF_TRY(need_ptr(k, "k"));
+  QCF_TRY(need_ptr(v, "v"));
+  QCF_TRY(need_idx_ptr(row_off_dev, "row_off_dev"));
+  QCF_TRY(need_idx_ptr(len_dev, "len_dev"));
+  if (pos_dev) QCF_TRY(need_idx_ptr(pos_dev, "pos_dev"));
+  QCF_TRY(check_row_stride("k", k_stride, (int64_t)desc->n_kv_heads * desc->head_dim));
+  QCF_TRY(check_row_stride("v", v_stride, (int64_t)desc->n_kv_heads * desc->head_dim));
+  if ((q == nullptr) != (q_out == nullptr)) return fail(QCF_ERR_INVALID_ARG, "q and q_out must both be given or both be NULL");
+  if (q) {
+    QCF_TRY(need_ptr(q, "q"));
+    QCF_TRY(need_ptr(q_out, "q_out"));
+    QCF_TRY(check_row_stride("q", q_stride, (int64_t)desc->n_q_heads * desc->head_dim));
+    if (q == q_out && q_stride != (int64_t)desc->n_q_heads * desc->head_dim)
+      return fail(QCF_ERR_INVALID_ARG, "q_out may be q only where its rows are dense");
+  }
+  return launch_page_append(*desc, *cache, B, q, q_stride, k, k_stride, v, v_stride, row_off_dev, total_rows, len_dev, pos_dev,
+                            q_out, (hipStream_t)stream);
+}
+
+// what the calls that read the cache have in common; *empty = nothing to do
+static qcf_status check_page_rows(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, int32_t n_keep,
+                                  bool* empty) {
+  QCF_TRY(check_page_cache(desc, cache));
+  if (B < 0 || n_q < 0 || n_keep < 0) return fail(QCF_ERR_INVALID_ARG, "negative size");
+  if (B > 65535) return fail(QCF_ERR_UNSUPPORTED, "B %d > 65535", B);
+  if (n_q > 16) return fail(QCF_ERR_UNSUPPORTED, "n_q %d > 16", n_q);
+  if ((int64_t)n_keep * cache->page_size > kMaxRows)
+    return fail(QCF_ERR_UNSUPPORTED, "n_keep %d of %d tokens: more than 2^30 tokens", n_keep, cache->page_size);
+  *empty = B == 0 || n_q == 0;
+  return QCF_OK;
+}
+
+size_t qcf_page_select_workspace_bytes(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, int32_t n_keep) {
+  bool empty = true;
+  if (check_page_rows(desc, cache, B, n_q, n_keep, &empty) != QCF_OK || empty || n_keep == 0) return 0;
+  return page_select_workspace(*desc, *cache, B, n_q);
+}
+
+qcf_status qcf_page_select(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, const void* q,
+                           const int32_t* seen_dev, int32_t n_keep, int32_t n_first, int32_t n_last, int32_t* pages,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  bool empty = true;
+  QCF_TRY(check_page_rows(desc, cache, B, n_q, n_keep, &empty));
+  if (n_first < 0 || n_last < 0) return fail(QCF_ERR_INVALID_ARG, "negative size");
+  if ((int64_t)n_first + n_last > n_keep)
+    return fail(QCF_ERR_INVALID_ARG, "n_first %d + n_last %d > n_keep %d", n_first, n_last, n_keep);
+  if (empty || n_keep == 0) return QCF_OK;
+  QCF_TRY(check_page_pointers(cache, true));
+  QCF_TRY(need_ptr(q, "q"));
+  QCF_TRY(need_idx_ptr(seen_dev, "seen_dev"));
+  QCF_TRY(need_idx_ptr(pages, "pages"));
+  QCF_TRY(need_ws(workspace, workspace_bytes, page_select_workspace(*desc, *cache, B, n_q)));
+  return launch_page_select(*desc, *cache, B, n_q, q, seen_dev, n_keep, n_first, n_last, pages, workspace, (hipStream_t)stream);
+}
+
+size_t qcf_page_attn_workspace_bytes(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, int32_t n_keep) {
+  bool empty = true;
+  if (check_page_rows(desc, cache, B, n_q, n_keep, &empty) != QCF_OK || empty) return 0;
+  return page_attn_workspace(*desc, *cache, B, n_q, n_keep);
+}
+
+qcf_status qcf_page_attn(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, const void* q,
+                         const int32_t* seen_dev, const int32_t* pages, int32_t n_keep, void* o_out, float* lse_out,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  bool empty = true;
+  QCF_TRY(check_page_rows(desc, cache, B, n_q, n_keep, &empty));
+  if ((pages == nullptr) != (n_keep == 0)) return fail(QCF_ERR_INVALID_ARG, "pages and n_keep must both be given, or NULL and 0");
+  if (empty) return QCF_OK;
+  QCF_TRY(check_page_pointers(cache, false));
+  QCF_TRY(need_ptr(q, "q"));
+  QCF_TRY(need_idx_ptr(seen_dev, "seen_dev"));
+  if (pages) QCF_TRY(need_idx_ptr(pages, "pages"));
+  QCF_TRY(need_ptr(o_out, "o_out"));
+  if (lse_out) QCF_TRY(need_idx_ptr(lse_out, "lse_out"));
+  QCF_TRY(need_ws(workspace, workspace_bytes, page_attn_workspace(*desc, *cache, B, n_q, n_keep)));
+  return launch_page_attn(*desc, *cache, B, n_q, q, seen_dev, pages, n_keep, o_out, lse_out, workspace, (hipStream_t)stream);
+}
+
 }  // extern "C"

@@ -13,6 +13,7 @@
 #include "qcf_layers.h"
 #include "qcf_anchors.h"
 #include "qcf_fuse.h"
+#include "qcf_pages.h"
 
 namespace qcf {
 
@@ -343,5 +344,22 @@ qcf_status launch_rmsnorm(const qcf_layer_desc& L, const void* x, const void* we
                           int32_t cols, void* out, hipStream_t st);
 qcf_status launch_swiglu(const qcf_layer_desc& L, const void* gate_up, int64_t M, int32_t F, void* out,
                          hipStream_t st);
+
+// decoding over a cache in pages (validated by the entry points)
+qcf_status launch_page_append(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, const void* q, int64_t q_stride,
+                              const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int64_t* row_off,
+                              int64_t total_rows, const int32_t* len, const int32_t* pos, void* q_out, hipStream_t st);
+size_t page_select_workspace(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q);
+qcf_status launch_page_select(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, const void* q,
+                              const int32_t* seen, int32_t n_keep, int32_t n_first, int32_t n_last, int32_t* pages, void* ws,
+                              hipStream_t st);
+// the n_keep pages of each (row, KV head), the first n_first and last n_last that the row sees and the largest scores of the others
+// (select.hip); row r sees ceil(seen[r] / page_size) pages, and has max_pages scores for each KV head
+qcf_status launch_page_top(const float* score, const int32_t* seen, int64_t rows, int32_t Hkv, int32_t page_size, int32_t max_pages,
+                           int32_t n_keep, int32_t n_first, int32_t n_last, int32_t* pages, hipStream_t st);
+size_t page_attn_workspace(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, int32_t n_keep);
+qcf_status launch_page_attn(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, const void* q,
+                            const int32_t* seen, const int32_t* pages, int32_t n_keep, void* o, float* lse, void* ws,
+                            hipStream_t st);
 
 }  // namespace qcf

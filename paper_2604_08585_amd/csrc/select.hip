@@ -524,6 +524,43 @@ __global__ __launch_bounds__(kThreads) void select_gather_kernel(const float* __
   }
 }
 
+// Pages of a row for one KV head: the first and the last ones that are kept whatever their scores, and the largest scores of those
+// between them.  They leave in the order first, chosen, last, which is ascending; -1 behind them.
+template <int MAX>
+__global__ __launch_bounds__(kThreads) void page_top_kernel(const float* __restrict__ score, const int32_t* __restrict__ seen,
+                                                            int Hkv, int log2_page, int max_pages, int n_keep, int n_first,
+                                                            int n_last, int32_t* __restrict__ pages) {
+  __shared__ SelectLds lds;
+  const int64_t row = blockIdx.x;
+  const int tid = threadIdx.x;
+  const int count = (int)min(((int64_t)max(seen[row / Hkv], 0) + (1 << log2_page) - 1) >> log2_page, (int64_t)max_pages);
+  const int n = min(count, n_keep);
+  int32_t* out = pages + row * n_keep;
+  for (int i = n + tid; i < n_keep; i += kThreads) out[i] = -1;
+  if (count <= n_keep) {
+    for (int i = tid; i < n; i += kThreads) out[i] = i;
+    return;
+  }
+  for (int i = tid; i < n_first; i += kThreads) out[i] = i;
+  for (int i = tid; i < n_last; i += kThreads) out[n - n_last + i] = count - n_last + i;
+  const int T = count - n_first - n_last, N = n - n_first - n_last;      // (T > N: there are more than n_keep)
+  if (N <= 0) return;
+  const float* s = score + row * max_pages + n_first;
+  const int64_t o0 = row * n_keep + n_first;
+  int seg = (T + kThreads - 1) / kThreads;
+  if (seg > 1) seg = (seg + 3) & ~3;
+#define QCF_SELECT(SEG) select_request<SEG>(lds, s, n_first, T, N, seg, o0, 0, nullptr, pages, nullptr)
+  if (seg <= 1) QCF_SELECT(1);
+  else if constexpr (MAX != 1) {
+    if (seg <= 8) QCF_SELECT(8);
+    else if constexpr (MAX == 0 || MAX > 8) {
+      if (seg <= 32) QCF_SELECT(32);
+      else if constexpr (MAX == 0) QCF_SELECT(0);
+    }
+  }
+#undef QCF_SELECT
+}
+
 }  // namespace
 
 size_t select_workspace(int32_t, int64_t) { return 0; }
@@ -543,6 +580,20 @@ qcf_status launch_select(int32_t B, const float* score, const int64_t* ctx_off, 
   else QCF_LAUNCH(0);
 #undef QCF_LAUNCH
   return check_launch("select");
+}
+
+qcf_status launch_page_top(const float* score, const int32_t* seen, int64_t rows, int32_t Hkv, int32_t page_size, int32_t max_pages,
+                           int32_t n_keep, int32_t n_first, int32_t n_last, int32_t* pages, hipStream_t st) {
+  const int log2_page = __builtin_ctz((unsigned)page_size);
+#define QCF_LAUNCH(MAX)                                                                                                          \
+  page_top_kernel<MAX><<<dim3((unsigned)(rows * Hkv)), dim3(kThreads), 0, st>>>(score, seen, Hkv, log2_page, max_pages, n_keep, \
+                                                                                n_first, n_last, pages)
+  if (max_pages <= kThreads) QCF_LAUNCH(1);
+  else if (max_pages <= 8 * kThreads) QCF_LAUNCH(8);
+  else if (max_pages <= 32 * kThreads) QCF_LAUNCH(32);
+  else QCF_LAUNCH(0);
+#undef QCF_LAUNCH
+  return check_launch("page selection");
 }
 
 qcf_status launch_select_sums(const ScoreSums& sums, float* score, const int64_t* ctx_off, int64_t total_ctx, const int64_t* sel_off,
