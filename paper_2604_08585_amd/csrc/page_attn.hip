@@ -1,112 +1,557 @@
 // Attention of the newest tokens over a cache in pages.
+//
+// One pass over the keys and values with a running reference point and sum of each row's softmax.  A context is divided into
+// units of equal length, as many as the GPU holds at once, which partial results of rows that have several join in a second launch.
+// Bound by memory: 4 d operations to a token and row against 4 d bytes (bf16) to a token and KV head, 4 to 64 a byte.
+//
+// A wave takes 32 tokens (16 in float32) at a time, without LDS: the logits are products K Q^T of 16 tokens x 16 rows, so a lane
+// owns a row and four tokens; the outputs are V^T P^T of 16 elements x 16 rows, in which the order of the tokens is free.  It
+// is taken so that a lane's four tokens of the logits are its tokens of that product, and the elements of a head so that a lane
+// loads 16 bytes of a value row.  What is left is a transposition inside the lane (bf16: 8 tokens x 8 elements, 32 v_perm).
 #include "qcf_internal.h"
+#include "page_layout.h"
 
 namespace qcf {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+using pages::kWaves;
+constexpr int kThreads = 64 * kWaves;
+constexpr float kLn2 = 0.6931471805599453f;
+// A row's reference point moves where a logit is more than 8 above it (in powers of two): weights are up to 256 then, and most
+// tiles neither exchange their maxima nor scale what has been summed.
+constexpr float kAhead = 8.f;
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+enum Mode { kOne = 0, kList = 1, kSeveral = 2 };         // one new row to a context, pages of its own, or several new rows
 
 struct PageAttnArgs {
   qcf_page_cache c;
   const void* q;
   const int32_t* seen;
-  const int32_t* pages;
-  int n_keep, B, n_q, H, Hkv, log2_page;
+  const int32_t* list;
+  int n_keep, n_q, H, Hkv, G, log2_page;
+  int contexts, rows, row_blocks, inner, slots, part_rows;
+  float scale;                                           // log2(e) / sqrt(d)
   void* o;
   float* lse;
+  float* part_o;
+  float2* part_ml;
 };
 
-// One workgroup per (row, head); a wave takes every fourth token, its lanes the elements of the head.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void page_attn_kernel(PageAttnArgs a) {
-  constexpr int E = D / 64, WAVES = kThreads / 64;
-  __shared__ float s_m[WAVES], s_l[WAVES], s_o[WAVES][D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = blockIdx.x / a.H;                  // (request, new row)
-  const int h = (int)(blockIdx.x - row * a.H), g = h / (a.H / a.Hkv), b = (int)(row / a.n_q);
-  const int64_t seen = min((int64_t)max(a.seen[row], 0), (int64_t)a.c.max_pages << a.log2_page);
-  const int count = (int)((seen + a.c.page_size - 1) >> a.log2_page);
-  const int32_t* list = a.pages ? a.pages + (row * a.Hkv + g) * a.n_keep : nullptr;
-  const int n_pages = list ? a.n_keep : count;
-  float x[E], o[E];
-  const T* q = static_cast<const T*>(a.q) + (row * a.H + h) * D;
+// Tokens that context x covers: what its rows see, or its listed pages.
+__device__ __forceinline__ int64_t context_tokens(const PageAttnArgs& a, int x) {
+  const int64_t most = (int64_t)a.c.max_pages << a.log2_page;
+  if (a.list) {
+    const int64_t seen = min((int64_t)max(a.seen[x], 0), most);
+    return min((seen + a.c.page_size - 1) >> a.log2_page, (int64_t)a.n_keep) << a.log2_page;
+  }
+  int seen = 0;
+  for (int i = 0; i < a.n_q; ++i) seen = max(seen, a.seen[(int64_t)x * a.n_q + i]);
+  return min((int64_t)seen, most);
+}
+
+__device__ __forceinline__ int64_t wave_add(int64_t x) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) { x[e] = Elem<T>::load(q + lane + 64 * e); o[e] = 0.f; }
-  const float scale = kLog2e / sqrtf((float)D);
-  float m = -INFINITY, l = 0.f;
-  bool any = false;
-  for (int i = 0; i < n_pages; ++i) {
-    const int p = list ? list[i] : i;
-    if (p < 0 || p >= count) continue;
-    const int phys = a.c.table[(int64_t)b * a.c.max_pages + p];
-    if (phys < 0 || phys >= a.c.n_pages) continue;
-    const int n = (int)min((int64_t)a.c.page_size, seen - ((int64_t)p << a.log2_page));
-    const int64_t at = phys * a.c.page_stride + g * a.c.head_stride;
-    for (int s = wave; s < n; s += WAVES) {
-      const T* k = static_cast<const T*>(a.c.k) + at + s * a.c.slot_stride;
-      const T* v = static_cast<const T*>(a.c.v) + at + s * a.c.slot_stride;
-      float dot = 0.f;
+  for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
+  return x;
+}
+__device__ __forceinline__ int wave_incl(int x, int lane) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) dot += x[e] * Elem<T>::load(k + lane + 64 * e);
-      const float logit = wave_sum(dot) * scale;
-      any = true;
-      const float top = fmaxf(m, logit);
-      const float ref = top == -INFINITY ? 0.f : top;     // (all logits so far -inf: their weights are 0, not NaN)
-      const float keep = m == top ? 1.f : exp2f(m - ref), w = exp2f(logit - ref);
-      m = top;
-      l = l * keep + w;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d, 64);
+    x += lane >= d ? y : 0;
+  }
+  return x;
+}
+
+struct Unit {
+  int x;                   // context (-1: no such unit)
+  int first, count;        // its first unit, and the number of its units
+  int64_t tokens, step;    // of the context, of a unit
+};
+
+// Every wave works the division out by itself, from the tokens of all contexts (of=false: the context of unit u; of=true: the units
+// of context u).
+__device__ __forceinline__ Unit find_unit(const PageAttnArgs& a, int64_t u, bool of, int lane) {
+  int64_t total = 0;
+  for (int x0 = 0; x0 < a.contexts; x0 += 64) total += x0 + lane < a.contexts ? context_tokens(a, x0 + lane) : 0;
+  total = wave_add(total);
+  Unit r;
+  r.step = pages::unit_tokens(total, a.slots);
+  int before = 0;
+  for (int x0 = 0; x0 < a.contexts; x0 += 64) {
+    const int x = x0 + lane;
+    const int64_t tokens = x < a.contexts ? context_tokens(a, x) : 0;
+    const int n = x < a.contexts ? (int)pages::units_of(tokens, r.step) : 0;
+    const int incl = before + wave_incl(n, lane);
+    const uint64_t hit = __ballot(x < a.contexts && (of ? x == u : u < incl));
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      r.x = x0 + l;
+      r.count = __builtin_amdgcn_readlane(n, l);
+      r.first = __builtin_amdgcn_readlane(incl, l) - r.count;
+      r.tokens = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)tokens, l);     // (at most 2^30)
+      return r;
+    }
+    before = __builtin_amdgcn_readlane(incl, 63);
+  }
+  r.x = -1;
+  return r;
+}
+
+// 64 entries of a context's pages, one to a lane, and the tile's part of them.
+struct Window {
+  int first;               // index of lane 0's page in the context's order
+  int phys, page;          // lane's page: number in the pool (-1: not there), and in the request
+};
+
+template <typename T, int D, int RT, int MODE>
+struct Walk {
+  static constexpr bool kHalf = sizeof(T) == 2;
+  static constexpr int kSub = kHalf ? 2 : 1;             // parts of 16 tokens of a tile; a part lies in one page
+  static constexpr int kTokens = 16 * kSub, kS = 4 * kSub;             // tokens of a tile, logits of a lane
+  static constexpr int kLoads = kHalf ? D / 32 : D / 16;               // 16-byte loads of a lane for 16 tokens' keys
+  static constexpr int kE = D / 16;                                    // 16-element slices of the output
+  static constexpr int kV = kHalf ? 8 : 4 * (D / 64);                  // value loads of a lane
+  static constexpr int kVWords = kHalf && D == 64 ? 2 : 4;
+  typedef uint32_t vec_v __attribute__((ext_vector_type(kVWords)));
+
+  struct Tile {
+    u32x4 k[kSub][kLoads];
+    vec_v v[kV];
+    int base[kSub];                                      // request's number of its first token (-1: not there)
+  };
+
+  const PageAttnArgs& a;
+  const int lane, quad, col, g, x, b;
+  const int64_t end;                                     // of the unit, in the context's order
+  int count;                                             // pages that a row sees (listed pages from there on are none)
+  Window w;
+  u32x4 q[RT][kLoads];
+  int lim[RT];                                           // tokens that the lane's row sees
+  int lim_lo, lim_hi;                                    // least and largest of the rows that see anything
+  float m[RT], l[RT];
+  bool any[RT];
+  floatx4 acc[RT][kE];
+
+  __device__ __forceinline__ Walk(const PageAttnArgs& args, int lane_, int g_, int x_, int64_t end_)
+      : a(args), lane(lane_), quad(lane_ >> 4), col(lane_ & 15), g(g_), x(x_), b(MODE == kList ? x_ / args.n_q : x_), end(end_) {}
+
+  __device__ __forceinline__ void open(int first) {
+    w.first = first;
+    int p = first + lane;
+    if constexpr (MODE == kList) p = p < a.n_keep ? a.list[((int64_t)x * a.Hkv + g) * a.n_keep + p] : -1;
+    const bool ok = p >= 0 && p < count;
+    const int phys = ok ? a.c.table[(int64_t)b * a.c.max_pages + p] : -1;
+    w.page = p;
+    w.phys = phys < a.c.n_pages ? phys : -1;
+  }
+
+  __device__ __forceinline__ void load(Tile& t, int64_t at) {
+    const int mask = a.c.page_size - 1;
+    const int last = (int)((at + kTokens - 1) >> a.log2_page);
+    if (last - w.first >= 64) open((int)(at >> a.log2_page));
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = o[e] * keep + w * Elem<T>::load(v + lane + 64 * e);
+    for (int h = 0; h < kSub; ++h) {
+      const int64_t mine = at + 16 * h;
+      const int i = (int)(mine >> a.log2_page) - w.first;
+      const int slot = (int)mine & mask;
+      int phys = __builtin_amdgcn_readlane(w.phys, i);
+      const int page = __builtin_amdgcn_readlane(w.page, i);
+      const bool there = phys >= 0 && mine < end;
+      t.base[h] = there ? (page << a.log2_page) + slot : -1;
+      // (a page that is not there: page 0 is read instead, and nothing of it used)
+      phys = max(phys, 0);
+      const int64_t off = phys * a.c.page_stride + g * a.c.head_stride + slot * a.c.slot_stride;
+      const char* k = reinterpret_cast<const char*>(static_cast<const T*>(a.c.k) + off);
+      const char* v = reinterpret_cast<const char*>(static_cast<const T*>(a.c.v) + off);
+      const uint32_t stride = (uint32_t)a.c.slot_stride * sizeof(T);
+#pragma unroll
+      for (int f = 0; f < kLoads; ++f)
+        t.k[h][f] = *reinterpret_cast<const u32x4*>(k + (col * stride + 16 * quad + 64 * f));
+#pragma unroll
+      for (int j = 0; j < kV / kSub; ++j) {
+        const int token = kHalf ? j : j & 3, part = kHalf ? 0 : j >> 2;
+        t.v[kHalf ? 4 * h + j : j] =
+            *reinterpret_cast<const vec_v*>(v + ((4 * quad + token) * stride + col * (uint32_t)sizeof(vec_v) + 256 * part));
+      }
     }
   }
-  if (any && m == -INFINITY) l = NAN;
-  if (lane == 0) { s_m[wave] = m; s_l[wave] = l; }
+
+  // products of the tile's values with the weights, added to c
+  __device__ __forceinline__ void values(const Tile& t, const float (&p)[RT][kS], floatx4 (&c)[RT][kE]) const {
+    if constexpr (kHalf) {
+      // weights as two bf16 terms, of 16 bits together: cut off, and what that left, rounded.  (The second term of a weight that
+      // is not 0 is kept from being 0, so that an infinite value comes out infinite and not NaN.)
+      bf16x8 hi[RT], lo[RT];
 #pragma unroll
-  for (int e = 0; e < E; ++e) s_o[wave][lane + 64 * e] = o[e];
-  __syncthreads();
-  if (wave > 0) return;
-  float top = s_m[0];
-  for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_m[w]);
-  float total = 0.f;
+      for (int r = 0; r < RT; ++r) {
+        u32x4 ph, pl;
 #pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int w = 0; w < WAVES; ++w) {
-    // (a part whose logits are all -inf weighs nothing beside others, and makes the row NaN alone)
-    if (s_m[w] == -INFINITY && !(top == -INFINITY && s_l[w] != 0.f)) continue;
-    const float f = s_m[w] == top ? 1.f : exp2f(s_m[w] - top);
-    total += f * s_l[w];
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x0 = __float_as_uint(p[r][2 * i]), x1 = __float_as_uint(p[r][2 * i + 1]);
+          ph[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+          float r0 = p[r][2 * i] - __uint_as_float(x0 & 0xffff0000u), r1 = p[r][2 * i + 1] - __uint_as_float(x1 & 0xffff0000u);
+          r0 = p[r][2 * i] > 0.f ? fmaxf(r0, 1e-30f) : r0;
+          r1 = p[r][2 * i + 1] > 0.f ? fmaxf(r1, 1e-30f) : r1;
+          pl[i] = cvt_pk_bf16(r0, r1);
+        }
+        hi[r] = __builtin_bit_cast(bf16x8, ph);
+        lo[r] = __builtin_bit_cast(bf16x8, pl);
+      }
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += f * s_o[w][lane + 64 * e];
+      for (int e = 0; e < kE; ++e) {
+        u32x4 vt;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          vt[i] = __builtin_amdgcn_perm(t.v[2 * i + 1][e / 2], t.v[2 * i][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+        const bf16x8 va = __builtin_bit_cast(bf16x8, vt);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          c[r][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, hi[r], c[r][e], 0, 0, 0);
+          c[r][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, lo[r], c[r][e], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kV; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+            c[r][4 * (j >> 2) + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.v[j][e]), p[r][j & 3], c[r][4 * (j >> 2) + e], 0, 0, 0);
+    }
   }
-  const bool nothing = top == -INFINITY && total == 0.f;
-  T* out = static_cast<T*>(a.o) + (row * a.H + h) * D;
+
+  __device__ __forceinline__ int token(const Tile& t, int i) const { return t.base[i >> 2] + 4 * quad + (i & 3); }
+
+  // values of tokens from `limit` on, and of pages that are not there, become 0
+  __device__ __forceinline__ void clear(Tile& t, int limit) const {
 #pragma unroll
-  for (int e = 0; e < E; ++e) Elem<T>::store(out + lane + 64 * e, nothing ? 0.f : o[e] / total);
-  if (a.lse && lane == 0) a.lse[row * a.H + h] = nothing ? -INFINITY : (top + log2f(total)) * kLn2;
+    for (int j = 0; j < kV; ++j) {
+      const int i = kHalf ? j : j & 3;
+      const bool ok = t.base[i >> 2] >= 0 && token(t, i) < limit;
+#pragma unroll
+      for (int e = 0; e < kVWords; ++e) t.v[j][e] = ok ? t.v[j][e] : 0u;
+    }
+  }
+
+  __device__ __forceinline__ void step(Tile& t) {
+    float s[RT][kS];
+#pragma unroll
+    for (int h = 0; h < kSub; ++h)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        floatx4 z = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (kHalf) {
+#pragma unroll
+          for (int f = 0; f < kLoads; ++f)
+            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[h][f]), __builtin_bit_cast(bf16x8, q[r][f]), z, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int f = 0; f < kLoads; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              z = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[h][f][e]), __uint_as_float(q[r][f][e]), z, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[r][4 * h + i] = z[i] * a.scale;
+      }
+    // a tile that every row sees as a whole needs no mask
+    bool whole = true;
+#pragma unroll
+    for (int h = 0; h < kSub; ++h) whole = whole && t.base[h] >= 0 && t.base[h] + 16 <= lim_lo;
+    bool shared = true;                                  // no token that some rows see and others do not
+    if (!whole) {
+#pragma unroll
+      for (int h = 0; h < kSub; ++h)
+        if (MODE == kSeveral && t.base[h] >= 0 && t.base[h] < lim_hi && t.base[h] + 16 > lim_lo) shared = lim_lo == lim_hi;
+      clear(t, lim_hi);
+    }
+    float p[RT][kS];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      if (whole) any[r] = true;
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kS; ++i) {
+        if (!whole) {
+          const bool ok = t.base[i >> 2] >= 0 && token(t, i) < lim[r];
+          any[r] = any[r] || ok;
+          top = ok ? fmaxf(top, s[r][i]) : top;
+        } else {
+          top = fmaxf(top, s[r][i]);
+        }
+      }
+      if (__any(top > m[r] + kAhead)) {
+        typedef unsigned u2v __attribute__((ext_vector_type(2)));
+        u2v y = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(y.x), __uint_as_float(y.y));
+        y = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(y.x), __uint_as_float(y.y));
+        const float next = top > m[r] + kAhead ? top : m[r];          // (each row by itself)
+        const float f = next == m[r] ? 1.f : __builtin_amdgcn_exp2f(m[r] - next);
+        m[r] = next;
+        l[r] *= f;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) acc[r][e] *= f;
+      }
+      const float ref = m[r] == -INFINITY ? 0.f : m[r];               // (all logits so far -inf: weights of 0, not NaN)
+#pragma unroll
+      for (int i = 0; i < kS; ++i) {
+        float e = __builtin_amdgcn_exp2f(s[r][i] - ref);
+        if (!whole) e = t.base[i >> 2] >= 0 && token(t, i) < lim[r] ? e : 0.f;
+        p[r][i] = e;
+        l[r] += e;
+      }
+    }
+    if (MODE != kSeveral || shared) {
+      values(t, p, acc);
+      return;
+    }
+    // Tokens that only some of the rows see: one new row after the other, with the values that it does not see cleared, so that 0
+    // times a value that is not finite does not reach it.
+    for (int i = a.n_q - 1; i >= 0; --i) {               // (copies of the tile are cleared further and further only if limits fall)
+      Tile mine = t;
+      int limit = a.seen[(int64_t)b * a.n_q + i];
+      clear(mine, limit);
+      floatx4 c[RT][kE];
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int e = 0; e < kE; ++e) c[r][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+      values(mine, p, c);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const bool here = row_of(r) / a.G == i;
+#pragma unroll
+        for (int e = 0; e < kE; ++e)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) acc[r][e][y] += here ? c[r][e][y] : 0.f;
+      }
+    }
+  }
+
+  int row0;                                              // first row of the workgroup
+  __device__ __forceinline__ int row_of(int r) const { return row0 + 16 * r + col; }
+
+  __device__ __forceinline__ void start(int first_row, int64_t begin) {
+    row0 = first_row;
+    const int64_t most = (int64_t)a.c.max_pages << a.log2_page;
+    int lo = 0x7fffffff, hi = 0;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const int row = row_of(r);
+      const bool there = row < a.rows;
+      const int i = there ? row / a.G : 0;
+      const int64_t out = MODE == kList ? x : (int64_t)x * a.n_q + i;
+      lim[r] = there ? (int)min((int64_t)max(a.seen[out], 0), most) : 0;
+      if (lim[r] > 0) { lo = min(lo, lim[r]); hi = max(hi, lim[r]); }
+      const T* src = static_cast<const T*>(a.q) + (out * a.H + g * a.G + (there ? row - i * a.G : 0)) * D;
+      const u32x4 zero = {0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int f = 0; f < kLoads; ++f)
+        q[r][f] = there ? *reinterpret_cast<const u32x4*>(src + (4 * f + quad) * (16 / (int)sizeof(T))) : zero;
+      m[r] = -INFINITY;
+      l[r] = 0.f;
+      any[r] = false;
+#pragma unroll
+      for (int e = 0; e < kE; ++e) acc[r][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    if constexpr (MODE == kSeveral) {
+#pragma unroll
+      for (int d = 8; d >= 1; d >>= 1) { lo = min(lo, __shfl_xor(lo, d, 64)); hi = max(hi, __shfl_xor(hi, d, 64)); }
+      lim_lo = hi > 0 ? __builtin_amdgcn_readfirstlane(lo) : 0;
+      lim_hi = __builtin_amdgcn_readfirstlane(hi);
+    } else {
+      lim_lo = lim_hi = __builtin_amdgcn_readfirstlane(lim[0]);       // (row 0 is always there)
+    }
+    count = (int)(((int64_t)lim_hi + a.c.page_size - 1) >> a.log2_page);
+    open((int)(begin >> a.log2_page));
+  }
+};
+
+template <typename T, int D, int RT, int MODE>
+__global__ __launch_bounds__(kThreads, RT == 1 ? 2 : 1) void page_attn_kernel(PageAttnArgs a) {
+  typedef Walk<T, D, RT, MODE> W;
+  constexpr int kRows = 16 * RT;
+  __shared__ __align__(16) float s_o[kWaves][kRows][D + 4];         // (rows 4 banks apart)
+  __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t u = blockIdx.x / a.inner;
+  const int in = (int)(blockIdx.x - u * a.inner), g = in % a.Hkv, row0 = in / a.Hkv * kRows;
+  const Unit unit = find_unit(a, u, false, lane);
+  if (unit.x < 0) return;
+  const int64_t begin = (u - unit.first) * unit.step, end = min(begin + unit.step, unit.tokens);
+  W w(a, lane, g, unit.x, end);
+  w.start(row0, begin);
+  int64_t at = begin + wave * W::kTokens;
+  constexpr int kStep = kWaves * W::kTokens;
+  if (at < end) {
+    typename W::Tile t0, t1;
+    w.load(t0, at);
+    while (true) {
+      at += kStep;
+      if (at < end) w.load(t1, at);
+      w.step(t0);
+      if (at >= end) break;
+      at += kStep;
+      if (at < end) w.load(t0, at);
+      w.step(t1);
+      if (at >= end) break;
+    }
+  }
+  // join the waves: their sums go through LDS, scaled to the largest of their reference points
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    if (w.lim[r] == 0) { w.m[r] = -INFINITY; w.l[r] = 0.f; w.any[r] = false; }       // (beside rows that see whole tiles)
+    float l = w.l[r];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    bool any = w.any[r];
+    any = __shfl_xor((int)any, 16, 64) || any;
+    any = __shfl_xor((int)any, 32, 64) || any;
+    if (any && w.m[r] == -INFINITY) l = NAN;             // only logits of -inf
+    if (lane < 16) { s_m[wave][16 * r + lane] = w.m[r]; s_l[wave][16 * r + lane] = l; }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < W::kE; e += 4) {
+        const int dim = W::kHalf ? D / 16 * (4 * w.quad + i) + e : 16 * e + 4 * (4 * w.quad + i);
+        *reinterpret_cast<floatx4*>(&s_o[wave][16 * r + w.col][dim]) =
+            floatx4{w.acc[r][e][i], w.acc[r][e + 1][i], w.acc[r][e + 2][i], w.acc[r][e + 3][i]};
+      }
+  }
+  __syncthreads();
+  const int rows = min(kRows, a.rows - row0);
+  for (int item = tid; item < rows * (D / 4); item += kThreads) {
+    const int r = item / (D / 4), e = item % (D / 4) * 4;
+    float top = s_m[0][r];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) top = fmaxf(top, s_m[i][r]);
+    float l = 0.f;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      const float mi = s_m[i][r], li = s_l[i][r];
+      // (what saw nothing or only logits of -inf weighs nothing beside others; the latter make a row NaN that has nothing else)
+      if (mi == -INFINITY) { l = top == -INFINITY ? l + li : l; continue; }
+      const float f = mi == top ? 1.f : __builtin_amdgcn_exp2f(mi - top);
+      l += f * li;
+      o += f * *reinterpret_cast<const floatx4*>(&s_o[i][r][e]);
+    }
+    if (unit.count > 1) {
+      const int64_t part = (u * a.inner + in) * a.part_rows + r;
+      *reinterpret_cast<floatx4*>(a.part_o + part * D + e) = o;
+      if (e == 0) a.part_ml[part] = make_float2(top, l);
+      continue;
+    }
+    const int row = row0 + r, i = row / a.G;
+    const int64_t out = ((MODE == kList ? unit.x : (int64_t)unit.x * a.n_q + i) * a.H + g * a.G + (row - i * a.G));
+    const bool nothing = top == -INFINITY && l == 0.f;
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) o[y] = nothing ? 0.f : o[y] * inv;
+    T* dst = static_cast<T*>(a.o) + out * D + e;
+    if constexpr (W::kHalf) *reinterpret_cast<u32x2*>(dst) = u32x2{cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3])};
+    else *reinterpret_cast<floatx4*>(dst) = o;
+    if (a.lse && e == 0) a.lse[out] = nothing ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+}
+
+// Joins the units of a context: one workgroup per (context, KV head and row block, row).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void page_join_kernel(PageAttnArgs a) {
+  constexpr int kVecs = D / 4, kGroups = 256 / kVecs;    // a group of threads takes every kGroups-th unit
+  __shared__ __align__(16) float s_o[kGroups][D];
+  __shared__ float s_l[kGroups], s_m[kGroups];
+  const int tid = threadIdx.x, lane = tid & 63, group = tid / kVecs, e = tid % kVecs * 4;
+  const int r = blockIdx.x % a.part_rows;
+  const int64_t rest = blockIdx.x / a.part_rows;
+  const int in = (int)(rest % a.inner), g = in % a.Hkv, row = in / a.Hkv * a.part_rows + r;
+  if (row >= a.rows) return;
+  const Unit unit = find_unit(a, rest / a.inner, true, lane);
+  if (unit.count <= 1) return;
+  const int64_t part0 = ((int64_t)unit.first * a.inner + in) * a.part_rows + r, step = (int64_t)a.inner * a.part_rows;
+  float top = -INFINITY;
+  for (int j = group; j < unit.count; j += kGroups) top = fmaxf(top, a.part_ml[part0 + j * step].x);
+  if (e == 0) s_m[group] = top;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kGroups; ++j) top = fmaxf(top, s_m[j]);
+  float l = 0.f;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int j = group; j < unit.count; j += kGroups) {
+    const float2 ml = a.part_ml[part0 + j * step];
+    const floatx4 v = *reinterpret_cast<const floatx4*>(a.part_o + (part0 + j * step) * D + e);
+    if (ml.x == -INFINITY) { l = top == -INFINITY ? l + ml.y : l; continue; }
+    const float f = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
+    l += f * ml.y;
+    o += f * v;
+  }
+  *reinterpret_cast<floatx4*>(&s_o[group][e]) = o;
+  if (e == 0) s_l[group] = l;
+  __syncthreads();
+  if (group > 0) return;
+#pragma unroll
+  for (int j = 1; j < kGroups; ++j) {
+    l += s_l[j];
+    o += *reinterpret_cast<const floatx4*>(&s_o[j][e]);
+  }
+  const int i = row / a.G;
+  const int64_t out = (a.list ? unit.x : (int64_t)unit.x * a.n_q + i) * a.H + g * a.G + (row - i * a.G);
+  const bool nothing = top == -INFINITY && l == 0.f;
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int y = 0; y < 4; ++y) o[y] = nothing ? 0.f : o[y] * inv;
+  T* dst = static_cast<T*>(a.o) + out * D + e;
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(dst) = u32x2{cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3])};
+  else *reinterpret_cast<floatx4*>(dst) = o;
+  if (a.lse && e == 0) a.lse[out] = nothing ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <typename T, int D>
+qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t st) {
+  const int64_t blocks = d.max_units * d.inner, joins = (int64_t)d.contexts * d.inner * a.part_rows;
+  if (blocks > 0x7fffffff || joins > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page attention: too many rows");
+  const dim3 grid((unsigned)blocks), block(kThreads);
+#define QCF_LAUNCH(RT, MODE) page_attn_kernel<T, D, RT, MODE><<<grid, block, 0, st>>>(a)
+#define QCF_ROWS(MODE) do { if (d.row_tiles == 1) QCF_LAUNCH(1, MODE); else QCF_LAUNCH(2, MODE); } while (0)
+  if (a.list) QCF_ROWS(kList);
+  else if (a.n_q == 1) QCF_ROWS(kOne);
+  else QCF_ROWS(kSeveral);
+#undef QCF_ROWS
+#undef QCF_LAUNCH
+  QCF_TRY_LAUNCH("page attention");
+  if (!pages::divides(d)) return QCF_OK;
+  page_join_kernel<T, D><<<dim3((unsigned)joins), dim3(256), 0, st>>>(a);
+  return check_launch("page attention join");
 }
 
 }  // namespace
 
-size_t page_attn_workspace(const qcf_layer_desc&, const qcf_page_cache&, int32_t, int32_t, int32_t) { return 0; }
+size_t page_attn_workspace(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, int32_t n_keep) {
+  return pages::workspace(L, pages::divide(L, c, B, n_q, n_keep));
+}
 
 qcf_status launch_page_attn(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, const void* q,
-                            const int32_t* seen, const int32_t* pages, int32_t n_keep, void* o, float* lse, void*,
+                            const int32_t* seen, const int32_t* list, int32_t n_keep, void* o, float* lse, void* ws,
                             hipStream_t st) {
+  const pages::Division d = pages::divide(L, c, B, n_q, n_keep);
   PageAttnArgs a;
-  a.c = c; a.q = q; a.seen = seen; a.pages = pages; a.n_keep = n_keep;
-  a.B = B; a.n_q = n_q; a.H = L.n_q_heads; a.Hkv = L.n_kv_heads;
+  a.c = c; a.q = q; a.seen = seen; a.list = list; a.n_keep = n_keep;
+  a.n_q = n_q; a.H = L.n_q_heads; a.Hkv = L.n_kv_heads; a.G = a.H / a.Hkv;
   a.log2_page = __builtin_ctz((unsigned)c.page_size);
+  a.contexts = d.contexts; a.rows = d.rows; a.row_blocks = d.row_blocks; a.inner = d.inner; a.slots = d.slots;
+  a.part_rows = pages::part_rows(d);
+  a.scale = (float)(1.4426950408889634 / std::sqrt((double)L.head_dim));
   a.o = o; a.lse = lse;
-  const dim3 grid((unsigned)((int64_t)B * n_q * L.n_q_heads)), block(kThreads);
-  if (L.dtype == QCF_DTYPE_BF16) {
-    if (L.head_dim == 128) page_attn_kernel<bf16_t, 128><<<grid, block, 0, st>>>(a);
-    else page_attn_kernel<bf16_t, 64><<<grid, block, 0, st>>>(a);
-  } else {
-    if (L.head_dim == 128) page_attn_kernel<float, 128><<<grid, block, 0, st>>>(a);
-    else page_attn_kernel<float, 64><<<grid, block, 0, st>>>(a);
-  }
-  return check_launch("page attention");
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + (pages::divides(d) ? pages::sums_bytes(L, d) : 0));
+  if (L.dtype == QCF_DTYPE_BF16) return L.head_dim == 128 ? launch<bf16_t, 128>(a, d, st) : launch<bf16_t, 64>(a, d, st);
+  return L.head_dim == 128 ? launch<float, 128>(a, d, st) : launch<float, 64>(a, d, st);
 }
 
 }  // namespace qcf
