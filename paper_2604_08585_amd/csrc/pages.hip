@@ -28,7 +28,6 @@ struct AppendArgs {
 
 // (cos, sin) of `positions` times a frequency given in turns per position.  The product is rounded at 2^-53 of up to 2^31
 // turns; its fraction is exact in float64 and loses less than 2^-25 of a turn as a float.
-template <typename T>
 __device__ __forceinline__ float2 turn_at(double positions, double turns) {
   const double t = positions * turns;
   const float f = (float)(t - __builtin_rint(t));
@@ -43,159 +42,250 @@ __device__ __forceinline__ float largest(float a, float b) { return __builtin_el
 
 // Request of a unit: units of request b start at row_off[b] / page + 2 b, which leaves room for every page that its rows can touch
 // (n rows touch at most floor((n - 1) / page) + 2), so that no sum over the requests stands in front of the rows.  Every wave
-// counts the requests that start at or before the unit.
-__device__ __forceinline__ int request_of(const AppendArgs& a, int64_t unit, int lane) {
-  int before = 0;
-  for (int b0 = 1; b0 < a.B; b0 += 64) {
+// counts the requests that start at or before the unit; offsets and lengths of the first 64 are on their way together.
+struct Request {
+  int b;
+  int64_t r0, r1, len, unit0;     // its rows, the tokens that it holds, its first unit
+};
+__device__ __forceinline__ Request request_of(const AppendArgs& a, int64_t unit, int lane) {
+  auto clamped = [&](int64_t off) { return min(max(off, (int64_t)0), a.total_rows); };
+  auto first = [&](int b, int64_t off) { return (off >> a.log2_page) + 2 * (int64_t)b; };
+  const int mine = min(lane, a.B - 1);
+  const int64_t off = clamped(a.row_off[mine]), next = clamped(a.row_off[mine + 1]);
+  const int len = a.len[mine];
+  int before = (int)__popcll(__ballot(lane >= 1 && lane < a.B && first(lane, off) <= unit));
+  for (int b0 = 64; b0 < a.B; b0 += 64) {
     const int b = b0 + lane;
-    const int64_t off = a.row_off[min(b, a.B - 1)];
-    const int64_t first = (min(max(off, (int64_t)0), a.total_rows) >> a.log2_page) + 2 * (int64_t)b;
-    before += (int)__popcll(__ballot(b < a.B && first <= unit));
+    const int64_t o = clamped(a.row_off[min(b, a.B - 1)]);
+    before += (int)__popcll(__ballot(b < a.B && first(b, o) <= unit));
   }
-  return before;
+  Request r;
+  r.b = before;
+  if (before < 64) {
+    // (rows are at most 2^30)
+    r.r0 = __builtin_amdgcn_readlane((int)off, before);
+    r.r1 = __builtin_amdgcn_readlane((int)next, before);
+    r.len = __builtin_amdgcn_readlane(len, before);
+  } else {
+    r.r0 = clamped(a.row_off[before]);
+    r.r1 = clamped(a.row_off[before + 1]);
+    r.len = a.len[before];
+  }
+  r.r1 = max(r.r1, r.r0);
+  r.unit0 = first(before, r.r0);
+  return r;
 }
 
-// One workgroup per (page that gets rows, KV head): its keys, turned and rounded, their bounds, its values, and the queries of
-// the head's group.  A thread takes VEC rotary pairs of a row, two 16-byte vectors.
+// One workgroup per (page that gets rows, `heads` KV heads of it): their keys, turned and rounded, the bounds, the values, and the
+// queries of the heads' groups.  A thread takes VEC rotary pairs of a row, two 16-byte vectors.  The (cos, sin) of 16 rows are kept
+// in LDS for all heads: formed for every vector anew they took the vector unit longer than the rows took memory (32K rows, 8
+// KV heads of 128: 238 us, 165 with them).
 template <typename T, int D, int STYLE>
-__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Turns turns) {
-  constexpr int VEC = Elem<T>::kVec, TPR = D / 2 / VEC, SLOTS = kThreads / TPR, WAVES = kThreads / 64;
-  __shared__ float s_lo[WAVES][D], s_hi[WAVES][D];
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Turns turns, int heads, int log2_lanes) {
+  constexpr int VEC = Elem<T>::kVec, TPR = D / 2 / VEC, WAVES = kThreads / 64, PAIRS = D / 2, ROWS = 16;
+  __shared__ __align__(16) float2 s_turn[ROWS][PAIRS];
+  __shared__ float s_bound[2][WAVES][64 / TPR][D];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t unit = blockIdx.x / a.Hkv;
-  const int g = (int)(blockIdx.x - unit * a.Hkv), G = a.H / a.Hkv;
-  const int b = request_of(a, unit, lane);
-  const int64_t r0 = min(max(a.row_off[b], (int64_t)0), a.total_rows);
-  const int64_t r1 = min(max(a.row_off[b + 1], r0), a.total_rows);
-  const int64_t len = a.len[b], page = a.c.page_size;
-  const int64_t p = (len >> a.log2_page) + unit - ((r0 >> a.log2_page) + 2 * (int64_t)b);
-  const int64_t t0 = max(p * page, len), t1 = min((p + 1) * page, len + (r1 - r0));
+  const int parts = a.Hkv / heads;
+  const int64_t unit = blockIdx.x / parts;
+  const int g0 = (int)(blockIdx.x - unit * parts) * heads, G = a.H / a.Hkv;
+  const Request rq = request_of(a, unit, lane);
+  const int64_t page = a.c.page_size, len = rq.len;
+  const int64_t p = (len >> a.log2_page) + unit - rq.unit0;
+  const int64_t t0 = max(p * page, len), t1 = min((p + 1) * page, len + (rq.r1 - rq.r0));
   if (t0 >= t1) return;
   const int n = (int)(t1 - t0);
-  const int64_t row0 = r0 + (t0 - len);
-  const int64_t phys = p >= 0 && p < a.c.max_pages ? a.c.table[(int64_t)b * a.c.max_pages + p] : -1;
+  const int64_t row0 = rq.r0 + (t0 - len);
+  const int64_t phys = p >= 0 && p < a.c.max_pages ? a.c.table[(int64_t)rq.b * a.c.max_pages + p] : -1;
   const bool there = phys >= 0 && phys < a.c.n_pages;
   const int slot0 = (int)(t0 - p * page);
-  const int64_t at = there ? phys * a.c.page_stride + g * a.c.head_stride + slot0 * a.c.slot_stride : 0;
+  const int64_t at = there ? phys * a.c.page_stride + slot0 * a.c.slot_stride : 0;
 
-  const int i0 = tid % TPR * VEC;                       // first pair
-  const int e0 = STYLE == 0 ? i0 : 2 * i0, e1 = STYLE == 0 ? i0 + D / 2 : 2 * i0 + VEC;
-  auto turned = [&](const T* src, int64_t row, u32x4& ra, u32x4& rb) {
-    ra = *reinterpret_cast<const u32x4*>(src + e0);
-    rb = *reinterpret_cast<const u32x4*>(src + e1);
+  // columns of a thread's pairs in a head; tid = (row, head, place in the head)
+  const int place = tid % TPR, i0 = place * VEC;
+  const int e0 = STYLE == 0 ? i0 : 2 * i0, e1 = STYLE == 0 ? i0 + PAIRS : 2 * i0 + VEC;
+  auto turned = [&](int j, u32x4& ra, u32x4& rb) {
     if (!a.pos) return;
-    const double pos = (double)a.pos[row];
     float f[2 * VEC], o[2 * VEC];
     Vec16<T>::unpack(ra, f);
     Vec16<T>::unpack(rb, f + VEC);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
       const int ia = STYLE == 0 ? i : 2 * i, ib = STYLE == 0 ? i + VEC : 2 * i + 1;
-      turn_pair(f[ia], f[ib], turn_at<T>(pos, turns.of[i0 + i]), o[ia], o[ib]);
+      turn_pair(f[ia], f[ib], s_turn[j][i0 + i], o[ia], o[ib]);
     }
     ra = Vec16<T>::pack(o);
     rb = Vec16<T>::pack(o + VEC);
   };
+  const int slots = kThreads >> log2_lanes, slot = tid >> log2_lanes;          // rows side by side; heads * TPR threads to a row
+  const int head = (tid & ((1 << log2_lanes) - 1)) / TPR;
+  float lo[2 * VEC], hi[2 * VEC];
+#pragma unroll
+  for (int e = 0; e < 2 * VEC; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
+  const T* k = static_cast<const T*>(a.k) + row0 * a.k_stride + (g0 + head) * D;
+  const T* v = static_cast<const T*>(a.v) + row0 * a.v_stride + (g0 + head) * D;
+  T* kc = static_cast<T*>(a.c.k) + at + (g0 + head) * a.c.head_stride;
+  T* vc = static_cast<T*>(a.c.v) + at + (g0 + head) * a.c.head_stride;
+  const int q_heads = heads * G, q_vecs = q_heads * TPR;
+  const T* q = static_cast<const T*>(a.q) + row0 * a.q_stride + g0 * G * D;
+  T* q_out = static_cast<T*>(a.q_out) + (row0 * a.H + g0 * G) * D;
 
-  if (there) {
-    float lo[2 * VEC], hi[2 * VEC];
-#pragma unroll
-    for (int e = 0; e < 2 * VEC; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
-    const T* k = static_cast<const T*>(a.k) + row0 * a.k_stride + g * D;
-    const T* v = static_cast<const T*>(a.v) + row0 * a.v_stride + g * D;
-    T* kc = static_cast<T*>(a.c.k) + at;
-    T* vc = static_cast<T*>(a.c.v) + at;
-    for (int j = tid / TPR; j < n; j += SLOTS) {
-      u32x4 ra, rb;
-      turned(k + j * a.k_stride, row0 + j, ra, rb);
-      *reinterpret_cast<u32x4*>(kc + j * a.c.slot_stride + e0) = ra;
-      *reinterpret_cast<u32x4*>(kc + j * a.c.slot_stride + e1) = rb;
-      *reinterpret_cast<u32x4*>(vc + j * a.c.slot_stride + e0) = *reinterpret_cast<const u32x4*>(v + j * a.v_stride + e0);
-      *reinterpret_cast<u32x4*>(vc + j * a.c.slot_stride + e1) = *reinterpret_cast<const u32x4*>(v + j * a.v_stride + e1);
-      float f[2 * VEC];
-      Vec16<T>::unpack(ra, f);
-      Vec16<T>::unpack(rb, f + VEC);
-#pragma unroll
-      for (int e = 0; e < 2 * VEC; ++e) { lo[e] = least(lo[e], f[e]); hi[e] = largest(hi[e], f[e]); }
-    }
-    if (a.c.bounds) {
-#pragma unroll
-      for (int x = TPR; x < 64; x *= 2)
-#pragma unroll
-        for (int e = 0; e < 2 * VEC; ++e) {
-          lo[e] = least(lo[e], __shfl_xor(lo[e], x, 64));
-          hi[e] = largest(hi[e], __shfl_xor(hi[e], x, 64));
-        }
-      if (lane < TPR) {
-#pragma unroll
-        for (int e = 0; e < 2 * VEC; ++e) {
-          const int col = e < VEC ? e0 + e : e1 + e - VEC;
-          s_lo[wave][col] = lo[e];
-          s_hi[wave][col] = hi[e];
-        }
+  for (int j0 = 0; j0 < n; j0 += ROWS) {
+    const int rows = min(n - j0, ROWS);
+    if (a.pos) {
+      if (j0 > 0) __syncthreads();
+      for (int item = tid; item < rows * PAIRS; item += kThreads) {
+        const int j = item / PAIRS, i = item % PAIRS;
+        s_turn[j][i] = turn_at((double)a.pos[row0 + j0 + j], turns.of[i]);
       }
-      __syncthreads();                                  // (by all threads: `there` is the workgroup's)
-      for (int col = tid; col < 2 * D; col += kThreads) {
-        T* bound = static_cast<T*>(a.c.bounds) + (phys * a.Hkv + g) * 2 * D + col;
-        const bool low = col < D;
-        float x = low ? s_lo[0][col] : s_hi[0][col - D];
+      __syncthreads();
+    }
+    if (there) {
+      for (int j = slot; j < rows; j += slots) {
+        const int64_t r = j0 + j;
+        u32x4 ka = *reinterpret_cast<const u32x4*>(k + r * a.k_stride + e0), kb = *reinterpret_cast<const u32x4*>(k + r * a.k_stride + e1);
+        const u32x4 va = *reinterpret_cast<const u32x4*>(v + r * a.v_stride + e0), vb = *reinterpret_cast<const u32x4*>(v + r * a.v_stride + e1);
+        turned(j, ka, kb);
+        *reinterpret_cast<u32x4*>(kc + r * a.c.slot_stride + e0) = ka;
+        *reinterpret_cast<u32x4*>(kc + r * a.c.slot_stride + e1) = kb;
+        *reinterpret_cast<u32x4*>(vc + r * a.c.slot_stride + e0) = va;
+        *reinterpret_cast<u32x4*>(vc + r * a.c.slot_stride + e1) = vb;
+        float f[2 * VEC];
+        Vec16<T>::unpack(ka, f);
+        Vec16<T>::unpack(kb, f + VEC);
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) x = low ? least(x, s_lo[w][col]) : largest(x, s_hi[w][col - D]);
-        if (slot0 > 0) {
-          const float old = Elem<T>::load(bound);
-          x = low ? least(x, old) : largest(x, old);
-        }
-        Elem<T>::store(bound, x);
+        for (int e = 0; e < 2 * VEC; ++e) { lo[e] = least(lo[e], f[e]); hi[e] = largest(hi[e], f[e]); }
+      }
+    }
+    if (a.q) {
+      for (int item = tid; item < rows * q_vecs; item += kThreads) {             // (kThreads is a multiple of TPR: the place stays)
+        const int j = item / q_vecs, h = (item - j * q_vecs) / TPR;
+        const int64_t r = j0 + j;
+        const T* src = q + r * a.q_stride + h * D;
+        u32x4 ra = *reinterpret_cast<const u32x4*>(src + e0), rb = *reinterpret_cast<const u32x4*>(src + e1);
+        turned(j, ra, rb);
+        T* out = q_out + (r * a.H + h) * D;
+        *reinterpret_cast<u32x4*>(out + e0) = ra;
+        *reinterpret_cast<u32x4*>(out + e1) = rb;
       }
     }
   }
-  if (a.q) {
-    for (int item = tid / TPR; item < n * G; item += SLOTS) {
-      const int j = item / G, h = g * G + item - j * G;
-      const int64_t row = row0 + j;
-      u32x4 ra, rb;
-      turned(static_cast<const T*>(a.q) + row * a.q_stride + h * D, row, ra, rb);
-      T* out = static_cast<T*>(a.q_out) + (row * a.H + h) * D;
-      *reinterpret_cast<u32x4*>(out + e0) = ra;
-      *reinterpret_cast<u32x4*>(out + e1) = rb;
+  if (!there || !a.c.bounds) return;                      // (of the workgroup)
+  for (int x = 1 << log2_lanes; x < 64; x *= 2)
+#pragma unroll
+    for (int e = 0; e < 2 * VEC; ++e) {
+      lo[e] = least(lo[e], __shfl_xor(lo[e], x, 64));
+      hi[e] = largest(hi[e], __shfl_xor(hi[e], x, 64));
     }
+  if (lane >> log2_lanes == 0) {
+#pragma unroll
+    for (int e = 0; e < 2 * VEC; ++e) {
+      const int col = e < VEC ? e0 + e : e1 + e - VEC;
+      s_bound[0][wave][head][col] = lo[e];
+      s_bound[1][wave][head][col] = hi[e];
+    }
+  }
+  __syncthreads();
+  T* bounds = static_cast<T*>(a.c.bounds) + (phys * a.Hkv + g0) * 2 * D;
+  for (int item = tid; item < heads * 2 * D; item += kThreads) {
+    const int h = item / (2 * D), col = item % D;
+    const bool low = item % (2 * D) < D;
+    const float(*b)[64 / TPR][D] = s_bound[low ? 0 : 1];
+    float x = b[0][h][col];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) x = low ? least(x, b[w][h][col]) : largest(x, b[w][h][col]);
+    if (slot0 > 0) {
+      const float old = Elem<T>::load(bounds + item);
+      x = low ? least(x, old) : largest(x, old);
+    }
+    Elem<T>::store(bounds + item, x);
   }
 }
 
-// Scores of pages (the definition is in qcf_pages.h): one wave per (page, row, KV head).  Products of two stored values are exact
-// in float64 and so, for values within 2^29 of each other, are their sums: the order of the sum does not decide between pages.
+// Scores of pages (the definition is in qcf_pages.h), 16 pages to a wave, in float64 products of 4 pages x 4 queries x 4 elements,
+// four of them side by side: score = sum of min(q, 0) lo + max(q, 0) hi.  Products of two stored bf16 values are exact in float64,
+// and so are their sums where the terms are within 2^37 of each other: the order of the sum does not decide between pages.
+// Bound by memory (512 bytes to a page and KV head of 128) and, close behind, by turning its values into float64.  A lane has
+// page lane % 16 and every fourth 16-byte vector of its bounds; of the result, query lane % 4 and page 4 (lane / 4 % 4) + lane / 16.
+constexpr int kScorePages = 16;
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void page_score_kernel(qcf_page_cache c, const T* __restrict__ q,
-                                                              const int32_t* __restrict__ seen, int n_q, int H, int Hkv,
-                                                              int log2_page, float* __restrict__ score) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = blockIdx.y;                       // (request, new row)
-  const int b = (int)(row / n_q), G = H / Hkv;
-  const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int g = (int)(item % Hkv);
-  const int64_t p = item / Hkv;
-  const int count = (int)(((int64_t)max(seen[row], 0) + c.page_size - 1) >> log2_page);
-  if (p >= min(count, c.max_pages)) return;
-  const int phys = c.table[(int64_t)b * c.max_pages + p];
-  float best = -INFINITY;
-  if (phys >= 0 && phys < c.n_pages) {
-    const T* lo = static_cast<const T*>(c.bounds) + ((int64_t)phys * Hkv + g) * 2 * D;
-    for (int h = 0; h < G; ++h) {
-      const T* x = q + (row * H + g * G + h) * D;
-      double sum = 0.0;
+__global__ __launch_bounds__(kThreads, 2) void page_score_kernel(qcf_page_cache c, const T* __restrict__ q,
+                                                                 const int32_t* __restrict__ seen, int n_q, int H, int Hkv,
+                                                                 int log2_page, int chunks, int chunk, float* __restrict__ score) {
+  constexpr int VEC = Elem<T>::kVec, LOADS = D / (4 * VEC), STEP = kScorePages * kThreads / 64;
+  constexpr bool AHEAD = sizeof(T) == 2;                // the next pages' bounds are on their way (float32: no registers for them)
+  const int lane = threadIdx.x & 63, quad = lane >> 4, col = lane & 15, j = lane & 3;
+  const int g = (int)(blockIdx.x % Hkv), G = H / Hkv;
+  const int64_t rest = blockIdx.x / Hkv, row = rest / chunks;           // (request, new row)
+  const int64_t b = row / n_q;
+  const int count = (int)min(((int64_t)max(seen[row], 0) + c.page_size - 1) >> log2_page, (int64_t)c.max_pages);
+  const int first = (int)(rest - row * chunks) * chunk, end = min(count, first + chunk);
+  const int p0 = first + kScorePages * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (p0 >= end) return;
+  const int32_t* table = c.table + b * c.max_pages;
+  float* out = score + (row * Hkv + g) * c.max_pages;
+  const T* bounds = static_cast<const T*>(c.bounds);
+  for (int h0 = 0; h0 < G; h0 += 4) {                   // four queries at a time
+    double up[LOADS * VEC], down[LOADS * VEC];
+    const T* x = q + (row * H + g * G + min(h0 + j, G - 1)) * D;
 #pragma unroll
-      for (int e = lane; e < D; e += 64) {
-        const double f = (double)Elem<T>::load(x + e);
-        sum += fmin(f, 0.0) * (double)Elem<T>::load(lo + e) + fmax(f, 0.0) * (double)Elem<T>::load(lo + D + e);
-        if (f != f) sum = f;
+    for (int f = 0; f < LOADS; ++f) {
+      float v[VEC];
+      Vec16<T>::unpack(*reinterpret_cast<const u32x4*>(x + (4 * f + quad) * VEC), v);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        up[f * VEC + e] = v[e] < 0.f ? 0.0 : (double)v[e];
+        down[f * VEC + e] = v[e] > 0.f ? 0.0 : (double)v[e];
       }
+    }
+    u32x4 lo[LOADS], hi[LOADS], next_lo[LOADS], next_hi[LOADS];
+    auto entry = [&](int p) { return p + col < end ? table[p + col] : -1; };
+    auto load = [&](int phys, u32x4 (&l)[LOADS], u32x4 (&h)[LOADS]) {
+      const T* src = bounds + ((int64_t)(phys >= 0 && phys < c.n_pages ? phys : 0) * Hkv + g) * 2 * D + quad * VEC;
 #pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 64);
-      const float s = (float)sum;
-      best = fmaxf(best, s == s ? fmaxf(s, -3.402823466e38f) : INFINITY);
+      for (int f = 0; f < LOADS; ++f) {
+        l[f] = *reinterpret_cast<const u32x4*>(src + 4 * f * VEC);
+        h[f] = *reinterpret_cast<const u32x4*>(src + D + 4 * f * VEC);
+      }
+    };
+    auto there = [&](int phys) { return __ballot(phys >= 0 && phys < c.n_pages); };
+    int phys = entry(p0), next = entry(p0 + STEP);
+    load(phys, lo, hi);
+    for (int p = p0; p < end; p += STEP) {
+      const uint64_t mask = there(phys);
+      if (AHEAD && p + STEP < end) load(next, next_lo, next_hi);
+      double a0 = 0.0, a1 = 0.0;
+#pragma unroll
+      for (int f = 0; f < LOADS; ++f) {
+        float l[VEC], h[VEC];
+        Vec16<T>::unpack(lo[f], l);
+        Vec16<T>::unpack(hi[f], h);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          a0 = __builtin_amdgcn_mfma_f64_4x4x4f64((double)l[e], down[f * VEC + e], a0, 0, 0, 0);
+          a1 = __builtin_amdgcn_mfma_f64_4x4x4f64((double)h[e], up[f * VEC + e], a1, 0, 0, 0);
+        }
+      }
+      const float sum = (float)(a0 + a1);
+      float s = sum == sum ? fmaxf(sum, -3.402823466e38f) : INFINITY;   // (the least float: above pages that are not there)
+      if (h0 + j >= G) s = -INFINITY;
+      s = fmaxf(s, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(s), 0xb1, 0xf, 0xf, false)));    // the four queries
+      s = fmaxf(s, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(s), 0x4e, 0xf, 0xf, false)));
+      const int mine = 4 * (lane >> 2 & 3) + quad;
+      if (j == 0 && p + mine < end) {
+        s = mask >> mine & 1 ? s : -INFINITY;
+        out[p + mine] = h0 > 0 ? fmaxf(out[p + mine], s) : s;           // (written by this lane)
+      }
+      phys = next;
+      if (AHEAD) {
+#pragma unroll
+        for (int f = 0; f < LOADS; ++f) { lo[f] = next_lo[f]; hi[f] = next_hi[f]; }
+      } else if (p + STEP < end) {
+        load(next, lo, hi);
+      }
+      next = entry(p + 2 * STEP);
     }
   }
-  if (lane == 0) score[(row * Hkv + g) * c.max_pages + p] = best;
 }
 
 }  // namespace
@@ -213,9 +303,17 @@ qcf_status launch_page_append(const qcf_layer_desc& L, const qcf_page_cache& c, 
   Turns turns;
   const double log2_base = std::log2(L.rope_base);
   for (int i = 0; i < L.head_dim / 2; ++i) turns.of[i] = std::exp2(-2.0 * i / L.head_dim * log2_base) * 0.15915494309189533577;
-  const int64_t blocks = ((total_rows >> a.log2_page) + 2 * (int64_t)B) * L.n_kv_heads;
+  // KV heads of a workgroup: a power of two of them, whose vectors of a row fill a wave at most, as long as every compute unit
+  // has two workgroups.  More share their (cos, sin), fewer give a short call more workgroups (@).
+  const int64_t units = (total_rows >> a.log2_page) + 2 * (int64_t)B;
+  const int per_row = L.head_dim / 2 / (16 / elem_size(L.dtype));
+  int heads = 1;
+  while (L.n_kv_heads % (2 * heads) == 0 && 2 * heads * per_row <= 64 && units * (L.n_kv_heads / (2 * heads)) >= 2 * compute_unit_count())
+    heads *= 2;
+  const int log2_lanes = __builtin_ctz((unsigned)(heads * per_row));
+  const int64_t blocks = units * (L.n_kv_heads / heads);
   if (blocks > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page append: too many rows");
-#define QCF_LAUNCH(T, D, S) append_kernel<T, D, S><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, turns)
+#define QCF_LAUNCH(T, D, S) append_kernel<T, D, S><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, turns, heads, log2_lanes)
 #define QCF_STYLE(T, D) do { if (L.rope_style == 0) QCF_LAUNCH(T, D, 0); else QCF_LAUNCH(T, D, 1); } while (0)
   if (L.dtype == QCF_DTYPE_BF16) {
     if (L.head_dim == 128) QCF_STYLE(bf16_t, 128); else QCF_STYLE(bf16_t, 64);
@@ -235,13 +333,17 @@ qcf_status launch_page_select(const qcf_layer_desc& L, const qcf_page_cache& c, 
                               const int32_t* seen, int32_t n_keep, int32_t n_first, int32_t n_last, int32_t* pages, void* ws,
                               hipStream_t st) {
   float* score = static_cast<float*>(ws);
-  const int64_t rows = (int64_t)B * n_q, items = (int64_t)c.max_pages * L.n_kv_heads, blocks = (items + 3) / 4;
-  if (rows * L.n_kv_heads > 0x7fffffff || blocks > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page select: too many rows");
-  const int log2_page = __builtin_ctz((unsigned)c.page_size);
-  if (rows > 65535) return fail(QCF_ERR_UNSUPPORTED, "page select: %lld rows > 65535", (long long)rows);
-#define QCF_LAUNCH(T, D)                                                                                                  \
-  page_score_kernel<T, D><<<dim3((unsigned)blocks, (unsigned)rows), dim3(kThreads), 0, st>>>(c, static_cast<const T*>(q), \
-                                                                                              seen, n_q, L.n_q_heads, L.n_kv_heads, log2_page, score)
+  const int64_t rows = (int64_t)B * n_q, tiles = ((int64_t)c.max_pages + 4 * kScorePages - 1) / (4 * kScorePages);
+  // tiles of 4 waves x 16 pages of a workgroup: up to four, as long as every compute unit has two workgroups (the queries are laid
+  // out once for them)
+  int64_t each = rows * L.n_kv_heads * tiles / (2 * compute_unit_count());
+  each = std::min<int64_t>(std::max<int64_t>(each, 1), 4);
+  const int64_t chunks = (tiles + each - 1) / each, blocks = rows * L.n_kv_heads * chunks;
+  if (blocks > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page select: too many rows");
+  const int log2_page = __builtin_ctz((unsigned)c.page_size), chunk = (int)(each * 4 * kScorePages);
+#define QCF_LAUNCH(T, D)                                                                                              \
+  page_score_kernel<T, D><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(c, static_cast<const T*>(q), seen, n_q,  \
+                                                                             L.n_q_heads, L.n_kv_heads, log2_page, (int)chunks, chunk, score)
   if (L.dtype == QCF_DTYPE_BF16) {
     if (L.head_dim == 128) QCF_LAUNCH(bf16_t, 128); else QCF_LAUNCH(bf16_t, 64);
   } else {
