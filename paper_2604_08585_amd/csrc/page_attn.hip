@@ -1,7 +1,7 @@
 // Attention of the newest tokens over a cache in pages.
 //
-// One pass over the keys and values with a running reference point and sum of each row's softmax.  A context is divided into
-// units of equal length, as many as the GPU holds at once, which partial results of rows that have several join in a second launch.
+// One pass over the keys and values with a running reference point and sum of each row's softmax.  The contexts are divided into
+// equal ranges, as many as the GPU holds at once; a second launch joins the partial results of contexts that several ranges have.
 // Bound by memory: 4 d operations to a token and row against 4 d bytes (bf16) to a token and KV head, 4 to 64 a byte.
 //
 // A wave takes 32 tokens (16 in float32) at a time, without LDS: the logits are products K Q^T of 16 tokens x 16 rows, so a lane
@@ -52,53 +52,60 @@ __device__ __forceinline__ int64_t context_tokens(const PageAttnArgs& a, int x) 
   return min((int64_t)seen, most);
 }
 
-__device__ __forceinline__ int64_t wave_add(int64_t x) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
-  return x;
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
 }
-__device__ __forceinline__ int wave_incl(int x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d, 64);
-    x += lane >= d ? y : 0;
-  }
-  return x;
+// Inclusive sum over the lanes of a wave: within rows (row_shr), then across them (row_bcast).
+__device__ __forceinline__ uint32_t wave_incl(uint32_t x) {
+  x += dpp<0x111>(x); x += dpp<0x112>(x); x += dpp<0x114>(x); x += dpp<0x118>(x);
+  x += dpp<0x142, 0xa>(x);
+  return x + dpp<0x143, 0xc>(x);
 }
+__device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 
-struct Unit {
-  int x;                   // context (-1: no such unit)
-  int first, count;        // its first unit, and the number of its units
-  int64_t tokens, step;    // of the context, of a unit
+// The contexts in grains, end to end.  Every wave works them out by itself; the first 64 stay in its lanes.
+struct Contexts {
+  uint32_t tokens, grains, incl;       // of context `lane` (64 of at most 2^25 grains: below 2^31)
+  int64_t range;                       // grains of a range
+};
+struct Place {
+  int x;                               // context
+  int64_t start, grains;               // its first grain, and how many it has
 };
 
-// Every wave works the division out by itself, from the tokens of all contexts (of=false: the context of unit u; of=true: the units
-// of context u).
-__device__ __forceinline__ Unit find_unit(const PageAttnArgs& a, int64_t u, bool of, int lane) {
-  int64_t total = 0;
-  for (int x0 = 0; x0 < a.contexts; x0 += 64) total += x0 + lane < a.contexts ? context_tokens(a, x0 + lane) : 0;
-  total = wave_add(total);
-  Unit r;
-  r.step = pages::unit_tokens(total, a.slots);
-  int before = 0;
+__device__ __forceinline__ Contexts contexts_of(const PageAttnArgs& a, int lane) {
+  Contexts c;
+  c.tokens = lane < a.contexts ? (uint32_t)context_tokens(a, lane) : 0u;
+  c.grains = lane < a.contexts ? (uint32_t)pages::grains_of(c.tokens) : 0u;
+  c.incl = wave_incl(c.grains);
+  int64_t total = from_lane(c.incl, 63);
+  for (int x0 = 64; x0 < a.contexts; x0 += 64)
+    total += from_lane(wave_incl(x0 + lane < a.contexts ? (uint32_t)pages::grains_of(context_tokens(a, x0 + lane)) : 0u), 63);
+  c.range = pages::range_of(total, a.slots);
+  return c;
+}
+// The context that has a grain (x -1: none has), or context x itself.
+template <bool OF>
+__device__ __forceinline__ Place place_of(const PageAttnArgs& a, const Contexts& c, int64_t grain, int x, int lane) {
+  Place p = {-1, 0, 0};
+  uint32_t n = c.grains, incl = c.incl;
   for (int x0 = 0; x0 < a.contexts; x0 += 64) {
-    const int x = x0 + lane;
-    const int64_t tokens = x < a.contexts ? context_tokens(a, x) : 0;
-    const int n = x < a.contexts ? (int)pages::units_of(tokens, r.step) : 0;
-    const int incl = before + wave_incl(n, lane);
-    const uint64_t hit = __ballot(x < a.contexts && (of ? x == u : u < incl));
+    if (x0 > 0) {
+      n = x0 + lane < a.contexts ? (uint32_t)pages::grains_of(context_tokens(a, x0 + lane)) : 0u;
+      incl = wave_incl(n);
+    }
+    const uint64_t hit = __ballot(n > 0u && (OF ? x0 + lane == x : grain < p.start + incl));
     if (hit) {
       const int l = __builtin_ctzll(hit);
-      r.x = x0 + l;
-      r.count = __builtin_amdgcn_readlane(n, l);
-      r.first = __builtin_amdgcn_readlane(incl, l) - r.count;
-      r.tokens = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)tokens, l);     // (at most 2^30)
-      return r;
+      p.x = x0 + l;
+      p.grains = from_lane(n, l);
+      p.start += from_lane(incl, l) - from_lane(n, l);
+      return p;
     }
-    before = __builtin_amdgcn_readlane(incl, 63);
+    p.start += from_lane(incl, 63);
   }
-  r.x = -1;
-  return r;
+  return p;
 }
 
 // 64 entries of a context's pages, one to a lane, and the tile's part of them.
@@ -125,8 +132,9 @@ struct Walk {
   };
 
   const PageAttnArgs& a;
-  const int lane, quad, col, g, x, b;
-  const int64_t end;                                     // of the unit, in the context's order
+  const int lane, quad, col, g;
+  int x, b;                                              // context, request
+  int64_t end;                                           // of the workgroup's part, in the context's order
   int count;                                             // pages that a row sees (listed pages from there on are none)
   Window w;
   u32x4 q[RT][kLoads];
@@ -136,8 +144,8 @@ struct Walk {
   bool any[RT];
   floatx4 acc[RT][kE];
 
-  __device__ __forceinline__ Walk(const PageAttnArgs& args, int lane_, int g_, int x_, int64_t end_)
-      : a(args), lane(lane_), quad(lane_ >> 4), col(lane_ & 15), g(g_), x(x_), b(MODE == kList ? x_ / args.n_q : x_), end(end_) {}
+  __device__ __forceinline__ Walk(const PageAttnArgs& args, int lane_, int g_)
+      : a(args), lane(lane_), quad(lane_ >> 4), col(lane_ & 15), g(g_) {}
 
   __device__ __forceinline__ void open(int first) {
     w.first = first;
@@ -334,10 +342,31 @@ struct Walk {
     }
   }
 
+  // tiles from token `at` on, every kWaves-th
+  __device__ __forceinline__ void run(int64_t at) {
+    constexpr int kStep = kWaves * kTokens;
+    if (at >= end) return;
+    Tile t0, t1;
+    load(t0, at);
+    while (true) {
+      at += kStep;
+      if (at < end) load(t1, at);
+      step(t0);
+      if (at >= end) return;
+      at += kStep;
+      if (at < end) load(t0, at);
+      step(t1);
+      if (at >= end) return;
+    }
+  }
+
   int row0;                                              // first row of the workgroup
   __device__ __forceinline__ int row_of(int r) const { return row0 + 16 * r + col; }
 
-  __device__ __forceinline__ void start(int first_row, int64_t begin) {
+  __device__ __forceinline__ void start(int context, int first_row, int64_t begin, int64_t end_) {
+    x = context;
+    b = MODE == kList ? x / a.n_q : x;
+    end = end_;
     row0 = first_row;
     const int64_t most = (int64_t)a.c.max_pages << a.log2_page;
     int lo = 0x7fffffff, hi = 0;
@@ -373,37 +402,29 @@ struct Walk {
   }
 };
 
+// One row's result: four elements of its sums over the sum of its weights.
+template <typename T, int D>
+__device__ __forceinline__ void store_row(const PageAttnArgs& a, int x, int g, int row, int e, float top, float l, floatx4 o) {
+  const int i = row / a.G;
+  const int64_t out = (a.list ? x : (int64_t)x * a.n_q + i) * a.H + g * a.G + (row - i * a.G);
+  const bool nothing = top == -INFINITY && l == 0.f;
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int y = 0; y < 4; ++y) o[y] = nothing ? 0.f : o[y] * inv;
+  T* dst = static_cast<T*>(a.o) + out * D + e;
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(dst) = u32x2{cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3])};
+  else *reinterpret_cast<floatx4*>(dst) = o;
+  if (a.lse && e == 0) a.lse[out] = nothing ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Joins the waves of a workgroup: their sums go through LDS, scaled to the largest of their reference points, and leave as rows of
+// the output, or as partial result `part`.
 template <typename T, int D, int RT, int MODE>
-__global__ __launch_bounds__(kThreads, RT == 1 ? 2 : 1) void page_attn_kernel(PageAttnArgs a) {
+__device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MODE>& w, float (&s_o)[kWaves][16 * RT][D + 4],
+                                       float (&s_m)[kWaves][16 * RT], float (&s_l)[kWaves][16 * RT], int in, int row0, int64_t part) {
   typedef Walk<T, D, RT, MODE> W;
   constexpr int kRows = 16 * RT;
-  __shared__ __align__(16) float s_o[kWaves][kRows][D + 4];         // (rows 4 banks apart)
-  __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t u = blockIdx.x / a.inner;
-  const int in = (int)(blockIdx.x - u * a.inner), g = in % a.Hkv, row0 = in / a.Hkv * kRows;
-  const Unit unit = find_unit(a, u, false, lane);
-  if (unit.x < 0) return;
-  const int64_t begin = (u - unit.first) * unit.step, end = min(begin + unit.step, unit.tokens);
-  W w(a, lane, g, unit.x, end);
-  w.start(row0, begin);
-  int64_t at = begin + wave * W::kTokens;
-  constexpr int kStep = kWaves * W::kTokens;
-  if (at < end) {
-    typename W::Tile t0, t1;
-    w.load(t0, at);
-    while (true) {
-      at += kStep;
-      if (at < end) w.load(t1, at);
-      w.step(t0);
-      if (at >= end) break;
-      at += kStep;
-      if (at < end) w.load(t0, at);
-      w.step(t1);
-      if (at >= end) break;
-    }
-  }
-  // join the waves: their sums go through LDS, scaled to the largest of their reference points
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     if (w.lim[r] == 0) { w.m[r] = -INFINITY; w.l[r] = 0.f; w.any[r] = false; }       // (beside rows that see whole tiles)
@@ -442,79 +463,107 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 2 : 1) void page_attn_kernel(Pa
       l += f * li;
       o += f * *reinterpret_cast<const floatx4*>(&s_o[i][r][e]);
     }
-    if (unit.count > 1) {
-      const int64_t part = (u * a.inner + in) * a.part_rows + r;
-      *reinterpret_cast<floatx4*>(a.part_o + part * D + e) = o;
-      if (e == 0) a.part_ml[part] = make_float2(top, l);
+    if (part >= 0) {
+      const int64_t at = (part * a.inner + in) * a.part_rows + r;
+      *reinterpret_cast<floatx4*>(a.part_o + at * D + e) = o;
+      if (e == 0) a.part_ml[at] = make_float2(top, l);
       continue;
     }
-    const int row = row0 + r, i = row / a.G;
-    const int64_t out = ((MODE == kList ? unit.x : (int64_t)unit.x * a.n_q + i) * a.H + g * a.G + (row - i * a.G));
-    const bool nothing = top == -INFINITY && l == 0.f;
-    const float inv = 1.f / l;
-#pragma unroll
-    for (int y = 0; y < 4; ++y) o[y] = nothing ? 0.f : o[y] * inv;
-    T* dst = static_cast<T*>(a.o) + out * D + e;
-    if constexpr (W::kHalf) *reinterpret_cast<u32x2*>(dst) = u32x2{cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3])};
-    else *reinterpret_cast<floatx4*>(dst) = o;
-    if (a.lse && e == 0) a.lse[out] = nothing ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
+    store_row<T, D>(a, w.x, w.g, row0 + r, e, top, l, o);
   }
 }
 
-// Joins the units of a context: one workgroup per (context, KV head and row block, row).
+template <typename T, int D, int RT, int MODE>
+__global__ __launch_bounds__(kThreads, RT == 1 ? 2 : 1) void page_attn_kernel(PageAttnArgs a) {
+  typedef Walk<T, D, RT, MODE> W;
+  constexpr int kRows = 16 * RT;
+  __shared__ __align__(16) float s_o[kWaves][kRows][D + 4];         // (rows 4 banks apart)
+  __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t r = blockIdx.x / a.inner;
+  const int in = (int)(blockIdx.x - r * a.inner), g = in % a.Hkv, row0 = in / a.Hkv * kRows;
+  const Contexts all = contexts_of(a, lane);
+  Place here = place_of<false>(a, all, r * all.range, 0, lane);
+  if (here.x < 0) return;
+  int64_t at = r * all.range;
+  W w(a, lane, g);
+  for (int64_t left = all.range; left > 0;) {
+    const int64_t n = min(left, here.start + here.grains - at);
+    const int64_t tokens = here.x < 64 ? from_lane(all.tokens, here.x) : context_tokens(a, here.x);
+    const int64_t begin = (at - here.start) * pages::kGrain;
+    w.start(here.x, row0, begin, min(begin + n * pages::kGrain, tokens));
+    w.run(begin + wave * W::kTokens);
+    const bool whole = n == here.grains;
+    finish(a, w, s_o, s_m, s_l, in, row0, whole ? -1 : 2 * r + (at == here.start));
+    at += n;
+    left -= n;
+    if (left == 0 || ++here.x >= a.contexts) break;
+    here.start = at;
+    here.grains = here.x < 64 ? (int64_t)from_lane(all.grains, here.x) : pages::grains_of(context_tokens(a, here.x));
+    __syncthreads();                                     // (before the sums in LDS are written again)
+  }
+}
+
+// Joins the parts of a context: one workgroup per (context, KV head and row block, row), or, where there are more contexts than
+// ranges, per range for the context that starts in it and goes on behind it.  A group of threads takes every kGroups-th part.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void page_join_kernel(PageAttnArgs a) {
-  constexpr int kVecs = D / 4, kGroups = 256 / kVecs;    // a group of threads takes every kGroups-th unit
+  constexpr int kVecs = D / 4, kGroups = 256 / kVecs, kAt = 4;
   __shared__ __align__(16) float s_o[kGroups][D];
   __shared__ float s_l[kGroups], s_m[kGroups];
   const int tid = threadIdx.x, lane = tid & 63, group = tid / kVecs, e = tid % kVecs * 4;
   const int r = blockIdx.x % a.part_rows;
-  const int64_t rest = blockIdx.x / a.part_rows;
-  const int in = (int)(rest % a.inner), g = in % a.Hkv, row = in / a.Hkv * a.part_rows + r;
+  const int64_t rest = blockIdx.x / a.part_rows, item = rest / a.inner;
+  const int in = (int)(rest - item * a.inner), row = in / a.Hkv * a.part_rows + r;
   if (row >= a.rows) return;
-  const Unit unit = find_unit(a, rest / a.inner, true, lane);
-  if (unit.count <= 1) return;
-  const int64_t part0 = ((int64_t)unit.first * a.inner + in) * a.part_rows + r, step = (int64_t)a.inner * a.part_rows;
-  float top = -INFINITY;
-  for (int j = group; j < unit.count; j += kGroups) top = fmaxf(top, a.part_ml[part0 + j * step].x);
-  if (e == 0) s_m[group] = top;
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < kGroups; ++j) top = fmaxf(top, s_m[j]);
-  float l = 0.f;
+  const Contexts all = contexts_of(a, lane);
+  const bool few = a.contexts <= a.slots;
+  const Place p = few ? place_of<true>(a, all, 0, (int)item, lane) : place_of<false>(a, all, (item + 1) * all.range - 1, 0, lane);
+  if (p.x < 0) return;
+  auto range_at = [&](int64_t grain) {
+    return (grain | all.range) >> 31 ? grain / all.range : (int64_t)((uint32_t)grain / (uint32_t)all.range);
+  };
+  const int64_t first = range_at(p.start), last = range_at(p.start + p.grains - 1);
+  if (last == first || (!few && first != item)) return;
+  const int count = (int)(last - first) + 1;
+  auto part = [&](int j) { return ((2 * (first + j) + (j == 0)) * a.inner + in) * a.part_rows + r; };
+  float top = -INFINITY, l = 0.f;
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int j = group; j < unit.count; j += kGroups) {
-    const float2 ml = a.part_ml[part0 + j * step];
-    const floatx4 v = *reinterpret_cast<const floatx4*>(a.part_o + (part0 + j * step) * D + e);
-    if (ml.x == -INFINITY) { l = top == -INFINITY ? l + ml.y : l; continue; }
-    const float f = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
-    l += f * ml.y;
-    o += f * v;
+  // part j: (ml, v) beside what there is; what has only logits of -inf weighs nothing beside others, and makes a row NaN alone
+  auto add = [&](float2 ml, floatx4 v) {
+    if (ml.x == -INFINITY) { l = top == -INFINITY ? l + ml.y : l; return; }
+    if (top == -INFINITY) l = 0.f;
+    const float next = fmaxf(top, ml.x);
+    const float f = top == next ? 1.f : __builtin_amdgcn_exp2f(top - next), g = ml.x == next ? 1.f : __builtin_amdgcn_exp2f(ml.x - next);
+    l = l * f + ml.y * g;
+    o = o * f + v * g;
+    top = next;
+  };
+  for (int j0 = group; j0 < count; j0 += kAt * kGroups) {
+    float2 ml[kAt];
+    floatx4 v[kAt];
+#pragma unroll
+    for (int i = 0; i < kAt; ++i) {
+      const int64_t at = part(min(j0 + i * kGroups, count - 1));
+      ml[i] = a.part_ml[at];
+      v[i] = *reinterpret_cast<const floatx4*>(a.part_o + at * D + e);
+    }
+#pragma unroll
+    for (int i = 0; i < kAt; ++i)
+      if (j0 + i * kGroups < count) add(ml[i], v[i]);
   }
   *reinterpret_cast<floatx4*>(&s_o[group][e]) = o;
-  if (e == 0) s_l[group] = l;
+  if (e == 0) { s_l[group] = l; s_m[group] = top; }
   __syncthreads();
   if (group > 0) return;
 #pragma unroll
-  for (int j = 1; j < kGroups; ++j) {
-    l += s_l[j];
-    o += *reinterpret_cast<const floatx4*>(&s_o[j][e]);
-  }
-  const int i = row / a.G;
-  const int64_t out = (a.list ? unit.x : (int64_t)unit.x * a.n_q + i) * a.H + g * a.G + (row - i * a.G);
-  const bool nothing = top == -INFINITY && l == 0.f;
-  const float inv = 1.f / l;
-#pragma unroll
-  for (int y = 0; y < 4; ++y) o[y] = nothing ? 0.f : o[y] * inv;
-  T* dst = static_cast<T*>(a.o) + out * D + e;
-  if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(dst) = u32x2{cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3])};
-  else *reinterpret_cast<floatx4*>(dst) = o;
-  if (a.lse && e == 0) a.lse[out] = nothing ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
+  for (int j = 1; j < kGroups; ++j) add(make_float2(s_m[j], s_l[j]), *reinterpret_cast<const floatx4*>(&s_o[j][e]));
+  store_row<T, D>(a, p.x, in % a.Hkv, row, e, top, l, o);
 }
 
 template <typename T, int D>
 qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t st) {
-  const int64_t blocks = d.max_units * d.inner, joins = (int64_t)d.contexts * d.inner * a.part_rows;
+  const int64_t blocks = (int64_t)d.slots * d.inner, joins = (int64_t)std::min(d.contexts, d.slots) * d.inner * a.part_rows;
   if (blocks > 0x7fffffff || joins > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page attention: too many rows");
   const dim3 grid((unsigned)blocks), block(kThreads);
 #define QCF_LAUNCH(RT, MODE) page_attn_kernel<T, D, RT, MODE><<<grid, block, 0, st>>>(a)
