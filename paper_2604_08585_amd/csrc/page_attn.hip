@@ -14,12 +14,10 @@
 namespace qcf {
 namespace {
 
-using pages::kWaves;
-constexpr int kThreads = 64 * kWaves;
 constexpr float kLn2 = 0.6931471805599453f;
 // A row's reference point moves where a logit is more than 8 above it (in powers of two): weights are up to 256 then, and most
 // tiles neither exchange their maxima nor scale what has been summed.
-constexpr float kAhead = 8.f;
+constexpr float kRoom = 8.f;
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -32,7 +30,7 @@ struct PageAttnArgs {
   const int32_t* seen;
   const int32_t* list;
   int n_keep, n_q, H, Hkv, G, log2_page;
-  int contexts, rows, row_blocks, inner, slots, part_rows;
+  int contexts, rows, inner, slots, least, part_rows;
   float scale;                                           // log2(e) / sqrt(d)
   void* o;
   float* lse;
@@ -48,7 +46,9 @@ __device__ __forceinline__ int64_t context_tokens(const PageAttnArgs& a, int x) 
     return min((seen + a.c.page_size - 1) >> a.log2_page, (int64_t)a.n_keep) << a.log2_page;
   }
   int seen = 0;
-  for (int i = 0; i < a.n_q; ++i) seen = max(seen, a.seen[(int64_t)x * a.n_q + i]);
+  for (int i0 = 0; i0 < a.n_q; i0 += 4)                  // (four loads on their way together)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) seen = max(seen, a.seen[(int64_t)x * a.n_q + min(i0 + i, a.n_q - 1)]);
   return min((int64_t)seen, most);
 }
 
@@ -66,8 +66,10 @@ __device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (ui
 
 // The contexts in grains, end to end.  Every wave works them out by itself; the first 64 stay in its lanes.
 struct Contexts {
-  uint32_t tokens, grains, incl;       // of context `lane` (64 of at most 2^25 grains: below 2^31)
+  uint32_t tokens, grains;             // of context `lane`
+  uint32_t room, incl;                 // grains that it is given, and the sum so far (64 of at most 2^25: below 2^31)
   int64_t range;                       // grains of a range
+  bool apart;                          // no range has two contexts
 };
 struct Place {
   int x;                               // context
@@ -78,29 +80,41 @@ __device__ __forceinline__ Contexts contexts_of(const PageAttnArgs& a, int lane)
   Contexts c;
   c.tokens = lane < a.contexts ? (uint32_t)context_tokens(a, lane) : 0u;
   c.grains = lane < a.contexts ? (uint32_t)pages::grains_of(c.tokens) : 0u;
-  c.incl = wave_incl(c.grains);
+  c.room = c.grains;
+  c.incl = wave_incl(c.room);
+  c.apart = false;
   int64_t total = from_lane(c.incl, 63);
   for (int x0 = 64; x0 < a.contexts; x0 += 64)
     total += from_lane(wave_incl(x0 + lane < a.contexts ? (uint32_t)pages::grains_of(context_tokens(a, x0 + lane)) : 0u), 63);
-  c.range = pages::range_of(total, a.slots);
+  c.range = pages::range_of(total, a.slots, a.least);
+  if (a.contexts <= 64 && c.range == a.least) {
+    // little work: every context begins a range of its own if there are enough of them (two parts in a row take a workgroup
+    // twice the latency: five requests of up to 600 tokens in float32 13.6 us, @ so)
+    const uint32_t room = (c.grains + a.least - 1) & ~(uint32_t)(a.least - 1), incl = wave_incl(room);
+    if (from_lane(incl, 63) <= (uint64_t)a.least * a.slots) {
+      c.room = room;
+      c.incl = incl;
+      c.apart = true;
+    }
+  }
   return c;
 }
 // The context that has a grain (x -1: none has), or context x itself.
 template <bool OF>
 __device__ __forceinline__ Place place_of(const PageAttnArgs& a, const Contexts& c, int64_t grain, int x, int lane) {
   Place p = {-1, 0, 0};
-  uint32_t n = c.grains, incl = c.incl;
+  uint32_t n = c.grains, room = c.room, incl = c.incl;
   for (int x0 = 0; x0 < a.contexts; x0 += 64) {
     if (x0 > 0) {
-      n = x0 + lane < a.contexts ? (uint32_t)pages::grains_of(context_tokens(a, x0 + lane)) : 0u;
-      incl = wave_incl(n);
+      n = room = x0 + lane < a.contexts ? (uint32_t)pages::grains_of(context_tokens(a, x0 + lane)) : 0u;
+      incl = wave_incl(room);
     }
     const uint64_t hit = __ballot(n > 0u && (OF ? x0 + lane == x : grain < p.start + incl));
     if (hit) {
       const int l = __builtin_ctzll(hit);
       p.x = x0 + l;
       p.grains = from_lane(n, l);
-      p.start += from_lane(incl, l) - from_lane(n, l);
+      p.start += from_lane(incl, l) - from_lane(room, l);
       return p;
     }
     p.start += from_lane(incl, 63);
@@ -114,7 +128,7 @@ struct Window {
   int phys, page;          // lane's page: number in the pool (-1: not there), and in the request
 };
 
-template <typename T, int D, int RT, int MODE>
+template <typename T, int D, int RT, int MODE, int WAVES>
 struct Walk {
   static constexpr bool kHalf = sizeof(T) == 2;
   static constexpr int kSub = kHalf ? 2 : 1;             // parts of 16 tokens of a tile; a part lies in one page
@@ -123,6 +137,7 @@ struct Walk {
   static constexpr int kE = D / 16;                                    // 16-element slices of the output
   static constexpr int kV = kHalf ? 8 : 4 * (D / 64);                  // value loads of a lane
   static constexpr int kVWords = kHalf && D == 64 ? 2 : 4;
+  static constexpr int kStep = WAVES * kTokens;                        // tokens that the workgroup's waves take side by side
   typedef uint32_t vec_v __attribute__((ext_vector_type(kVWords)));
 
   struct Tile {
@@ -151,10 +166,10 @@ struct Walk {
     w.first = first;
     int p = first + lane;
     if constexpr (MODE == kList) p = p < a.n_keep ? a.list[((int64_t)x * a.Hkv + g) * a.n_keep + p] : -1;
-    const bool ok = p >= 0 && p < count;
-    const int phys = ok ? a.c.table[(int64_t)b * a.c.max_pages + p] : -1;
+    // (the table is asked before it is known how many of its pages are seen)
+    const int phys = p >= 0 && p < a.c.max_pages ? a.c.table[(int64_t)b * a.c.max_pages + p] : -1;
     w.page = p;
-    w.phys = phys < a.c.n_pages ? phys : -1;
+    w.phys = p < count && phys < a.c.n_pages ? phys : -1;
   }
 
   __device__ __forceinline__ void load(Tile& t, int64_t at) {
@@ -246,6 +261,8 @@ struct Walk {
     }
   }
 
+  // CAREFUL: the tile may have tokens that only some of the rows see
+  template <bool CAREFUL>
   __device__ __forceinline__ void step(Tile& t) {
     float s[RT][kS];
 #pragma unroll
@@ -271,13 +288,7 @@ struct Walk {
     bool whole = true;
 #pragma unroll
     for (int h = 0; h < kSub; ++h) whole = whole && t.base[h] >= 0 && t.base[h] + 16 <= lim_lo;
-    bool shared = true;                                  // no token that some rows see and others do not
-    if (!whole) {
-#pragma unroll
-      for (int h = 0; h < kSub; ++h)
-        if (MODE == kSeveral && t.base[h] >= 0 && t.base[h] < lim_hi && t.base[h] + 16 > lim_lo) shared = lim_lo == lim_hi;
-      clear(t, lim_hi);
-    }
+    if (!whole) clear(t, lim_hi);
     float p[RT][kS];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -293,13 +304,13 @@ struct Walk {
           top = fmaxf(top, s[r][i]);
         }
       }
-      if (__any(top > m[r] + kAhead)) {
+      if (__any(top > m[r] + kRoom)) {
         typedef unsigned u2v __attribute__((ext_vector_type(2)));
         u2v y = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         top = fmaxf(__uint_as_float(y.x), __uint_as_float(y.y));
         y = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         top = fmaxf(__uint_as_float(y.x), __uint_as_float(y.y));
-        const float next = top > m[r] + kAhead ? top : m[r];          // (each row by itself)
+        const float next = top > m[r] + kRoom ? top : m[r];          // (each row by itself)
         const float f = next == m[r] ? 1.f : __builtin_amdgcn_exp2f(m[r] - next);
         m[r] = next;
         l[r] *= f;
@@ -315,16 +326,16 @@ struct Walk {
         l[r] += e;
       }
     }
-    if (MODE != kSeveral || shared) {
+    if (!CAREFUL || whole) {
       values(t, p, acc);
       return;
     }
-    // Tokens that only some of the rows see: one new row after the other, with the values that it does not see cleared, so that 0
-    // times a value that is not finite does not reach it.
-    for (int i = a.n_q - 1; i >= 0; --i) {               // (copies of the tile are cleared further and further only if limits fall)
+    // one new row after the other, with the values that it does not see cleared: 0 times a value that is not finite is not 0
+    const int last = min(row0 + 16 * RT, a.rows) - 1;
+    for (int i = row0 / a.G; i <= last / a.G; ++i) {
+      const int at = max(i * a.G, row0) - row0;          // a row of it in the workgroup
       Tile mine = t;
-      int limit = a.seen[(int64_t)b * a.n_q + i];
-      clear(mine, limit);
+      clear(mine, __builtin_amdgcn_readlane(RT == 2 && at >= 16 ? lim[RT - 1] : lim[0], at & 15));
       floatx4 c[RT][kE];
 #pragma unroll
       for (int r = 0; r < RT; ++r)
@@ -342,21 +353,30 @@ struct Walk {
     }
   }
 
-  // tiles from token `at` on, every kWaves-th
+  // Tiles from token `at` on, every WAVES-th: those that all rows see as far as they see them, then, without a second tile on its
+  // way (its registers hold what each row's product takes there), those that only some of them see.
   __device__ __forceinline__ void run(int64_t at) {
-    constexpr int kStep = kWaves * kTokens;
-    if (at >= end) return;
-    Tile t0, t1;
-    load(t0, at);
-    while (true) {
-      at += kStep;
-      if (at < end) load(t1, at);
-      step(t0);
-      if (at >= end) return;
-      at += kStep;
-      if (at < end) load(t0, at);
-      step(t1);
-      if (at >= end) return;
+    const int64_t shared = MODE == kSeveral && lim_lo < lim_hi ? min(end, (int64_t)(lim_lo & -kTokens)) : end;
+    if (at < shared) {
+      Tile t0, t1;
+      load(t0, at);
+      while (true) {
+        at += kStep;
+        if (at < shared) load(t1, at);
+        step<false>(t0);
+        if (at >= shared) break;
+        at += kStep;
+        if (at < shared) load(t0, at);
+        step<false>(t1);
+        if (at >= shared) break;
+      }
+    }
+    if constexpr (MODE == kSeveral) {
+      for (; at < end; at += kStep) {
+        Tile t;
+        load(t, at);
+        step<true>(t);
+      }
     }
   }
 
@@ -419,11 +439,11 @@ __device__ __forceinline__ void store_row(const PageAttnArgs& a, int x, int g, i
 
 // Joins the waves of a workgroup: their sums go through LDS, scaled to the largest of their reference points, and leave as rows of
 // the output, or as partial result `part`.
-template <typename T, int D, int RT, int MODE>
-__device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MODE>& w, float (&s_o)[kWaves][16 * RT][D + 4],
-                                       float (&s_m)[kWaves][16 * RT], float (&s_l)[kWaves][16 * RT], int in, int row0, int64_t part) {
-  typedef Walk<T, D, RT, MODE> W;
-  constexpr int kRows = 16 * RT;
+template <typename T, int D, int RT, int MODE, int WAVES>
+__device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MODE, WAVES>& w, float (&s_o)[WAVES][16 * RT][D + 4],
+                                       float (&s_m)[WAVES][16 * RT], float (&s_l)[WAVES][16 * RT], int in, int row0, int64_t part) {
+  typedef Walk<T, D, RT, MODE, WAVES> W;
+  constexpr int kRows = 16 * RT, kThreads = 64 * WAVES;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
@@ -451,11 +471,11 @@ __device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MOD
     const int r = item / (D / 4), e = item % (D / 4) * 4;
     float top = s_m[0][r];
 #pragma unroll
-    for (int i = 1; i < kWaves; ++i) top = fmaxf(top, s_m[i][r]);
+    for (int i = 1; i < WAVES; ++i) top = fmaxf(top, s_m[i][r]);
     float l = 0.f;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
+    for (int i = 0; i < WAVES; ++i) {
       const float mi = s_m[i][r], li = s_l[i][r];
       // (what saw nothing or only logits of -inf weighs nothing beside others; the latter make a row NaN that has nothing else)
       if (mi == -INFINITY) { l = top == -INFINITY ? l + li : l; continue; }
@@ -473,20 +493,27 @@ __device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MOD
   }
 }
 
-template <typename T, int D, int RT, int MODE>
-__global__ __launch_bounds__(kThreads, RT == 1 ? 2 : 1) void page_attn_kernel(PageAttnArgs a) {
-  typedef Walk<T, D, RT, MODE> W;
+// WHOLE: a workgroup has a context as a whole, and nothing is joined.
+template <typename T, int D, int RT, int MODE, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(64 * WAVES, RT == 1 || D == 64 ? 2 : 1) void page_attn_kernel(PageAttnArgs a) {
+  typedef Walk<T, D, RT, MODE, WAVES> W;
   constexpr int kRows = 16 * RT;
-  __shared__ __align__(16) float s_o[kWaves][kRows][D + 4];         // (rows 4 banks apart)
-  __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+  __shared__ __align__(16) float s_o[WAVES][kRows][D + 4];         // (rows 4 banks apart)
+  __shared__ float s_m[WAVES][kRows], s_l[WAVES][kRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t r = blockIdx.x / a.inner;
   const int in = (int)(blockIdx.x - r * a.inner), g = in % a.Hkv, row0 = in / a.Hkv * kRows;
+  W w(a, lane, g);
+  if constexpr (WHOLE) {
+    w.start((int)r, row0, 0, context_tokens(a, (int)r));
+    w.run(wave * W::kTokens);
+    finish(a, w, s_o, s_m, s_l, in, row0, -1);
+    return;
+  }
   const Contexts all = contexts_of(a, lane);
   Place here = place_of<false>(a, all, r * all.range, 0, lane);
   if (here.x < 0) return;
   int64_t at = r * all.range;
-  W w(a, lane, g);
   for (int64_t left = all.range; left > 0;) {
     const int64_t n = min(left, here.start + here.grains - at);
     const int64_t tokens = here.x < 64 ? from_lane(all.tokens, here.x) : context_tokens(a, here.x);
@@ -497,7 +524,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 2 : 1) void page_attn_kernel(Pa
     finish(a, w, s_o, s_m, s_l, in, row0, whole ? -1 : 2 * r + (at == here.start));
     at += n;
     left -= n;
-    if (left == 0 || ++here.x >= a.contexts) break;
+    if (left == 0 || all.apart || ++here.x >= a.contexts) break;
     here.start = at;
     here.grains = here.x < 64 ? (int64_t)from_lane(all.grains, here.x) : pages::grains_of(context_tokens(a, here.x));
     __syncthreads();                                     // (before the sums in LDS are written again)
@@ -563,11 +590,20 @@ __global__ __launch_bounds__(256) void page_join_kernel(PageAttnArgs a) {
 
 template <typename T, int D>
 qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t st) {
-  const int64_t blocks = (int64_t)d.slots * d.inner, joins = (int64_t)std::min(d.contexts, d.slots) * d.inner * a.part_rows;
+  const int64_t blocks = (int64_t)(d.whole ? d.contexts : d.slots) * d.inner;
+  const int64_t joins = (int64_t)std::min(d.contexts, d.slots) * d.inner * a.part_rows;
   if (blocks > 0x7fffffff || joins > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page attention: too many rows");
-  const dim3 grid((unsigned)blocks), block(kThreads);
-#define QCF_LAUNCH(RT, MODE) page_attn_kernel<T, D, RT, MODE><<<grid, block, 0, st>>>(a)
-#define QCF_ROWS(MODE) do { if (d.row_tiles == 1) QCF_LAUNCH(1, MODE); else QCF_LAUNCH(2, MODE); } while (0)
+  const dim3 grid((unsigned)blocks);
+#define QCF_LAUNCH(RT, MODE, WAVES, WHOLE) page_attn_kernel<T, D, RT, MODE, WAVES, WHOLE><<<grid, dim3(64 * WAVES), 0, st>>>(a)
+#define QCF_ROWS(MODE)                                                                          \
+  do {                                                                                          \
+    if (d.row_tiles == 1) {                                                                     \
+      if (d.whole) QCF_LAUNCH(1, MODE, pages::kWholeWaves, true);                               \
+      else QCF_LAUNCH(1, MODE, pages::kWaves, false);                                           \
+    } else {                                                                                    \
+      QCF_LAUNCH(2, MODE, pages::kWaves, false);                                                \
+    }                                                                                           \
+  } while (0)
   if (a.list) QCF_ROWS(kList);
   else if (a.n_q == 1) QCF_ROWS(kOne);
   else QCF_ROWS(kSeveral);
@@ -593,7 +629,7 @@ qcf_status launch_page_attn(const qcf_layer_desc& L, const qcf_page_cache& c, in
   a.c = c; a.q = q; a.seen = seen; a.list = list; a.n_keep = n_keep;
   a.n_q = n_q; a.H = L.n_q_heads; a.Hkv = L.n_kv_heads; a.G = a.H / a.Hkv;
   a.log2_page = __builtin_ctz((unsigned)c.page_size);
-  a.contexts = d.contexts; a.rows = d.rows; a.row_blocks = d.row_blocks; a.inner = d.inner; a.slots = d.slots;
+  a.contexts = d.contexts; a.rows = d.rows; a.inner = d.inner; a.slots = d.slots; a.least = d.least;
   a.part_rows = pages::part_rows(d);
   a.scale = (float)(1.4426950408889634 / std::sqrt((double)L.head_dim));
   a.o = o; a.lse = lse;

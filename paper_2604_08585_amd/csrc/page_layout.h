@@ -3,6 +3,7 @@
 
 #include <stdint.h>
 #include <stddef.h>
+#include <algorithm>
 
 #include "qcf_pages.h"
 
@@ -17,12 +18,14 @@ int compute_unit_count();
 namespace pages {
 
 constexpr int kWaves = 4;                 // of a workgroup; each takes every fourth tile of its part of a context
+constexpr int kWholeWaves = 8;            // of a workgroup that has a context as a whole
 constexpr int kGrain = 32;                // contexts are divided at multiples of this many tokens
-constexpr int kLeast = 4;                 // grains of a range: a tile for every wave
+// Grains of a range: a tile of 32 tokens (bf16) or 16 for every wave.
+inline int least_range(const qcf_layer_desc& L) { return L.dtype == QCF_DTYPE_BF16 ? 4 : 2; }
 
 // The contexts, laid end to end in grains (one at least for each), are cut into equal ranges, one to a workgroup, as many as the
 // GPU holds at once: a range may end inside a context, and may hold several.  (Units of equal length within each context, the last
-// one shorter, left the workgroups unequal where lengths differ: 64 requests of 4K to 12K 480 us, 16 of 1K to 8K 84; @ and @ so.)
+// one shorter, left the workgroups unequal where lengths differ: 64 requests of 4K to 12K 480 us, 16 of 1K to 8K 84; 399 and 71 so.)
 struct Division {
   int contexts;                           // B, or B * n_q where every row has pages of its own
   int rows;                               // rows of a context and KV head: (new rows) * heads of the group
@@ -30,8 +33,21 @@ struct Division {
   int row_blocks;                         // workgroups that take the rows of a context and KV head
   int inner;                              // workgroups of a range: KV heads x row blocks
   int slots;                              // ranges at most
+  int least;                              // grains of a range at least (a power of two)
   int64_t most;                           // grains at most
+  bool whole;                             // a workgroup to every context, KV head and row block: nothing is divided
 };
+
+// Whether workgroups of eight waves take whole contexts, in one launch, or four waves each range of them, in two.  The second launch
+// takes 4 to 5 us, a compute unit reads 50 to 60 GB/s at most; what is saved by dividing shrinks as more workgroups share the
+// memory.  Heads of 128 in bf16, whole and divided, us: 8 workgroups (a request, 8 KV heads) of 512 tokens 9.9 and 10.8, 1024 14.8 and
+// 11.7; 64 of up to 1024 tokens 15.9 and 14.8; 128 of up to 1536 21.2 and 23.6, 2048 36.5 and 30.9; 512 of up to 1024 49 and 55, 4096
+// 159 and 161, 8192 313 and 302.  Heads of 64: 16 of 1536 tokens 12.4 and 13.4, 2048 15.7 and 11.8; 512 of up to 4096 97 and 103.
+inline bool takes_whole(const qcf_layer_desc& L, int64_t workgroups, int64_t longest) {
+  const int64_t bytes = longest * 2 * L.head_dim * (L.dtype == QCF_DTYPE_BF16 ? 2 : 4);
+  const int64_t alone = std::max<int64_t>(30, 200 - workgroups * 256 / compute_unit_count());      // of 200
+  return bytes * alone <= (int64_t)(290 << 10) * 200;
+}
 
 inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, int32_t n_keep) {
   Division d;
@@ -41,20 +57,22 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   d.row_tiles = d.rows > 16 ? 2 : 1;
   d.row_blocks = (d.rows + 16 * d.row_tiles - 1) / (16 * d.row_tiles);
   d.inner = L.n_kv_heads * d.row_blocks;
-  d.slots = 2 * compute_unit_count() / d.inner;
+  d.slots = (d.row_tiles == 1 || L.head_dim == 64 ? 2 : 1) * compute_unit_count() / d.inner;       // (two waves to a SIMD, or one)
   if (d.slots < 1) d.slots = 1;
   const int64_t longest = (int64_t)(n_keep && n_keep < c.max_pages ? n_keep : c.max_pages) * c.page_size;
   d.most = (int64_t)d.contexts * ((longest + kGrain - 1) / kGrain);
-  const int64_t ranges = (d.most + kLeast - 1) / kLeast;
+  d.least = least_range(L);
+  d.whole = d.row_tiles == 1 && takes_whole(L, (int64_t)d.contexts * d.inner, longest);
+  const int64_t ranges = (d.most + d.least - 1) / d.least;
   if (d.slots > ranges) d.slots = (int)ranges;
   return d;
 }
 
 // Grains of a context and of a range, where there are `total` of them in all.
 QCF_BOTH int64_t grains_of(int64_t tokens) { return tokens <= kGrain ? 1 : (tokens + kGrain - 1) / kGrain; }
-QCF_BOTH int64_t range_of(int64_t total, int slots) {
+QCF_BOTH int64_t range_of(int64_t total, int slots, int least) {
   const int64_t even = total >> 31 ? (total + slots - 1) / slots : (int64_t)(((uint32_t)total + (uint32_t)slots - 1u) / (uint32_t)slots);
-  return even > kLeast ? even : kLeast;
+  return even > least ? even : least;
 }
 
 // Partial results, [2 * range + 1 where the context starts in the range, + 0 where it started before][inner][rows of a workgroup]: d
@@ -64,7 +82,7 @@ inline int part_rows(const Division& d) { return d.rows < 16 * d.row_tiles ? d.r
 inline size_t parts(const Division& d) { return (size_t)2 * d.slots * d.inner * part_rows(d); }
 inline size_t sums_bytes(const qcf_layer_desc& L, const Division& d) { return parts(d) * L.head_dim * sizeof(float); }
 // (one range: nothing is left to be joined)
-inline bool divides(const Division& d) { return d.slots > 1; }
+inline bool divides(const Division& d) { return !d.whole && d.slots > 1; }
 inline size_t workspace(const qcf_layer_desc& L, const Division& d) {
   return divides(d) ? sums_bytes(L, d) + parts(d) * 2 * sizeof(float) : 0;
 }

@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Turns tu
     }
   }
   if (!there || !a.c.bounds) return;                      // (of the workgroup)
-  for (int x = 1 << log2_lanes; x < 64; x *= 2)
+  for (int x = 1 << log2_lanes; x < 64 && x >> log2_lanes < n; x *= 2)     // (rows side by side in a wave, as many as there are)
 #pragma unroll
     for (int e = 0; e < 2 * VEC; ++e) {
       lo[e] = least(lo[e], __shfl_xor(lo[e], x, 64));
@@ -218,11 +218,13 @@ __global__ __launch_bounds__(kThreads, 2) void page_score_kernel(qcf_page_cache 
   const int g = (int)(blockIdx.x % Hkv), G = H / Hkv;
   const int64_t rest = blockIdx.x / Hkv, row = rest / chunks;           // (request, new row)
   const int64_t b = row / n_q;
-  const int count = (int)min(((int64_t)max(seen[row], 0) + c.page_size - 1) >> log2_page, (int64_t)c.max_pages);
-  const int first = (int)(rest - row * chunks) * chunk, end = min(count, first + chunk);
-  const int p0 = first + kScorePages * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (p0 >= end) return;
+  const int first = (int)(rest - row * chunks) * chunk, p0 = first + kScorePages * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t* table = c.table + b * c.max_pages;
+  auto entry = [&](int p) { return p + col < c.max_pages ? table[p + col] : -1; };
+  const int phys0 = entry(p0);                          // (asked for with the count, not behind it)
+  const int count = (int)min(((int64_t)max(seen[row], 0) + c.page_size - 1) >> log2_page, (int64_t)c.max_pages);
+  const int end = min(count, first + chunk);
+  if (p0 >= end) return;
   float* out = score + (row * Hkv + g) * c.max_pages;
   const T* bounds = static_cast<const T*>(c.bounds);
   for (int h0 = 0; h0 < G; h0 += 4) {                   // four queries at a time
@@ -239,7 +241,6 @@ __global__ __launch_bounds__(kThreads, 2) void page_score_kernel(qcf_page_cache 
       }
     }
     u32x4 lo[LOADS], hi[LOADS], next_lo[LOADS], next_hi[LOADS];
-    auto entry = [&](int p) { return p + col < end ? table[p + col] : -1; };
     auto load = [&](int phys, u32x4 (&l)[LOADS], u32x4 (&h)[LOADS]) {
       const T* src = bounds + ((int64_t)(phys >= 0 && phys < c.n_pages ? phys : 0) * Hkv + g) * 2 * D + quad * VEC;
 #pragma unroll
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(kThreads, 2) void page_score_kernel(qcf_page_cache 
       }
     };
     auto there = [&](int phys) { return __ballot(phys >= 0 && phys < c.n_pages); };
-    int phys = entry(p0), next = entry(p0 + STEP);
+    int phys = phys0, next = entry(p0 + STEP);
     load(phys, lo, hi);
     for (int p = p0; p < end; p += STEP) {
       const uint64_t mask = there(phys);
