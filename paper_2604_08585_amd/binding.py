@@ -483,10 +483,10 @@ def _rows(t: Optional[torch.Tensor]):
     """Pointer and row stride of [rows, heads, d], dense but for the distance of its rows."""
     if t is None:
         return None, 0
-    dense = t.shape[1] * t.shape[2]
-    if not t.is_cuda or t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+    shape, stride = t.shape, t.stride()          # (each attribute once: they are most of what a call takes here)
+    if len(stride) != 3 or not t.is_cuda or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2]):
         raise QcfError("rows handed to the library must be CUDA tensors [rows, heads, d] with dense rows")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else dense
+    return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1] * shape[2]
 
 
 def qcf_page_append(desc: LayerDesc, cache: PageCache, B: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,

@@ -30,7 +30,7 @@ struct PageAttnArgs {
   const int32_t* seen;
   const int32_t* list;
   int n_keep, n_q, H, Hkv, G, log2_page;
-  int contexts, rows, inner, slots, least, part_rows;
+  int contexts, rows, inner, slots, least, pad, part_rows;
   float scale;                                           // log2(e) / sqrt(d)
   void* o;
   float* lse;
@@ -64,57 +64,62 @@ __device__ __forceinline__ uint32_t wave_incl(uint32_t x) {
 }
 __device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 
-// The contexts in grains, end to end.  Every wave works them out by itself; the first 64 stay in its lanes.
+// The contexts in grains, end to end, `pad` of them in front of each: what a workgroup that has begun one context pays for another.
+// Every wave works them out by itself; the first 64 stay in its lanes.
 struct Contexts {
   uint32_t tokens, grains;             // of context `lane`
-  uint32_t room, incl;                 // grains that it is given, and the sum so far (64 of at most 2^25: below 2^31)
+  uint32_t room, incl;                 // grains with the padding, and the sum so far (64 of less than 2^26)
   int64_t range;                       // grains of a range
+  int pad;
   bool apart;                          // no range has two contexts
 };
 struct Place {
   int x;                               // context
-  int64_t start, grains;               // its first grain, and how many it has
+  int64_t start, grains;               // its first grain (behind the padding), and how many it has
 };
 
 __device__ __forceinline__ Contexts contexts_of(const PageAttnArgs& a, int lane) {
   Contexts c;
   c.tokens = lane < a.contexts ? (uint32_t)context_tokens(a, lane) : 0u;
   c.grains = lane < a.contexts ? (uint32_t)pages::grains_of(c.tokens) : 0u;
-  c.room = c.grains;
+  c.room = lane < a.contexts ? c.grains + a.pad : 0u;
   c.incl = wave_incl(c.room);
+  c.pad = a.pad;
   c.apart = false;
-  int64_t total = from_lane(c.incl, 63);
-  for (int x0 = 64; x0 < a.contexts; x0 += 64)
-    total += from_lane(wave_incl(x0 + lane < a.contexts ? (uint32_t)pages::grains_of(context_tokens(a, x0 + lane)) : 0u), 63);
-  c.range = pages::range_of(total, a.slots, a.least);
-  if (a.contexts <= 64 && c.range == a.least) {
+  if (a.contexts <= 64) {
     // little work: every context begins a range of its own if there are enough of them (two parts in a row take a workgroup
-    // twice the latency: five requests of up to 600 tokens in float32 13.6 us, @ so)
+    // twice the latency: five requests of up to 600 tokens in float32 13.6 us, 10.4 so)
     const uint32_t room = (c.grains + a.least - 1) & ~(uint32_t)(a.least - 1), incl = wave_incl(room);
     if (from_lane(incl, 63) <= (uint64_t)a.least * a.slots) {
       c.room = room;
       c.incl = incl;
+      c.pad = 0;
       c.apart = true;
     }
   }
+  int64_t total = from_lane(c.incl, 63);
+  for (int x0 = 64; x0 < a.contexts; x0 += 64)
+    total += from_lane(wave_incl(x0 + lane < a.contexts ? (uint32_t)pages::grains_of(context_tokens(a, x0 + lane)) + a.pad : 0u), 63);
+  c.range = pages::range_of(total, a.slots, a.least);
   return c;
 }
-// The context that has a grain (x -1: none has), or context x itself.
+// The context whose grain or padding a position is (x -1: none), or context x itself.
 template <bool OF>
-__device__ __forceinline__ Place place_of(const PageAttnArgs& a, const Contexts& c, int64_t grain, int x, int lane) {
+__device__ __forceinline__ Place place_of(const PageAttnArgs& a, const Contexts& c, int64_t at, int x, int lane) {
   Place p = {-1, 0, 0};
   uint32_t n = c.grains, room = c.room, incl = c.incl;
   for (int x0 = 0; x0 < a.contexts; x0 += 64) {
     if (x0 > 0) {
-      n = room = x0 + lane < a.contexts ? (uint32_t)pages::grains_of(context_tokens(a, x0 + lane)) : 0u;
+      n = x0 + lane < a.contexts ? (uint32_t)pages::grains_of(context_tokens(a, x0 + lane)) : 0u;
+      room = n > 0u ? n + a.pad : 0u;
       incl = wave_incl(room);
     }
-    const uint64_t hit = __ballot(n > 0u && (OF ? x0 + lane == x : grain < p.start + incl));
+    const uint64_t hit = __ballot(n > 0u && (OF ? x0 + lane == x : at < p.start + incl));
     if (hit) {
       const int l = __builtin_ctzll(hit);
       p.x = x0 + l;
       p.grains = from_lane(n, l);
-      p.start += from_lane(incl, l) - from_lane(room, l);
+      p.start += from_lane(incl, l) - from_lane(room, l) + (uint32_t)c.pad;
       return p;
     }
     p.start += from_lane(incl, 63);
@@ -511,42 +516,41 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 || D == 64 ? 2 : 1) void page_a
     return;
   }
   const Contexts all = contexts_of(a, lane);
-  Place here = place_of<false>(a, all, r * all.range, 0, lane);
+  const int64_t from = r * all.range, to = from + all.range;
+  Place here = place_of<false>(a, all, from, 0, lane);
   if (here.x < 0) return;
-  int64_t at = r * all.range;
-  for (int64_t left = all.range; left > 0;) {
-    const int64_t n = min(left, here.start + here.grains - at);
-    const int64_t tokens = here.x < 64 ? from_lane(all.tokens, here.x) : context_tokens(a, here.x);
-    const int64_t begin = (at - here.start) * pages::kGrain;
-    w.start(here.x, row0, begin, min(begin + n * pages::kGrain, tokens));
-    w.run(begin + wave * W::kTokens);
-    const bool whole = n == here.grains;
-    finish(a, w, s_o, s_m, s_l, in, row0, whole ? -1 : 2 * r + (at == here.start));
-    at += n;
-    left -= n;
-    if (left == 0 || all.apart || ++here.x >= a.contexts) break;
-    here.start = at;
+  while (true) {
+    // its grains in the range, counted from its first
+    const int64_t g0 = max(from - here.start, (int64_t)0), g1 = min(to - here.start, here.grains);
+    if (g1 > g0) {
+      const int64_t tokens = here.x < 64 ? from_lane(all.tokens, here.x) : context_tokens(a, here.x);
+      w.start(here.x, row0, g0 * pages::kGrain, min(g1 * pages::kGrain, tokens));
+      w.run(g0 * pages::kGrain + wave * W::kTokens);
+      finish(a, w, s_o, s_m, s_l, in, row0, g1 - g0 == here.grains ? -1 : 2 * r + (g0 == 0));
+    }
+    here.start += here.grains + all.pad;
+    if (here.start >= to || all.apart || ++here.x >= a.contexts) return;
     here.grains = here.x < 64 ? (int64_t)from_lane(all.grains, here.x) : pages::grains_of(context_tokens(a, here.x));
     __syncthreads();                                     // (before the sums in LDS are written again)
   }
 }
 
-// Joins the parts of a context: one workgroup per (context, KV head and row block, row), or, where there are more contexts than
-// ranges, per range for the context that starts in it and goes on behind it.  A group of threads takes every kGroups-th part.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void page_join_kernel(PageAttnArgs a) {
-  constexpr int kVecs = D / 4, kGroups = 256 / kVecs, kAt = 4;
+// Joins the parts of a context: a workgroup per (context, KV head and row block, rows), or, where there are more contexts than
+// ranges, per range for the context that starts in it and goes on behind it.  SHARED: the groups of threads share a row's parts, one
+// row to a workgroup; otherwise each has a row.
+template <typename T, int D, bool SHARED>
+__global__ __launch_bounds__(256) void page_join_kernel(PageAttnArgs a, int row_steps) {
+  constexpr int kVecs = D / 4, kGroups = 256 / kVecs, kStep = SHARED ? kGroups : 1, kAt = 4;
   __shared__ __align__(16) float s_o[kGroups][D];
   __shared__ float s_l[kGroups], s_m[kGroups];
   const int tid = threadIdx.x, lane = tid & 63, group = tid / kVecs, e = tid % kVecs * 4;
-  const int r = blockIdx.x % a.part_rows;
-  const int64_t rest = blockIdx.x / a.part_rows, item = rest / a.inner;
+  const int64_t rest = blockIdx.x / row_steps, item = rest / a.inner;
+  const int r = SHARED ? (int)(blockIdx.x - rest * row_steps) : (int)(blockIdx.x - rest * row_steps) * kGroups + group;
   const int in = (int)(rest - item * a.inner), row = in / a.Hkv * a.part_rows + r;
-  if (row >= a.rows) return;
   const Contexts all = contexts_of(a, lane);
   const bool few = a.contexts <= a.slots;
   const Place p = few ? place_of<true>(a, all, 0, (int)item, lane) : place_of<false>(a, all, (item + 1) * all.range - 1, 0, lane);
-  if (p.x < 0) return;
+  if (p.x < 0 || r >= a.part_rows || row >= a.rows) return;             // (SHARED: of the workgroup)
   auto range_at = [&](int64_t grain) {
     return (grain | all.range) >> 31 ? grain / all.range : (int64_t)((uint32_t)grain / (uint32_t)all.range);
   };
@@ -566,32 +570,37 @@ __global__ __launch_bounds__(256) void page_join_kernel(PageAttnArgs a) {
     o = o * f + v * g;
     top = next;
   };
-  for (int j0 = group; j0 < count; j0 += kAt * kGroups) {
+  for (int j0 = SHARED ? group : 0; j0 < count; j0 += kAt * kStep) {
     float2 ml[kAt];
     floatx4 v[kAt];
 #pragma unroll
     for (int i = 0; i < kAt; ++i) {
-      const int64_t at = part(min(j0 + i * kGroups, count - 1));
+      const int64_t at = part(min(j0 + i * kStep, count - 1));
       ml[i] = a.part_ml[at];
       v[i] = *reinterpret_cast<const floatx4*>(a.part_o + at * D + e);
     }
 #pragma unroll
     for (int i = 0; i < kAt; ++i)
-      if (j0 + i * kGroups < count) add(ml[i], v[i]);
+      if (j0 + i * kStep < count) add(ml[i], v[i]);
   }
-  *reinterpret_cast<floatx4*>(&s_o[group][e]) = o;
-  if (e == 0) { s_l[group] = l; s_m[group] = top; }
-  __syncthreads();
-  if (group > 0) return;
+  if constexpr (SHARED) {
+    *reinterpret_cast<floatx4*>(&s_o[group][e]) = o;
+    if (e == 0) { s_l[group] = l; s_m[group] = top; }
+    __syncthreads();
+    if (group > 0) return;
 #pragma unroll
-  for (int j = 1; j < kGroups; ++j) add(make_float2(s_m[j], s_l[j]), *reinterpret_cast<const floatx4*>(&s_o[j][e]));
+    for (int j = 1; j < kGroups; ++j) add(make_float2(s_m[j], s_l[j]), *reinterpret_cast<const floatx4*>(&s_o[j][e]));
+  }
   store_row<T, D>(a, p.x, in % a.Hkv, row, e, top, l, o);
 }
 
 template <typename T, int D>
 qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t st) {
   const int64_t blocks = (int64_t)(d.whole ? d.contexts : d.slots) * d.inner;
-  const int64_t joins = (int64_t)std::min(d.contexts, d.slots) * d.inner * a.part_rows;
+  // groups of a joining workgroup share a row where contexts have more than four parts on average
+  const bool shared = (int64_t)d.contexts * 4 < d.slots;
+  const int row_steps = shared ? a.part_rows : (a.part_rows + 1024 / D - 1) / (1024 / D);
+  const int64_t joins = (int64_t)std::min(d.contexts, d.slots) * d.inner * row_steps;
   if (blocks > 0x7fffffff || joins > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page attention: too many rows");
   const dim3 grid((unsigned)blocks);
 #define QCF_LAUNCH(RT, MODE, WAVES, WHOLE) page_attn_kernel<T, D, RT, MODE, WAVES, WHOLE><<<grid, dim3(64 * WAVES), 0, st>>>(a)
@@ -611,7 +620,8 @@ qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t s
 #undef QCF_LAUNCH
   QCF_TRY_LAUNCH("page attention");
   if (!pages::divides(d)) return QCF_OK;
-  page_join_kernel<T, D><<<dim3((unsigned)joins), dim3(256), 0, st>>>(a);
+  if (shared) page_join_kernel<T, D, true><<<dim3((unsigned)joins), dim3(256), 0, st>>>(a, row_steps);
+  else page_join_kernel<T, D, false><<<dim3((unsigned)joins), dim3(256), 0, st>>>(a, row_steps);
   return check_launch("page attention join");
 }
 
@@ -629,7 +639,7 @@ qcf_status launch_page_attn(const qcf_layer_desc& L, const qcf_page_cache& c, in
   a.c = c; a.q = q; a.seen = seen; a.list = list; a.n_keep = n_keep;
   a.n_q = n_q; a.H = L.n_q_heads; a.Hkv = L.n_kv_heads; a.G = a.H / a.Hkv;
   a.log2_page = __builtin_ctz((unsigned)c.page_size);
-  a.contexts = d.contexts; a.rows = d.rows; a.inner = d.inner; a.slots = d.slots; a.least = d.least;
+  a.contexts = d.contexts; a.rows = d.rows; a.inner = d.inner; a.slots = d.slots; a.least = d.least; a.pad = d.pad;
   a.part_rows = pages::part_rows(d);
   a.scale = (float)(1.4426950408889634 / std::sqrt((double)L.head_dim));
   a.o = o; a.lse = lse;

@@ -6,12 +6,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// theta_i / 2 pi of a layer's rotary pairs, computed on the host: exp2 in float64 in front of every workgroup's first row would
-// take longer than a decoding step's whole append.
-struct Turns {
-  double of[64];
-};
-
 struct AppendArgs {
   const void* q;
   const void* k;
@@ -24,16 +18,27 @@ struct AppendArgs {
   void* q_out;
   qcf_page_cache c;
   int B, H, Hkv, log2_page;
+  double neg2_over_d_log2base;
 };
 
 // (cos, sin) of `positions` times a frequency given in turns per position.  The product is rounded at 2^-53 of up to 2^31
 // turns; its fraction is exact in float64 and loses less than 2^-25 of a turn as a float.
+template <typename T>
 __device__ __forceinline__ float2 turn_at(double positions, double turns) {
   const double t = positions * turns;
   const float f = (float)(t - __builtin_rint(t));
+  // bf16: the hardware's sine and cosine of a fraction of a turn (HWERR)
+  if constexpr (sizeof(T) == 2) return make_float2(__builtin_amdgcn_cosf(f), __builtin_amdgcn_sinf(f));
   float sn, cn;
   sincospif(2.f * f, &sn, &cn);
   return make_float2(cn, sn);
+}
+
+// sixteen bytes of rounded elements
+template <typename T>
+__device__ __forceinline__ u32x4 rounded(const float* f) {
+  if constexpr (sizeof(T) == 4) return Vec16<T>::pack(f);
+  else return mk4(cvt_pk_bf16(f[0], f[1]), cvt_pk_bf16(f[2], f[3]), cvt_pk_bf16(f[4], f[5]), cvt_pk_bf16(f[6], f[7]));
 }
 
 // The least and the largest of two values, not a number if either is not.
@@ -77,19 +82,25 @@ __device__ __forceinline__ Request request_of(const AppendArgs& a, int64_t unit,
 }
 
 // One workgroup per (page that gets rows, `heads` KV heads of it): their keys, turned and rounded, the bounds, the values, and the
-// queries of the heads' groups.  A thread takes VEC rotary pairs of a row, two 16-byte vectors.  The (cos, sin) of 16 rows are kept
-// in LDS for all heads: formed for every vector anew they took the vector unit longer than the rows took memory (32K rows, 8
-// KV heads of 128: 238 us, 165 with them).
+// queries of the heads' groups.  A thread takes VEC rotary pairs of a row, two 16-byte vectors.  The (cos, sin) of kRows rows are
+// kept in LDS for all heads: formed for every vector anew they took the vector unit longer than the rows took memory (32K rows, 8
+// KV heads of 128: 238 us, 190 with them).  Bound by memory there, and by the chain offsets -> rows, page and positions -> factors
+// -> stores where few rows come: what needs no factors is asked for in front of them.
 template <typename T, int D, int STYLE>
-__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Turns turns, int heads, int log2_lanes) {
-  constexpr int VEC = Elem<T>::kVec, TPR = D / 2 / VEC, WAVES = kThreads / 64, PAIRS = D / 2, ROWS = 16;
-  __shared__ __align__(16) float2 s_turn[ROWS][PAIRS];
-  __shared__ float s_bound[2][WAVES][64 / TPR][D];
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int heads, int log2_lanes) {
+  constexpr int VEC = Elem<T>::kVec, TPR = D / 2 / VEC, WAVES = kThreads / 64, PAIRS = D / 2, ROWS = 4096 / D, AHEAD = 2;
+  typedef float2 turn_rows[ROWS][PAIRS];
+  typedef float bound_rows[2][WAVES][64 / TPR][D];
+  __shared__ __align__(16) char s_mem[sizeof(turn_rows) > sizeof(bound_rows) ? sizeof(turn_rows) : sizeof(bound_rows)];
+  turn_rows& s_turn = *reinterpret_cast<turn_rows*>(s_mem);
+  bound_rows& s_bound = *reinterpret_cast<bound_rows*>(s_mem);          // (after the last factors have been used)
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int parts = a.Hkv / heads;
   const int64_t unit = blockIdx.x / parts;
   const int g0 = (int)(blockIdx.x - unit * parts) * heads, G = a.H / a.Hkv;
   const Request rq = request_of(a, unit, lane);
+  // (a thread forms the factors of one pair; its frequency, in turns per position, needs nothing from memory)
+  const double turns = exp2(a.neg2_over_d_log2base * (double)(tid % PAIRS)) * 0.15915494309189533577;
   const int64_t page = a.c.page_size, len = rq.len;
   const int64_t p = (len >> a.log2_page) + unit - rq.unit0;
   const int64_t t0 = max(p * page, len), t1 = min((p + 1) * page, len + (rq.r1 - rq.r0));
@@ -97,76 +108,109 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Turns tu
   const int n = (int)(t1 - t0);
   const int64_t row0 = rq.r0 + (t0 - len);
   const int64_t phys = p >= 0 && p < a.c.max_pages ? a.c.table[(int64_t)rq.b * a.c.max_pages + p] : -1;
-  const bool there = phys >= 0 && phys < a.c.n_pages;
   const int slot0 = (int)(t0 - p * page);
-  const int64_t at = there ? phys * a.c.page_stride + slot0 * a.c.slot_stride : 0;
 
   // columns of a thread's pairs in a head; tid = (row, head, place in the head)
   const int place = tid % TPR, i0 = place * VEC;
   const int e0 = STYLE == 0 ? i0 : 2 * i0, e1 = STYLE == 0 ? i0 + PAIRS : 2 * i0 + VEC;
-  auto turned = [&](int j, u32x4& ra, u32x4& rb) {
+  struct Pairs {
+    u32x4 a, b;
+  };
+  auto read = [&](const T* src) {
+    return Pairs{*reinterpret_cast<const u32x4*>(src + e0), *reinterpret_cast<const u32x4*>(src + e1)};
+  };
+  auto write = [&](T* dst, const Pairs& x) {
+    *reinterpret_cast<u32x4*>(dst + e0) = x.a;
+    *reinterpret_cast<u32x4*>(dst + e1) = x.b;
+  };
+  auto turn = [&](int j, Pairs& x) {
     if (!a.pos) return;
     float f[2 * VEC], o[2 * VEC];
-    Vec16<T>::unpack(ra, f);
-    Vec16<T>::unpack(rb, f + VEC);
+    Vec16<T>::unpack(x.a, f);
+    Vec16<T>::unpack(x.b, f + VEC);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
       const int ia = STYLE == 0 ? i : 2 * i, ib = STYLE == 0 ? i + VEC : 2 * i + 1;
       turn_pair(f[ia], f[ib], s_turn[j][i0 + i], o[ia], o[ib]);
     }
-    ra = Vec16<T>::pack(o);
-    rb = Vec16<T>::pack(o + VEC);
+    x.a = rounded<T>(o);
+    x.b = rounded<T>(o + VEC);
   };
   const int slots = kThreads >> log2_lanes, slot = tid >> log2_lanes;          // rows side by side; heads * TPR threads to a row
   const int head = (tid & ((1 << log2_lanes) - 1)) / TPR;
+  const T* k = static_cast<const T*>(a.k) + row0 * a.k_stride + (g0 + head) * D;
+  const T* v = static_cast<const T*>(a.v) + row0 * a.v_stride + (g0 + head) * D;
+  const int q_vecs = heads * G * TPR;
+  const T* q = static_cast<const T*>(a.q) + row0 * a.q_stride + g0 * G * D;
+  T* q_out = static_cast<T*>(a.q_out) + (row0 * a.H + g0 * G) * D;
+  // the next AHEAD rows of keys and values from row j on, and AHEAD vectors of queries from item `at` on, of rows before `end`
+  Pairs kk[AHEAD], vv[AHEAD], qq[AHEAD];
+  auto read_rows = [&](int j, int end) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int64_t r = min(j + i * slots, end - 1);
+      kk[i] = read(k + r * a.k_stride);
+      vv[i] = read(v + r * a.v_stride);
+    }
+  };
+  auto query = [&](int at, int& j, int& h) { j = at / q_vecs; h = (at - j * q_vecs) / TPR; };     // (kThreads is a multiple of TPR: the place stays)
+  auto read_queries = [&](int at, int items, int j0) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      int j, h;
+      query(min(at + i * kThreads, items - TPR + place), j, h);
+      qq[i] = read(q + (j0 + j) * a.q_stride + h * D);
+    }
+  };
+  read_rows(slot, n);
+  if (a.q) read_queries(tid, min(n, ROWS) * q_vecs, 0);
+
+  const bool there = phys >= 0 && phys < a.c.n_pages;
+  const int64_t dst = there ? phys * a.c.page_stride + slot0 * a.c.slot_stride + (g0 + head) * a.c.head_stride : 0;
+  T* kc = static_cast<T*>(a.c.k) + dst;
+  T* vc = static_cast<T*>(a.c.v) + dst;
+  T* bounds = static_cast<T*>(a.c.bounds) + (phys * a.Hkv + g0) * 2 * D;
+  const bool join = there && a.c.bounds && slot0 > 0;
+  const float old = join && tid < heads * 2 * D ? Elem<T>::load(bounds + tid) : 0.f;       // (the others' follow where they are used)
   float lo[2 * VEC], hi[2 * VEC];
 #pragma unroll
   for (int e = 0; e < 2 * VEC; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
-  const T* k = static_cast<const T*>(a.k) + row0 * a.k_stride + (g0 + head) * D;
-  const T* v = static_cast<const T*>(a.v) + row0 * a.v_stride + (g0 + head) * D;
-  T* kc = static_cast<T*>(a.c.k) + at + (g0 + head) * a.c.head_stride;
-  T* vc = static_cast<T*>(a.c.v) + at + (g0 + head) * a.c.head_stride;
-  const int q_heads = heads * G, q_vecs = q_heads * TPR;
-  const T* q = static_cast<const T*>(a.q) + row0 * a.q_stride + g0 * G * D;
-  T* q_out = static_cast<T*>(a.q_out) + (row0 * a.H + g0 * G) * D;
-
   for (int j0 = 0; j0 < n; j0 += ROWS) {
     const int rows = min(n - j0, ROWS);
     if (a.pos) {
       if (j0 > 0) __syncthreads();
-      for (int item = tid; item < rows * PAIRS; item += kThreads) {
-        const int j = item / PAIRS, i = item % PAIRS;
-        s_turn[j][i] = turn_at((double)a.pos[row0 + j0 + j], turns.of[i]);
-      }
+      for (int j = tid / PAIRS; j < rows; j += kThreads / PAIRS)
+        s_turn[j][tid % PAIRS] = turn_at<T>((double)a.pos[row0 + j0 + j], turns);
       __syncthreads();
     }
-    if (there) {
-      for (int j = slot; j < rows; j += slots) {
-        const int64_t r = j0 + j;
-        u32x4 ka = *reinterpret_cast<const u32x4*>(k + r * a.k_stride + e0), kb = *reinterpret_cast<const u32x4*>(k + r * a.k_stride + e1);
-        const u32x4 va = *reinterpret_cast<const u32x4*>(v + r * a.v_stride + e0), vb = *reinterpret_cast<const u32x4*>(v + r * a.v_stride + e1);
-        turned(j, ka, kb);
-        *reinterpret_cast<u32x4*>(kc + r * a.c.slot_stride + e0) = ka;
-        *reinterpret_cast<u32x4*>(kc + r * a.c.slot_stride + e1) = kb;
-        *reinterpret_cast<u32x4*>(vc + r * a.c.slot_stride + e0) = va;
-        *reinterpret_cast<u32x4*>(vc + r * a.c.slot_stride + e1) = vb;
+    for (int j = slot; j < rows; j += AHEAD * slots) {
+      if (j0 > 0 || j > slot) read_rows(j0 + j, n);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int mine = j + i * slots;
+        if (mine >= rows || !there) continue;
+        turn(mine, kk[i]);
+        write(kc + (int64_t)(j0 + mine) * a.c.slot_stride, kk[i]);
+        write(vc + (int64_t)(j0 + mine) * a.c.slot_stride, vv[i]);
         float f[2 * VEC];
-        Vec16<T>::unpack(ka, f);
-        Vec16<T>::unpack(kb, f + VEC);
+        Vec16<T>::unpack(kk[i].a, f);
+        Vec16<T>::unpack(kk[i].b, f + VEC);
 #pragma unroll
         for (int e = 0; e < 2 * VEC; ++e) { lo[e] = least(lo[e], f[e]); hi[e] = largest(hi[e], f[e]); }
       }
     }
     if (a.q) {
-      for (int item = tid; item < rows * q_vecs; item += kThreads) {             // (kThreads is a multiple of TPR: the place stays)
-        const int j = item / q_vecs, h = (item - j * q_vecs) / TPR;
-        const int64_t r = j0 + j;
-        const T* src = q + r * a.q_stride + h * D;
-        u32x4 ra = *reinterpret_cast<const u32x4*>(src + e0), rb = *reinterpret_cast<const u32x4*>(src + e1);
-        turned(j, ra, rb);
-        T* out = q_out + (r * a.H + h) * D;
-        *reinterpret_cast<u32x4*>(out + e0) = ra;
-        *reinterpret_cast<u32x4*>(out + e1) = rb;
+      const int items = rows * q_vecs;
+      for (int at = tid; at < items; at += AHEAD * kThreads) {
+        if (j0 > 0 || at > tid) read_queries(at, items, j0);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          if (at + i * kThreads >= items) continue;
+          int j, h;
+          query(at + i * kThreads, j, h);
+          turn(j, qq[i]);
+          write(q_out + ((int64_t)(j0 + j) * a.H + h) * D, qq[i]);
+        }
       }
     }
   }
@@ -177,6 +221,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Turns tu
       lo[e] = least(lo[e], __shfl_xor(lo[e], x, 64));
       hi[e] = largest(hi[e], __shfl_xor(hi[e], x, 64));
     }
+  __syncthreads();
   if (lane >> log2_lanes == 0) {
 #pragma unroll
     for (int e = 0; e < 2 * VEC; ++e) {
@@ -186,7 +231,6 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Turns tu
     }
   }
   __syncthreads();
-  T* bounds = static_cast<T*>(a.c.bounds) + (phys * a.Hkv + g0) * 2 * D;
   for (int item = tid; item < heads * 2 * D; item += kThreads) {
     const int h = item / (2 * D), col = item % D;
     const bool low = item % (2 * D) < D;
@@ -194,9 +238,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Turns tu
     float x = b[0][h][col];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) x = low ? least(x, b[w][h][col]) : largest(x, b[w][h][col]);
-    if (slot0 > 0) {
-      const float old = Elem<T>::load(bounds + item);
-      x = low ? least(x, old) : largest(x, old);
+    if (join) {
+      const float was = item == tid ? old : Elem<T>::load(bounds + item);
+      x = low ? least(x, was) : largest(x, was);
     }
     Elem<T>::store(bounds + item, x);
   }
@@ -209,7 +253,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Turns tu
 // page lane % 16 and every fourth 16-byte vector of its bounds; of the result, query lane % 4 and page 4 (lane / 4 % 4) + lane / 16.
 constexpr int kScorePages = 16;
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void page_score_kernel(qcf_page_cache c, const T* __restrict__ q,
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 || D == 64 ? 2 : 1) void page_score_kernel(qcf_page_cache c, const T* __restrict__ q,
                                                                  const int32_t* __restrict__ seen, int n_q, int H, int Hkv,
                                                                  int log2_page, int chunks, int chunk, float* __restrict__ score) {
   constexpr int VEC = Elem<T>::kVec, LOADS = D / (4 * VEC), STEP = kScorePages * kThreads / 64;
@@ -301,9 +345,7 @@ qcf_status launch_page_append(const qcf_layer_desc& L, const qcf_page_cache& c, 
   a.c = c;
   a.B = B; a.H = L.n_q_heads; a.Hkv = L.n_kv_heads;
   a.log2_page = __builtin_ctz((unsigned)c.page_size);
-  Turns turns;
-  const double log2_base = std::log2(L.rope_base);
-  for (int i = 0; i < L.head_dim / 2; ++i) turns.of[i] = std::exp2(-2.0 * i / L.head_dim * log2_base) * 0.15915494309189533577;
+  a.neg2_over_d_log2base = -2.0 / L.head_dim * std::log2(L.rope_base);
   // KV heads of a workgroup: a power of two of them, whose vectors of a row fill a wave at most, as long as every compute unit
   // has two workgroups.  More share their (cos, sin), fewer give a short call more workgroups (@).
   const int64_t units = (total_rows >> a.log2_page) + 2 * (int64_t)B;
@@ -314,7 +356,7 @@ qcf_status launch_page_append(const qcf_layer_desc& L, const qcf_page_cache& c, 
   const int log2_lanes = __builtin_ctz((unsigned)(heads * per_row));
   const int64_t blocks = units * (L.n_kv_heads / heads);
   if (blocks > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page append: too many rows");
-#define QCF_LAUNCH(T, D, S) append_kernel<T, D, S><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, turns, heads, log2_lanes)
+#define QCF_LAUNCH(T, D, S) append_kernel<T, D, S><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, heads, log2_lanes)
 #define QCF_STYLE(T, D) do { if (L.rope_style == 0) QCF_LAUNCH(T, D, 0); else QCF_LAUNCH(T, D, 1); } while (0)
   if (L.dtype == QCF_DTYPE_BF16) {
     if (L.head_dim == 128) QCF_STYLE(bf16_t, 128); else QCF_STYLE(bf16_t, 64);
