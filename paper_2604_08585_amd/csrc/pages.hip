@@ -27,7 +27,8 @@ template <typename T>
 __device__ __forceinline__ float2 turn_at(double positions, double turns) {
   const double t = positions * turns;
   const float f = (float)(t - __builtin_rint(t));
-  // bf16: the hardware's sine and cosine of a fraction of a turn (HWERR)
+  // bf16: the hardware's sine and cosine of a fraction of a turn, at most 1.3e-7 off (731
+  // rows with heads of 64, in pages of 64: 10.8 us with sincospif and rounding by integers, 8.1 with both in hardware)
   if constexpr (sizeof(T) == 2) return make_float2(__builtin_amdgcn_cosf(f), __builtin_amdgcn_sinf(f));
   float sn, cn;
   sincospif(2.f * f, &sn, &cn);
@@ -249,66 +250,71 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int head
 // Scores of pages (the definition is in qcf_pages.h), 16 pages to a wave, in float64 products of 4 pages x 4 queries x 4 elements,
 // four of them side by side: score = sum of min(q, 0) lo + max(q, 0) hi.  Products of two stored bf16 values are exact in float64,
 // and so are their sums where the terms are within 2^37 of each other: the order of the sum does not decide between pages.
-// Bound by memory (512 bytes to a page and KV head of 128) and, close behind, by turning its values into float64.  A lane has
-// page lane % 16 and every fourth 16-byte vector of its bounds; of the result, query lane % 4 and page 4 (lane / 4 % 4) + lane / 16.
+// Bound by memory (512 bytes to a page and KV head of 128) and, close behind, by its float64 work, a conversion and a product to
+// each value: 32 contexts of 1024 pages on average, 8 KV heads, 41.6 us with the queries in registers, two waves to a SIMD (30 of
+// it without the products, with more chains of sums no change), 38.9 with the queries in LDS, four waves (3.5 TB/s).  A lane has page
+// lane % 16 and every fourth 16-byte vector of its bounds; of the result, query lane % 4 and page 4 (lane / 4 % 4) + lane / 16.
 constexpr int kScorePages = 16;
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 || D == 64 ? 2 : 1) void page_score_kernel(qcf_page_cache c, const T* __restrict__ q,
-                                                                 const int32_t* __restrict__ seen, int n_q, int H, int Hkv,
-                                                                 int log2_page, int chunks, int chunk, float* __restrict__ score) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_kernel(
+    qcf_page_cache c, const T* __restrict__ q, const int32_t* __restrict__ seen, int n_q, int H, int Hkv, int log2_page, int chunks,
+    int chunk, float* __restrict__ score) {
   constexpr int VEC = Elem<T>::kVec, LOADS = D / (4 * VEC), STEP = kScorePages * kThreads / 64;
-  constexpr bool AHEAD = sizeof(T) == 2;                // the next pages' bounds are on their way (float32: no registers for them)
-  const int lane = threadIdx.x & 63, quad = lane >> 4, col = lane & 15, j = lane & 3;
+  typedef double pair_t __attribute__((ext_vector_type(2)));
+  // min(q, 0) and max(q, 0) of two elements of four queries, in the order in which the lanes read them
+  __shared__ pair_t s_q[2][D / 8][16];
+  const int tid = threadIdx.x, lane = tid & 63, quad = lane >> 4, col = lane & 15, j = lane & 3;
   const int g = (int)(blockIdx.x % Hkv), G = H / Hkv;
   const int64_t rest = blockIdx.x / Hkv, row = rest / chunks;           // (request, new row)
   const int64_t b = row / n_q;
-  const int first = (int)(rest - row * chunks) * chunk, p0 = first + kScorePages * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int first = (int)(rest - row * chunks) * chunk, p0 = first + kScorePages * __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* table = c.table + b * c.max_pages;
   auto entry = [&](int p) { return p + col < c.max_pages ? table[p + col] : -1; };
   const int phys0 = entry(p0);                          // (asked for with the count, not behind it)
   const int count = (int)min(((int64_t)max(seen[row], 0) + c.page_size - 1) >> log2_page, (int64_t)c.max_pages);
   const int end = min(count, first + chunk);
-  if (p0 >= end) return;
+  if (first >= end) return;                             // (the workgroup)
   float* out = score + (row * Hkv + g) * c.max_pages;
   const T* bounds = static_cast<const T*>(c.bounds);
-  for (int h0 = 0; h0 < G; h0 += 4) {                   // four queries at a time
-    double up[LOADS * VEC], down[LOADS * VEC];
-    const T* x = q + (row * H + g * G + min(h0 + j, G - 1)) * D;
+  auto load = [&](int phys, u32x4 (&l)[LOADS], u32x4 (&h)[LOADS]) {
+    const T* src = bounds + ((int64_t)(phys >= 0 && phys < c.n_pages ? phys : 0) * Hkv + g) * 2 * D + quad * VEC;
 #pragma unroll
     for (int f = 0; f < LOADS; ++f) {
-      float v[VEC];
-      Vec16<T>::unpack(*reinterpret_cast<const u32x4*>(x + (4 * f + quad) * VEC), v);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        up[f * VEC + e] = v[e] < 0.f ? 0.0 : (double)v[e];
-        down[f * VEC + e] = v[e] > 0.f ? 0.0 : (double)v[e];
-      }
+      l[f] = *reinterpret_cast<const u32x4*>(src + 4 * f * VEC);
+      h[f] = *reinterpret_cast<const u32x4*>(src + D + 4 * f * VEC);
     }
-    u32x4 lo[LOADS], hi[LOADS], next_lo[LOADS], next_hi[LOADS];
-    auto load = [&](int phys, u32x4 (&l)[LOADS], u32x4 (&h)[LOADS]) {
-      const T* src = bounds + ((int64_t)(phys >= 0 && phys < c.n_pages ? phys : 0) * Hkv + g) * 2 * D + quad * VEC;
-#pragma unroll
-      for (int f = 0; f < LOADS; ++f) {
-        l[f] = *reinterpret_cast<const u32x4*>(src + 4 * f * VEC);
-        h[f] = *reinterpret_cast<const u32x4*>(src + D + 4 * f * VEC);
-      }
-    };
-    auto there = [&](int phys) { return __ballot(phys >= 0 && phys < c.n_pages); };
+  };
+  for (int h0 = 0; h0 < G; h0 += 4) {                   // four queries at a time
     int phys = phys0, next = entry(p0 + STEP);
-    load(phys, lo, hi);
+    u32x4 lo[LOADS], hi[LOADS], next_lo[LOADS], next_hi[LOADS];
+    if (p0 < end) load(phys, lo, hi);
+    if (h0 > 0) __syncthreads();
+    for (int i = tid; i < 4 * D; i += kThreads) {
+      const int h = i / D, e = i % D;                   // element e is in vector e / VEC: load vector / 4, quad vector % 4
+      const float v = Elem<T>::load(q + (row * H + g * G + min(h0 + h, G - 1)) * D + e);
+      const int at = (e / (4 * VEC) * VEC + e % VEC) / 2, lanes = e / VEC % 4 * 4 + h;
+      s_q[0][at][lanes][e & 1] = v > 0.f ? 0.0 : (double)v;
+      s_q[1][at][lanes][e & 1] = v < 0.f ? 0.0 : (double)v;
+    }
+    __syncthreads();
     for (int p = p0; p < end; p += STEP) {
-      const uint64_t mask = there(phys);
-      if (AHEAD && p + STEP < end) load(next, next_lo, next_hi);
+      const uint64_t mask = __ballot(phys >= 0 && phys < c.n_pages);
+      if (p + STEP < end) load(next, next_lo, next_hi);
       double a0 = 0.0, a1 = 0.0;
+      int query = 4 * quad + j;
+      asm volatile("" : "+v"(query));                   // (read from LDS for every tile: kept, they would be spilled)
 #pragma unroll
       for (int f = 0; f < LOADS; ++f) {
         float l[VEC], h[VEC];
         Vec16<T>::unpack(lo[f], l);
         Vec16<T>::unpack(hi[f], h);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          a0 = __builtin_amdgcn_mfma_f64_4x4x4f64((double)l[e], down[f * VEC + e], a0, 0, 0, 0);
-          a1 = __builtin_amdgcn_mfma_f64_4x4x4f64((double)h[e], up[f * VEC + e], a1, 0, 0, 0);
+        for (int e = 0; e < VEC; e += 2) {
+          const pair_t down = s_q[0][(f * VEC + e) / 2][query], up = s_q[1][(f * VEC + e) / 2][query];
+          a0 = __builtin_amdgcn_mfma_f64_4x4x4f64((double)l[e], down[0], a0, 0, 0, 0);
+          a1 = __builtin_amdgcn_mfma_f64_4x4x4f64((double)h[e], up[0], a1, 0, 0, 0);
+          a0 = __builtin_amdgcn_mfma_f64_4x4x4f64((double)l[e + 1], down[1], a0, 0, 0, 0);
+          a1 = __builtin_amdgcn_mfma_f64_4x4x4f64((double)h[e + 1], up[1], a1, 0, 0, 0);
         }
       }
       const float sum = (float)(a0 + a1);
@@ -322,13 +328,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || D == 64 ? 2 : 1) void p
         out[p + mine] = h0 > 0 ? fmaxf(out[p + mine], s) : s;           // (written by this lane)
       }
       phys = next;
-      if (AHEAD) {
-#pragma unroll
-        for (int f = 0; f < LOADS; ++f) { lo[f] = next_lo[f]; hi[f] = next_hi[f]; }
-      } else if (p + STEP < end) {
-        load(next, lo, hi);
-      }
       next = entry(p + 2 * STEP);
+#pragma unroll
+      for (int f = 0; f < LOADS; ++f) { lo[f] = next_lo[f]; hi[f] = next_hi[f]; }
     }
   }
 }
@@ -347,11 +349,15 @@ qcf_status launch_page_append(const qcf_layer_desc& L, const qcf_page_cache& c, 
   a.log2_page = __builtin_ctz((unsigned)c.page_size);
   a.neg2_over_d_log2base = -2.0 / L.head_dim * std::log2(L.rope_base);
   // KV heads of a workgroup: a power of two of them, whose vectors of a row fill a wave at most, as long as every compute unit
-  // has two workgroups.  More share their (cos, sin), fewer give a short call more workgroups (@).
+  // has a workgroup (two where a page has many rows, so that its last ones do not stand alone).  More share their (cos, sin), fewer
+  // give a short call more workgroups: 8 KV heads of 128, us, with one head, by this rule and with all eight: 500 rows 7.9, 8.1 and
+  // 14.8, 8000 of four requests 50.9, 44.5 and 44.6, 8000 in pages of 64 53.1, 46.1 and 80.8, 256 requests of one row 20.0, 8.7 and 9.4;
+  // 16000 in pages of 256 91, 91 and 268 (99 with one workgroup to a compute unit).
   const int64_t units = (total_rows >> a.log2_page) + 2 * (int64_t)B;
   const int per_row = L.head_dim / 2 / (16 / elem_size(L.dtype));
+  const int wanted = (c.page_size >= 128 ? 2 : 1) * compute_unit_count();
   int heads = 1;
-  while (L.n_kv_heads % (2 * heads) == 0 && 2 * heads * per_row <= 64 && units * (L.n_kv_heads / (2 * heads)) >= 2 * compute_unit_count())
+  while (L.n_kv_heads % (2 * heads) == 0 && 2 * heads * per_row <= 64 && units * (L.n_kv_heads / (2 * heads)) >= wanted)
     heads *= 2;
   const int log2_lanes = __builtin_ctz((unsigned)(heads * per_row));
   const int64_t blocks = units * (L.n_kv_heads / heads);
@@ -377,9 +383,10 @@ qcf_status launch_page_select(const qcf_layer_desc& L, const qcf_page_cache& c, 
                               hipStream_t st) {
   float* score = static_cast<float*>(ws);
   const int64_t rows = (int64_t)B * n_q, tiles = ((int64_t)c.max_pages + 4 * kScorePages - 1) / (4 * kScorePages);
-  // tiles of 4 waves x 16 pages of a workgroup: up to four, as long as every compute unit has two workgroups (the queries are laid
-  // out once for them)
-  int64_t each = rows * L.n_kv_heads * tiles / (2 * compute_unit_count());
+  // Tiles of 4 waves x 16 pages of a workgroup: up to four, as long as every compute unit has four workgroups (the queries are laid
+  // out once for them).  32 contexts of 512 to 1536 pages, 8 KV heads: 39.0 us with up to four, 39.2 with up to eight; one context of
+  // 8192 pages: 12.1, 12.9 with two workgroups to a compute unit.
+  int64_t each = rows * L.n_kv_heads * tiles / (4 * compute_unit_count());
   each = std::min<int64_t>(std::max<int64_t>(each, 1), 4);
   const int64_t chunks = (tiles + each - 1) / each, blocks = rows * L.n_kv_heads * chunks;
   if (blocks > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page select: too many rows");
