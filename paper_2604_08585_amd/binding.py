@@ -456,7 +456,14 @@ class PageCache:
 
     def __init__(self, desc: PageCacheDesc, tensors: tuple):
         self.desc, self.tensors = desc, tensors
+        self.requests = tensors[3].shape[0]        # rows of the table
         self.ref = C.byref(desc)
+
+    def of(self, B: int):
+        """The descriptor for a call over B requests."""
+        if B > self.requests:
+            raise QcfError(f"{B} requests, {self.requests} rows in the table of pages")
+        return self.ref
 
 
 def page_cache(k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor], table: torch.Tensor) -> PageCache:
@@ -494,7 +501,7 @@ def qcf_page_append(desc: LayerDesc, cache: PageCache, B: int, q: Optional[torch
                     q_out: Optional[torch.Tensor]) -> None:
     """Rows of k and v behind what their requests hold (lens), keys and queries turned by pos on the way."""
     (qp, qs), (kp, ks), (vp, vs) = _rows(q), _rows(k), _rows(v)
-    _check(load_library().qcf_page_append(C.byref(desc), cache.ref, B, qp, qs, kp, ks, vp, vs, _ptr(row_off), total_rows,
+    _check(load_library().qcf_page_append(C.byref(desc), cache.of(B), B, qp, qs, kp, ks, vp, vs, _ptr(row_off), total_rows,
                                           _ptr(lens), _ptr(pos), _ptr(q_out), _stream()))
 
 
@@ -507,7 +514,7 @@ def qcf_page_select(desc: LayerDesc, cache: PageCache, B: int, n_q: int, q: torc
     if workspace is None:
         workspace = _workspace(qcf_page_select_workspace_bytes(desc, cache, B, n_q, n_keep), q.device)
     wp, wn = _ws_args(workspace)
-    _check(load_library().qcf_page_select(C.byref(desc), cache.ref, B, n_q, _ptr(q), _ptr(seen), n_keep, n_first, n_last,
+    _check(load_library().qcf_page_select(C.byref(desc), cache.of(B), B, n_q, _ptr(q), _ptr(seen), n_keep, n_first, n_last,
                                           _ptr(pages), wp, wn, _stream()))
 
 
@@ -522,5 +529,5 @@ def qcf_page_attn(desc: LayerDesc, cache: PageCache, B: int, n_q: int, q: torch.
     if workspace is None:
         workspace = _workspace(qcf_page_attn_workspace_bytes(desc, cache, B, n_q, n_keep), q.device)
     wp, wn = _ws_args(workspace)
-    _check(load_library().qcf_page_attn(C.byref(desc), cache.ref, B, n_q, _ptr(q), _ptr(seen), _ptr(pages), n_keep, _ptr(o_out),
+    _check(load_library().qcf_page_attn(C.byref(desc), cache.of(B), B, n_q, _ptr(q), _ptr(seen), _ptr(pages), n_keep, _ptr(o_out),
                                         _ptr(lse_out), wp, wn, _stream()))

@@ -31,7 +31,8 @@ struct PageAttnArgs {
   const int32_t* list;
   int n_keep, n_q, H, Hkv, G, log2_page;
   int contexts, rows, inner, slots, least, pad, part_rows;
-  float scale;                                           // log2(e) / sqrt(d)
+  float scale, scale_low;                                // log2(e) / sqrt(d), rounded down, and what that leaves (positive, so that a
+                                                         // product that is infinite keeps its sign)
   void* o;
   float* lse;
   float* part_o;
@@ -80,12 +81,18 @@ struct Place {
 
 __device__ __forceinline__ Contexts contexts_of(const PageAttnArgs& a, int lane) {
   Contexts c;
+  c.pad = a.pad;
+  c.apart = false;
+  if (a.contexts == 1) {                                 // (the latency of one request: no sums over the lanes)
+    c.tokens = (uint32_t)context_tokens(a, 0);
+    c.grains = c.room = c.incl = (uint32_t)pages::grains_of(c.tokens);
+    c.range = pages::range_of(c.grains, a.slots, a.least);
+    return c;
+  }
   c.tokens = lane < a.contexts ? (uint32_t)context_tokens(a, lane) : 0u;
   c.grains = lane < a.contexts ? (uint32_t)pages::grains_of(c.tokens) : 0u;
   c.room = lane < a.contexts ? c.grains + a.pad : 0u;
   c.incl = wave_incl(c.room);
-  c.pad = a.pad;
-  c.apart = false;
   if (a.contexts <= 64) {
     // little work: every context begins a range of its own if there are enough of them (two parts in a row take a workgroup
     // twice the latency: five requests of up to 600 tokens in float32 13.6 us, 10.4 so)
@@ -280,14 +287,19 @@ struct Walk {
           for (int f = 0; f < kLoads; ++f)
             z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[h][f]), __builtin_bit_cast(bf16x8, q[r][f]), z, 0, 0, 0);
         } else {
+          // (two sums side by side: half the chain, and less rounding)
+          floatx4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int f = 0; f < kLoads; ++f)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              z = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[h][f][e]), __uint_as_float(q[r][f][e]), z, 0, 0, 0);
+            for (int e = 0; e < 4; ++e) {
+              floatx4& sum = e & 1 ? y : z;
+              sum = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[h][f][e]), __uint_as_float(q[r][f][e]), sum, 0, 0, 0);
+            }
+          z += y;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[r][4 * h + i] = z[i] * a.scale;
+        for (int i = 0; i < 4; ++i) s[r][4 * h + i] = z[i];
       }
     // a tile that every row sees as a whole needs no mask
     bool whole = true;
@@ -309,6 +321,7 @@ struct Walk {
           top = fmaxf(top, s[r][i]);
         }
       }
+      top *= a.scale;
       if (__any(top > m[r] + kRoom)) {
         typedef unsigned u2v __attribute__((ext_vector_type(2)));
         u2v y = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
@@ -325,7 +338,9 @@ struct Walk {
       const float ref = m[r] == -INFINITY ? 0.f : m[r];               // (all logits so far -inf: weights of 0, not NaN)
 #pragma unroll
       for (int i = 0; i < kS; ++i) {
-        float e = __builtin_amdgcn_exp2f(s[r][i] - ref);
+        // (float32: the scale as two floats, so that a large logit does not lose the bits behind the first)
+        const float from = kHalf ? -ref : __builtin_fmaf(s[r][i], a.scale_low, -ref);
+        float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][i], a.scale, from));
         if (!whole) e = t.base[i >> 2] >= 0 && token(t, i) < lim[r] ? e : 0.f;
         p[r][i] = e;
         l[r] += e;
@@ -461,6 +476,7 @@ __device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MOD
     any = __shfl_xor((int)any, 32, 64) || any;
     if (any && w.m[r] == -INFINITY) l = NAN;             // only logits of -inf
     if (lane < 16) { s_m[wave][16 * r + lane] = w.m[r]; s_l[wave][16 * r + lane] = l; }
+    if (row0 + 16 * r + w.col >= a.rows) continue;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -641,7 +657,10 @@ qcf_status launch_page_attn(const qcf_layer_desc& L, const qcf_page_cache& c, in
   a.log2_page = __builtin_ctz((unsigned)c.page_size);
   a.contexts = d.contexts; a.rows = d.rows; a.inner = d.inner; a.slots = d.slots; a.least = d.least; a.pad = d.pad;
   a.part_rows = pages::part_rows(d);
-  a.scale = (float)(1.4426950408889634 / std::sqrt((double)L.head_dim));
+  const double scale = 1.4426950408889634 / std::sqrt((double)L.head_dim);
+  a.scale = (float)scale;
+  if (a.scale > scale) a.scale = std::nextafterf(a.scale, 0.f);
+  a.scale_low = (float)(scale - a.scale);
   a.o = o; a.lse = lse;
   a.part_o = static_cast<float*>(ws);
   a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + (pages::divides(d) ? pages::sums_bytes(L, d) : 0));

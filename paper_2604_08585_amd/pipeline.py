@@ -379,3 +379,86 @@ def host_chunk_caches(L: DeviceLayer, seed: int, n_layers: int):
             hv.copy_(torch.randn(vs.shape, generator=g).to(vs.dtype))
         out.append((hk, hv))
     return out
+
+
+# ------------------------------------------------------------------ decoding over the fused cache, in pages
+
+@dataclasses.dataclass
+class PagedLayer:
+    """A fused layer's cache in pages, room for new tokens behind every request, and what a decoding step of `new` tokens needs."""
+    desc: qb.LayerDesc
+    B: int
+    new: int                       # tokens of each request in one step
+    keep: int                      # pages that attention is cut down to (0: all)
+    first: int                     # of them, always kept: the first pages of a request
+    last: int                      # and its last ones
+    cache: qb.PageCache
+    held: torch.Tensor             # [B] int32: tokens that a request holds
+    seen: torch.Tensor             # [B, new] int32: tokens that each new row sees
+    pos: torch.Tensor              # [B * new] int32: absolute positions of the new rows
+    row_off: torch.Tensor          # [B + 1] int64: rows of a request in a step
+    qkv: torch.Tensor              # [B * new, (H + 2 H_kv) d]
+    parts: tuple                   # its queries, keys and values [B * new, heads, d]
+    q: torch.Tensor                # [B, new, H, d]
+    pages: Optional[torch.Tensor]  # [B, new, H_kv, keep] int32
+    o: torch.Tensor                # [B, new, H, d]
+    lse: torch.Tensor              # [B, new, H] float32
+    ws_linear: Optional[torch.Tensor]
+    ws_select: Optional[torch.Tensor]
+    ws_attn: Optional[torch.Tensor]
+
+
+def paged_layer(L: DeviceLayer, more: int, page_size: int = 16, new: int = 1, keep: int = 0, first: int = 1,
+                last: int = 1) -> PagedLayer:
+    """The fused cache of a layer in pages, with room for `more` tokens behind every request's context (which begins at position
+    0).  keep > 0: each new row's attention is cut down to that many pages for each KV head, the first `first` and the last `last`
+    among them; the pages' bounds are kept for that."""
+    desc, dev, dt = L.desc, L.k_fused.device, L.k_fused.dtype
+    H, Hkv, d = desc.n_q_heads, desc.n_kv_heads, desc.head_dim
+    counts = [-(-(n + more) // page_size) for n in L.ctx_lens]
+    width, n_pages = max(counts + [1]), max(sum(counts), 1)
+    table = np.full((L.B, width), -1, dtype=np.int32)
+    at = 0
+    for b, n in enumerate(counts):
+        table[b, :n] = np.arange(at, at + n, dtype=np.int32)
+        at += n
+    empty = lambda *s, dtype=dt: torch.empty(*s, dtype=dtype, device=dev)
+    cache = qb.page_cache(empty(n_pages, page_size, Hkv, d), empty(n_pages, page_size, Hkv, d),
+                          empty(n_pages, Hkv, 2, d) if keep else None, torch.from_numpy(table).to(dev))
+    rows = L.B * new
+    held = torch.tensor(L.ctx_lens, dtype=torch.int32, device=dev)
+    step = torch.arange(new, dtype=torch.int32, device=dev)
+    qkv = empty(rows, (H + 2 * Hkv) * d)
+    P = PagedLayer(
+        desc=desc, B=L.B, new=new, keep=keep, first=first, last=last, cache=cache, held=held, seen=held[:, None] + 1 + step,
+        pos=(held[:, None] + step).flatten(), row_off=torch.arange(L.B + 1, dtype=torch.int64, device=dev) * new, qkv=qkv,
+        parts=tuple(t.unflatten(1, (-1, d)) for t in qkv.split([H * d, Hkv * d, Hkv * d], 1)), q=empty(L.B, new, H, d),
+        pages=empty(L.B, new, Hkv, keep, dtype=torch.int32) if keep else None, o=empty(L.B, new, H, d),
+        lse=empty(L.B, new, H, dtype=torch.float32),
+        ws_linear=_ws(qb.qcf_linear_workspace_bytes(desc, rows, desc.d_model, (H + 2 * Hkv) * d), dev),
+        ws_select=_ws(qb.qcf_page_select_workspace_bytes(desc, cache, L.B, new, keep), dev) if keep else None,
+        ws_attn=_ws(qb.qcf_page_attn_workspace_bytes(desc, cache, L.B, new, keep), dev))
+    qb.qcf_page_append(desc, cache, L.B, None, L.k_fused[:L.total_ctx], L.v_fused[:L.total_ctx], L.ctx_off, L.total_ctx,
+                       torch.zeros_like(held), None, None)
+    return P
+
+
+def decode_step(P: PagedLayer, x: torch.Tensor, w_qkv: torch.Tensor) -> torch.Tensor:
+    """One layer's attention for `new` tokens behind each request: x [B * new, d_model] (normed hidden states) is projected, keys and
+    values go into the cache, rotated on the way, and the queries attend.  Returns o [B, new, H, d].  Lengths and positions live
+    on the device and are not moved: call `advance` after a step's last layer, or to accept fewer tokens than were drafted."""
+    rows, dm = x.shape
+    qb.qcf_linear(P.desc, x, rows, dm, w_qkv, P.qkv.shape[1], None, P.qkv, P.ws_linear)
+    q, k, v = P.parts
+    qb.qcf_page_append(P.desc, P.cache, P.B, q, k, v, P.row_off, rows, P.held, P.pos, P.q.flatten(0, 1))
+    if P.keep:
+        qb.qcf_page_select(P.desc, P.cache, P.B, P.new, P.q, P.seen, P.keep, P.first, P.last, P.pages, P.ws_select)
+    qb.qcf_page_attn(P.desc, P.cache, P.B, P.new, P.q, P.seen, P.pages, P.keep, P.o, P.lse, P.ws_attn)
+    return P.o
+
+
+def advance(P: PagedLayer, tokens: int) -> None:
+    """Every request holds `tokens` tokens more (fewer than were appended: the others' slots are written again)."""
+    P.held += tokens
+    P.seen += tokens
+    P.pos += tokens

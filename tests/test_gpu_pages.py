@@ -16,6 +16,7 @@ import torch
 from oracle import qcf_oracle as orc
 from paper_2604_08585_amd import binding as qb
 from paper_2604_08585_amd import inputs
+import page_rules
 from gpu_util import DEV, i32, i64, to_np
 
 pytestmark = pytest.mark.gpu
@@ -247,11 +248,42 @@ ATTENTIONS = [
 
 
 @pytest.mark.parametrize("case", ATTENTIONS)
+def test_attention_over_all_pages_in_ranges(case):
+    """The same contexts in a table that is wide enough for long ones: divided over the GPU and joined."""
+    dtype, H, Hkv, D, page, order, seen = case
+    rng = np.random.default_rng(15)
+    seen = np.array(seen, dtype=np.int32)
+    sh = shape(H, Hkv, D, dtype)
+    p = Paged(rng, sh, page, seen.max(1).tolist(), order, width=65536 // page)
+    assert page_rules.division(p.desc, p.cache, seen.shape[0], seen.shape[1], 0)["whole"] == 0
+    _attend_and_check(p, rng, seen)
+
+
+@pytest.mark.parametrize("case", ATTENTIONS)
 def test_attention_over_all_pages(case):
     dtype, H, Hkv, D, page, order, seen = case
     rng = np.random.default_rng(5)
     seen = np.array(seen, dtype=np.int32)
     p = Paged(rng, shape(H, Hkv, D, dtype), page, seen.max(1).tolist(), order)
+    _attend_and_check(p, rng, seen)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D,page,seen", [
+    # rows of one request that see very different parts of it, in ranges that begin and end among them
+    ("bf16", 8, 2, 128, 16, [[3000, 17, 1500, 2999], [40, 900, 0, 33]]),
+    ("bf16", 16, 2, 128, 32, [[5000, 2500, 0, 64, 4999], [1, 2, 3, 4, 2000]]),           # 40 rows: three blocks of 16 or two of 32
+    ("bf16", 128, 2, 64, 16, [[700], [2100]]),                                           # 64 rows of one token
+    ("f32", 24, 2, 128, 64, [[1000, 999, 31], [3, 640, 0]]),
+    ("f32", 8, 1, 64, 16, [[4000, 100, 3999, 2048, 2047, 0, 5, 9]]),
+    # more contexts than ranges (64 KV heads: 8 ranges), and more than 64
+    ("bf16", 64, 64, 64, 16, [[37 * i % 900 + 1] for i in range(30)]),
+    ("bf16", 32, 32, 128, 16, [[97 * i % 1300] for i in range(80)]),
+    ("f32", 16, 16, 64, 32, [[61 * i % 500, 7 * i] for i in range(70)])])
+def test_attention_of_uneven_rows_and_contexts_in_ranges(dtype, H, Hkv, D, page, seen):
+    rng = np.random.default_rng(16)
+    seen = np.array(seen, dtype=np.int32)
+    p = Paged(rng, shape(H, Hkv, D, dtype), page, np.maximum(seen.max(1), 1).tolist(), width=131072 // page)
+    assert page_rules.division(p.desc, p.cache, seen.shape[0], seen.shape[1], 0)["whole"] == 0
     _attend_and_check(p, rng, seen)
 
 
@@ -265,12 +297,13 @@ def test_attention_divided_over_long_and_many_contexts(dtype, H, Hkv, D, page, l
     assert torch.isfinite(o.float()).all()
 
 
-def test_attention_does_not_read_what_is_not_seen():
+@pytest.mark.parametrize("width", [9, 8192])                  # contexts taken whole, and in ranges
+def test_attention_does_not_read_what_is_not_seen(width):
     """NaN and infinities in slots behind `seen`, in absent pages' place (page 0 of the pool) and in pages of no request."""
     rng = np.random.default_rng(7)
-    for dtype, D, n_q in [("bf16", 128, 1), ("bf16", 64, 3), ("f32", 64, 2), ("bf16", 128, 8), ("f32", 128, 1)]:
+    for dtype, D, n_q in [("bf16", 128, 1), ("bf16", 64, 3), ("f32", 64, 2), ("bf16", 128, 8), ("f32", 128, 1), ("f32", 128, 6)]:
         seen = np.array([[75 - n_q + 1 + i for i in range(n_q)], [16] * n_q, [33] * n_q, [0] * n_q], dtype=np.int32)
-        p = Paged(rng, shape(8, 2, D, dtype), 16, [75, 16, 33, 40], width=9)
+        p = Paged(rng, shape(8, 2, D, dtype), 16, [75, 16, 33, 40], width=width)
         free = np.setdiff1d(np.arange(len(p.k)), p.table)
         p.k[free], p.v[free] = np.nan, np.inf
         for b, n in enumerate([75, 16, 33, 0]):
@@ -286,14 +319,16 @@ def test_attention_does_not_read_what_is_not_seen():
         _attend_and_check(p, rng, seen)
 
 
+@pytest.mark.parametrize("width", [4, 16384])                 # (whole, in ranges)
+@pytest.mark.parametrize("H", [8, 20])                        # rows in one tile and in two
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
-def test_values_that_only_later_drafts_see_do_not_reach_earlier_ones(dtype, D):
+def test_values_that_only_later_drafts_see_do_not_reach_earlier_ones(dtype, D, H, width):
     rng = np.random.default_rng(8)
-    p = Paged(rng, shape(8, 2, D, dtype), 16, [60])
+    p = Paged(rng, shape(H, 2, D, dtype), 16, [60], width=width)
     p.v[p.table[0, 58 // 16], 58 % 16] = np.inf
     p.v[p.table[0, 59 // 16], 59 % 16] = np.nan
     p.upload()
-    q = torch.from_numpy(normal(rng, (1, 4, 8, D), dtype)).to(device=DEV, dtype=p.dt)
+    q = torch.from_numpy(normal(rng, (1, 4, H, D), dtype)).to(device=DEV, dtype=p.dt)
     o, alone = torch.empty_like(q), torch.empty_like(q)
     qb.qcf_page_attn(p.desc, p.cache, 1, 4, q, i32([[57, 58, 59, 60]]), None, 0, o, None)
     qb.qcf_page_attn(p.desc, p.cache, 1, 4, q, i32([[57, 58, 57, 57]]), None, 0, alone, None)
@@ -328,12 +363,15 @@ def test_logits_that_are_not_finite():
         assert torch.isfinite(lse[0, 0, 0]) and torch.isfinite(lse[0, 0, 3])
 
 
-@pytest.mark.parametrize("dtype,H,Hkv,D,page", [("bf16", 32, 8, 128, 16), ("bf16", 8, 2, 64, 64), ("f32", 4, 2, 64, 32)])
-def test_attention_over_listed_pages(dtype, H, Hkv, D, page):
+@pytest.mark.parametrize("dtype,H,Hkv,D,page,keep", [
+    ("bf16", 32, 8, 128, 16, 11), ("bf16", 8, 2, 64, 64, 11), ("f32", 4, 2, 64, 32, 11),
+    ("bf16", 32, 8, 128, 16, 3000), ("f32", 4, 2, 64, 32, 900), ("bf16", 24, 1, 128, 32, 2000)])     # (long lists are divided)
+def test_attention_over_listed_pages(dtype, H, Hkv, D, page, keep):
     rng = np.random.default_rng(10)
     lens = [page * 21 + 3, page * 2, 1, page * 9 - 1]
-    p = Paged(rng, shape(H, Hkv, D, dtype), page, lens)
-    n_q, keep = 2, 11
+    p = Paged(rng, shape(H, Hkv, D, dtype), page, lens, width=4096 if keep > 100 else None)
+    n_q = 2
+    assert page_rules.division(p.desc, p.cache, 4, n_q, keep)["whole"] == (keep < 100)
     seen = np.array([[n - 1, n] for n in lens], dtype=np.int32)
     pages = np.full((4, n_q, Hkv, keep), -1, dtype=np.int32)
     for b, n in enumerate(lens):
@@ -343,7 +381,7 @@ def test_attention_over_listed_pages(dtype, H, Hkv, D, page):
                 some = rng.permutation(count)[:min(keep, max(1, count - 1))]
                 pages[b, i, g, :len(some)] = some
     pages[0, 0, 0, :] = -1                                      # nothing at all
-    pages[0, 0, 1, 3:6] = [-7, 22, 10 ** 9]                     # no pages of this row
+    pages[0, 0, Hkv - 1, 3:6] = [-7, 22, 10 ** 9]               # no pages of this row
     pages[0, 1, 0, :4] = [21, 3, 3, 0]                          # the same page twice
     _attend_and_check(p, rng, seen, pages)
 
@@ -356,6 +394,75 @@ def test_a_list_of_all_pages_is_no_list():
     a, _ = _attend_and_check(p, rng, seen, None, q)
     b, _ = _attend_and_check(p, rng, seen, np.tile(np.arange(40, dtype=np.int32)[::-1], (1, 1, 2, 1)), q)
     assert (a.float() - b.float()).abs().max() <= 2.0 ** -7 * a.float().abs().max()
+
+
+def test_parts_without_finite_logits_beside_others():
+    """A part of a context, joined with others, whose logits are all -inf weighs nothing; a context of such parts is NaN."""
+    rng = np.random.default_rng(17)
+    for dtype, D in [("bf16", 128), ("bf16", 64), ("f32", 64)]:
+        p = Paged(rng, shape(2, 2, D, dtype), 16, [2000, 300], width=8192)
+        keys = p.k[p.table[0, :125]]
+        keys[10:60, :, 0] = -np.inf                            # head 0: tokens 160..959
+        keys[:, :, 1] = -np.inf
+        p.k[p.table[0, :125]] = keys
+        p.upload()
+        q = torch.ones(2, 1, 2, D, device=DEV, dtype=p.dt)
+        o, lse = torch.empty_like(q), torch.empty(2, 1, 2, device=DEV)
+        qb.qcf_page_attn(p.desc, p.cache, 2, 1, q, i32([[2000], [300]]), None, 0, o, lse)
+        torch.cuda.synchronize()
+        got = to_np(o)
+        z = np.concatenate([keys[:10, :, 0], keys[60:, :, 0]]).reshape(-1, D).astype(np.float64).sum(-1) / math.sqrt(D)
+        v = np.concatenate([p.v[p.table[0, :10], :, 0], p.v[p.table[0, 60:125], :, 0]]).reshape(-1, D).astype(np.float64)
+        w = np.exp(z - z.max())
+        ref = w @ v / w.sum()
+        assert np.all(np.abs(got[0, 0, 0] - ref) <= HALF_STEP[dtype] * np.abs(ref) + 2.0 ** -10 * np.abs(v).max())
+        assert np.isnan(got[0, 0, 1]).all() and np.isfinite(got[1]).all() and np.isfinite(to_np(lse)[0, 0, 0])
+
+
+def test_lengths_beyond_the_table_and_below_nothing():
+    rng = np.random.default_rng(18)
+    p = Paged(rng, shape(8, 2, 128, "bf16"), 16, [64, 48])
+    q = torch.from_numpy(normal(rng, (2, 2, 8, 128), "bf16")).to(device=DEV, dtype=p.dt)
+    outs = []
+    for seen in ([[2 ** 31 - 1, -5], [1000, 48]], [[64, 0], [48, 48]]):
+        o, lse = torch.empty_like(q), torch.empty(2, 2, 8, device=DEV)
+        pages = torch.empty(2, 2, 2, 3, dtype=torch.int32, device=DEV)
+        qb.qcf_page_attn(p.desc, p.cache, 2, 2, q, i32(seen), None, 0, o, lse)
+        qb.qcf_page_select(p.desc, p.cache, 2, 2, q, i32(seen), 3, 1, 1, pages)
+        outs.append((o, lse, pages))
+    torch.cuda.synchronize()
+    for a, b in zip(outs[0][:2], outs[1][:2]):
+        assert torch.equal(a, b)
+    # (the last pages of the table are not there for the second request: its own last page is the third)
+    assert torch.equal(outs[0][2][0], outs[1][2][0]) and not outs[0][0][0, 1].any()
+
+
+def test_a_pool_beyond_32_bits_of_elements():
+    """Pages 16 MB apart: offsets of 6e9 elements, appended to, selected from and attended to."""
+    rng = np.random.default_rng(19)
+    sh = shape(8, 2, 128, "bf16")
+    n_pages, stride = 720, 1 << 23
+    pools = [torch.empty(n_pages * stride, dtype=torch.bfloat16, device=DEV).as_strided((n_pages, 16, 2, 128), (stride, 256, 128, 1)) for _ in range(2)]
+    bounds = torch.empty(n_pages, 2, 2, 128, dtype=torch.bfloat16, device=DEV)
+    table = np.array([[719, 3, 700, 650, 1, 718]], dtype=np.int32)
+    cache = qb.page_cache(*pools, bounds, i32(table))
+    desc = qb.make_desc(sh)
+    k, v, q = (normal(rng, (n, h, 128), "bf16") for n, h in ((90, 2), (90, 2), (1, 8)))
+    dev = lambda a: torch.from_numpy(a).to(device=DEV, dtype=torch.bfloat16)
+    qb.qcf_page_append(desc, cache, 1, None, dev(k), dev(v), i64([0, 90]), 90, i32([0]), None, None)
+    pages = torch.empty(1, 1, 2, 4, dtype=torch.int32, device=DEV)
+    o, some = torch.empty(1, 1, 8, 128, dtype=torch.bfloat16, device=DEV), torch.empty(1, 1, 8, 128, dtype=torch.bfloat16, device=DEV)
+    qb.qcf_page_attn(desc, cache, 1, 1, dev(q), i32([[90]]), None, 0, o, None)
+    qb.qcf_page_select(desc, cache, 1, 1, dev(q), i32([[90]]), 4, 0, 1, pages)
+    qb.qcf_page_attn(desc, cache, 1, 1, dev(q), i32([[90]]), pages, 4, some, None)
+    torch.cuda.synchronize()
+    small = np.zeros((6, 16, 2, 128)), np.zeros((6, 16, 2, 128)), np.zeros((6, 2, 2, 128))
+    kp, vp, bp = orc.page_append(small, np.arange(6)[None], [0], [0, 90], k, v, None, 1e4)
+    want = orc.page_select(orc.page_scores(q[0], bp, np.arange(6)), 4, 0, 1)
+    assert np.array_equal(pages.cpu().numpy()[0, 0], want)
+    for got, listed in ((o, None), (some, want)):
+        ref, _ = orc.page_attn(q[0], kp, vp, np.arange(6), 90, listed)
+        assert np.all(np.abs(to_np(got)[0, 0] - ref) <= 2.0 ** -8 * np.abs(ref) + 1e-3)
 
 
 # ------------------------------------------------------------------ selection
@@ -469,3 +576,44 @@ def test_a_step_replays_from_a_captured_graph_and_on_another_stream():
         for got, want in zip((o, lse, pages, p.kd, p.bd), eager[i]):
             assert torch.equal(got, want), i
         grow(1)
+
+
+def test_two_graphs_that_share_a_workspace_take_turns():
+    """Two captured calls over different requests, divided, replayed in turn with eager calls between them: the same bits each time."""
+    rng = np.random.default_rng(20)
+    sh = shape(32, 8, 128, "bf16")
+    a, b = (Paged(rng, sh, 16, lens, width=4096) for lens in ([3000, 50], [700, 900, 4000]))
+    calls = []
+    ws = torch.empty(max(qb.qcf_page_attn_workspace_bytes(sh_p.desc, sh_p.cache, n, 1, 0) for sh_p, n in ((a, 2), (b, 3))), dtype=torch.uint8, device=DEV)
+    for p, lens in ((a, [3000, 50]), (b, [700, 900, 4000])):
+        q = torch.from_numpy(normal(rng, (len(lens), 1, 32, 128), "bf16")).to(device=DEV, dtype=p.dt)
+        o, lse = torch.empty_like(q), torch.empty(len(lens), 1, 32, device=DEV)
+        calls.append((lambda p=p, q=q, s=i32(lens)[:, None].contiguous(), o=o, lse=lse: qb.qcf_page_attn(p.desc, p.cache, len(q), 1, q, s, None, 0, o, lse, ws), o, lse))
+    graphs, want = [], []
+    for call, o, lse in calls:
+        call()
+        torch.cuda.synchronize()
+        want.append((o.clone(), lse.clone()))
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call()
+        graphs.append(g)
+    for turn in range(3):
+        for i in (0, 1):
+            calls[i][1].fill_(2.0), calls[i][2].fill_(2.0)
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(calls[i][1], want[i][0]) and torch.equal(calls[i][2], want[i][1]), (turn, i)
+            calls[1 - i][0]()
+            torch.cuda.synchronize()
+            assert torch.equal(calls[1 - i][1], want[1 - i][0]), (turn, i)
+
+
+def test_append_of_many_requests():
+    """More requests than a wave has lanes, some without rows, lengths all over a page."""
+    for dtype, B in [("bf16", 300), ("f32", 65), ("bf16", 64)]:
+        rng = np.random.default_rng(21)
+        lens = rng.integers(0, 40, B).tolist()
+        new = (rng.integers(0, 5, B) * (rng.random(B) < 0.8)).astype(int).tolist()
+        p = Paged(rng, shape(4, 2, 64, dtype), 16, [a + b for a, b in zip(lens, new)], width=4)
+        _check_append(p, *_append(p, rng, lens, new, True), True)
