@@ -184,28 +184,43 @@ struct Walk {
     w.phys = p < count && phys < a.c.n_pages ? phys : -1;
   }
 
-  __device__ __forceinline__ void load(Tile& t, int64_t at) {
+  // where the parts of a tile are; a page that is not there: page 0 is read instead, and nothing of it used
+  struct Where {
+    int base[kSub];
+    int64_t off[kSub];
+  };
+  __device__ __forceinline__ Where find(int64_t at) {
     const int mask = a.c.page_size - 1;
     const int last = (int)((at + kTokens - 1) >> a.log2_page);
     if (last - w.first >= 64) open((int)(at >> a.log2_page));
+    Where r;
 #pragma unroll
     for (int h = 0; h < kSub; ++h) {
       const int64_t mine = at + 16 * h;
       const int i = (int)(mine >> a.log2_page) - w.first;
       const int slot = (int)mine & mask;
-      int phys = __builtin_amdgcn_readlane(w.phys, i);
+      const int phys = __builtin_amdgcn_readlane(w.phys, i);
       const int page = __builtin_amdgcn_readlane(w.page, i);
-      const bool there = phys >= 0 && mine < end;
-      t.base[h] = there ? (page << a.log2_page) + slot : -1;
-      // (a page that is not there: page 0 is read instead, and nothing of it used)
-      phys = max(phys, 0);
-      const int64_t off = phys * a.c.page_stride + g * a.c.head_stride + slot * a.c.slot_stride;
-      const char* k = reinterpret_cast<const char*>(static_cast<const T*>(a.c.k) + off);
-      const char* v = reinterpret_cast<const char*>(static_cast<const T*>(a.c.v) + off);
-      const uint32_t stride = (uint32_t)a.c.slot_stride * sizeof(T);
+      r.base[h] = phys >= 0 && mine < end ? (page << a.log2_page) + slot : -1;
+      r.off[h] = max(phys, 0) * a.c.page_stride + g * a.c.head_stride + slot * a.c.slot_stride;
+    }
+    return r;
+  }
+  __device__ __forceinline__ void load_keys(Tile& t, const Where& r) const {
+    const uint32_t stride = (uint32_t)a.c.slot_stride * sizeof(T);
 #pragma unroll
-      for (int f = 0; f < kLoads; ++f)
-        t.k[h][f] = *reinterpret_cast<const u32x4*>(k + (col * stride + 16 * quad + 64 * f));
+    for (int h = 0; h < kSub; ++h) {
+      const char* k = reinterpret_cast<const char*>(static_cast<const T*>(a.c.k) + r.off[h]);
+#pragma unroll
+      for (int f = 0; f < kLoads; ++f) t.k[h][f] = *reinterpret_cast<const u32x4*>(k + (col * stride + 16 * quad + 64 * f));
+    }
+  }
+  __device__ __forceinline__ void load_values(Tile& t, const Where& r) const {
+    const uint32_t stride = (uint32_t)a.c.slot_stride * sizeof(T);
+#pragma unroll
+    for (int h = 0; h < kSub; ++h) {
+      const char* v = reinterpret_cast<const char*>(static_cast<const T*>(a.c.v) + r.off[h]);
+      t.base[h] = r.base[h];
 #pragma unroll
       for (int j = 0; j < kV / kSub; ++j) {
         const int token = kHalf ? j : j & 3, part = kHalf ? 0 : j >> 2;
@@ -214,15 +229,21 @@ struct Walk {
       }
     }
   }
+  __device__ __forceinline__ void load(Tile& t, int64_t at) {
+    const Where r = find(at);
+    load_keys(t, r);
+    load_values(t, r);
+  }
 
   // products of the tile's values with the weights, added to c
-  __device__ __forceinline__ void values(const Tile& t, const float (&p)[RT][kS], floatx4 (&c)[RT][kE]) const {
+  template <int N>
+  __device__ __forceinline__ void values(const Tile& t, const float (&p)[N][kS], floatx4 (&c)[N][kE]) const {
     if constexpr (kHalf) {
       // weights as two bf16 terms, of 16 bits together: cut off, and what that left, rounded.  (The second term of a weight that
       // is not 0 is kept from being 0, so that an infinite value comes out infinite and not NaN.)
-      bf16x8 hi[RT], lo[RT];
+      bf16x8 hi[N], lo[N];
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
+      for (int r = 0; r < N; ++r) {
         u32x4 ph, pl;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -244,7 +265,7 @@ struct Walk {
           vt[i] = __builtin_amdgcn_perm(t.v[2 * i + 1][e / 2], t.v[2 * i][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
         const bf16x8 va = __builtin_bit_cast(bf16x8, vt);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
+        for (int r = 0; r < N; ++r) {
           c[r][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, hi[r], c[r][e], 0, 0, 0);
           c[r][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, lo[r], c[r][e], 0, 0, 0);
         }
@@ -255,7 +276,7 @@ struct Walk {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int r = 0; r < RT; ++r)
+          for (int r = 0; r < N; ++r)
             c[r][4 * (j >> 2) + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.v[j][e]), p[r][j & 3], c[r][4 * (j >> 2) + e], 0, 0, 0);
     }
   }
@@ -274,8 +295,9 @@ struct Walk {
   }
 
   // CAREFUL: the tile may have tokens that only some of the rows see
-  template <bool CAREFUL>
-  __device__ __forceinline__ void step(Tile& t) {
+  // (after_logits(): the keys' registers are free)
+  template <bool CAREFUL, typename F>
+  __device__ __forceinline__ void step(Tile& t, F&& after_logits) {
     float s[RT][kS];
 #pragma unroll
     for (int h = 0; h < kSub; ++h)
@@ -301,6 +323,7 @@ struct Walk {
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[r][4 * h + i] = z[i];
       }
+    after_logits();
     // a tile that every row sees as a whole needs no mask
     bool whole = true;
 #pragma unroll
@@ -356,19 +379,21 @@ struct Walk {
       const int at = max(i * a.G, row0) - row0;          // a row of it in the workgroup
       Tile mine = t;
       clear(mine, __builtin_amdgcn_readlane(RT == 2 && at >= 16 ? lim[RT - 1] : lim[0], at & 15));
-      floatx4 c[RT][kE];
-#pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int e = 0; e < kE; ++e) c[r][e] = floatx4{0.f, 0.f, 0.f, 0.f};
-      values(mine, p, c);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const bool here = row_of(r) / a.G == i;
+        if (!__any(here)) continue;
+        float one[1][kS];
+        floatx4 c[1][kE];
+#pragma unroll
+        for (int y = 0; y < kS; ++y) one[0][y] = p[r][y];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) c[0][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+        values(mine, one, c);
 #pragma unroll
         for (int e = 0; e < kE; ++e)
 #pragma unroll
-          for (int y = 0; y < 4; ++y) acc[r][e][y] += here ? c[r][e][y] : 0.f;
+          for (int y = 0; y < 4; ++y) acc[r][e][y] += here ? c[0][e][y] : 0.f;
       }
     }
   }
@@ -377,17 +402,35 @@ struct Walk {
   // way (its registers hold what each row's product takes there), those that only some of them see.
   __device__ __forceinline__ void run(int64_t at) {
     const int64_t shared = MODE == kSeveral && lim_lo < lim_hi ? min(end, (int64_t)(lim_lo & -kTokens)) : end;
-    if (at < shared) {
+    auto nothing = [] {};
+    if constexpr (RT == 2 && D == 128) {
+      // (no registers for a second tile: the next keys are asked for once the logits are there, the next values after the products)
+      if (at < shared) {
+        Tile t;
+        load(t, at);
+        for (; at < shared; at += kStep) {
+          Where next;
+          const bool more = at + kStep < shared;
+          step<false>(t, [&] {
+            if (more) {
+              next = find(at + kStep);
+              load_keys(t, next);
+            }
+          });
+          if (more) load_values(t, next);
+        }
+      }
+    } else if (at < shared) {
       Tile t0, t1;
       load(t0, at);
       while (true) {
         at += kStep;
         if (at < shared) load(t1, at);
-        step<false>(t0);
+        step<false>(t0, nothing);
         if (at >= shared) break;
         at += kStep;
         if (at < shared) load(t0, at);
-        step<false>(t1);
+        step<false>(t1, nothing);
         if (at >= shared) break;
       }
     }
@@ -395,7 +438,7 @@ struct Walk {
       for (; at < end; at += kStep) {
         Tile t;
         load(t, at);
-        step<true>(t);
+        step<true>(t, nothing);
       }
     }
   }
