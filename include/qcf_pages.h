@@ -45,7 +45,8 @@ typedef struct qcf_page_cache {
  * Bounds (where the cache has them) are joined with the stored keys of the rows; a page whose slot 0 is written starts anew.
  * Rows whose token would lie beyond max_pages pages or before token 0, or whose page is not there, are not stored (their queries
  * are still turned).  Rows behind row_off[B] are left as they were, and so are slots that get no row.  A page that is written
- * must be in the table once only. */
+ * must be in the table once only, and the rows must not lie in the cache.  A slot that is written again leaves its page's bounds
+ * wider than they need be, until slot 0 is. */
 qcf_status qcf_page_append(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, const void* q, int64_t q_stride,
                            const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int64_t* row_off_dev,
                            int64_t total_rows, const int32_t* len_dev, const int32_t* pos_dev, void* q_out, void* stream);

@@ -48,7 +48,7 @@ __device__ __forceinline__ float largest(float a, float b) { return __builtin_el
 
 // Request of a unit: units of request b start at row_off[b] / page + 2 b, which leaves room for every page that its rows can touch
 // (n rows touch at most floor((n - 1) / page) + 2), so that no sum over the requests stands in front of the rows.  Every wave
-// counts the requests that start at or before the unit; offsets and lengths of the first 64 are on their way together.
+// looks for the last request that starts at or before the unit; offsets and lengths of the first 64 are on their way together.
 struct Request {
   int b;
   int64_t r0, r1, len, unit0;     // its rows, the tokens that it holds, its first unit
@@ -60,10 +60,17 @@ __device__ __forceinline__ Request request_of(const AppendArgs& a, int64_t unit,
   const int64_t off = clamped(a.row_off[mine]), next = clamped(a.row_off[mine + 1]);
   const int len = a.len[mine];
   int before = (int)__popcll(__ballot(lane >= 1 && lane < a.B && first(lane, off) <= unit));
-  for (int b0 = 64; b0 < a.B; b0 += 64) {
-    const int b = b0 + lane;
-    const int64_t o = clamped(a.row_off[min(b, a.B - 1)]);
-    before += (int)__popcll(__ballot(b < a.B && first(b, o) <= unit));
+  if (a.B > 64) {
+    // the request lies in [at, end): 64 places of that are looked at a time
+    int at = 0, end = a.B;
+    while (end - at > 1) {
+      const int step = (end - at + 63) / 64, b = at + lane * step;
+      const int64_t o = clamped(a.row_off[min(b, a.B - 1)]);
+      const int n = (int)__popcll(__ballot(b < end && first(b, o) <= unit));
+      at += max(n - 1, 0) * step;
+      end = min(end, at + step);
+    }
+    before = at;
   }
   Request r;
   r.b = before;

@@ -611,7 +611,7 @@ def test_two_graphs_that_share_a_workspace_take_turns():
 
 def test_append_of_many_requests():
     """More requests than a wave has lanes, some without rows, lengths all over a page."""
-    for dtype, B in [("bf16", 300), ("f32", 65), ("bf16", 64)]:
+    for dtype, B in [("bf16", 300), ("f32", 65), ("bf16", 64), ("f32", 4097), ("bf16", 4500)]:
         rng = np.random.default_rng(21)
         lens = rng.integers(0, 40, B).tolist()
         new = (rng.integers(0, 5, B) * (rng.random(B) < 0.8)).astype(int).tolist()
