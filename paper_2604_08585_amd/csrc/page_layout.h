@@ -47,7 +47,7 @@ struct Division {
 inline bool takes_whole(const qcf_layer_desc& L, int64_t workgroups, int64_t longest) {
   const int64_t bytes = longest * 2 * L.head_dim * (L.dtype == QCF_DTYPE_BF16 ? 2 : 4);
   const int64_t alone = std::max<int64_t>(30, 200 - workgroups * 256 / compute_unit_count());      // of 200
-  return bytes * alone <= (int64_t)(290 << 10) * 200;
+  return bytes * alone <= (int64_t)(272 << 10) * 200;
 }
 
 inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, int32_t n_keep) {
