@@ -20,6 +20,8 @@ namespace pages {
 constexpr int kWaves = 4;                 // of a workgroup; each takes every fourth tile of its part of a context
 constexpr int kWholeWaves = 8;            // of a workgroup that has a context as a whole
 constexpr int kGrain = 32;                // contexts are divided at multiples of this many tokens
+constexpr int kShared = 16 << 20;         // bytes of keys and values from which on two tiles of rows share a workgroup
+
 // Grains of a range: a tile of 32 tokens (bf16) or 16 for every wave.
 inline int least_range(const qcf_layer_desc& L) { return L.dtype == QCF_DTYPE_BF16 ? 4 : 2; }
 
@@ -44,10 +46,11 @@ struct Division {
 // memory.  Heads of 128 in bf16, whole and divided, us: 8 workgroups (a request, 8 KV heads) of 512 tokens 9.9 and 10.8, 1024 14.8 and
 // 11.7; 64 of up to 1024 tokens 15.9 and 14.8; 128 of up to 1536 21.2 and 23.6, 2048 36.5 and 30.9; 512 of up to 1024 49 and 55, 4096
 // 159 and 161, 8192 313 and 302.  Heads of 64: 16 of 1536 tokens 12.4 and 13.4, 2048 15.7 and 11.8; 512 of up to 4096 97 and 103.
+// In float32, heads of 64: 2 of 512 tokens 10.4 and 10.8, 768 13.6 and 11.2; 16 of up to 512 10.9 and 10.8.
 inline bool takes_whole(const qcf_layer_desc& L, int64_t workgroups, int64_t longest) {
   const int64_t bytes = longest * 2 * L.head_dim * (L.dtype == QCF_DTYPE_BF16 ? 2 : 4);
   const int64_t alone = std::max<int64_t>(30, 200 - workgroups * 256 / compute_unit_count());      // of 200
-  return bytes * alone <= (int64_t)(272 << 10) * 200;
+  return bytes * alone <= (int64_t)((L.dtype == QCF_DTYPE_BF16 ? 272 : 240) << 10) * 200;
 }
 
 inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, int32_t n_keep) {
@@ -55,12 +58,17 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   const int G = L.n_q_heads / L.n_kv_heads;
   d.contexts = n_keep ? B * n_q : B;
   d.rows = n_keep ? G : n_q * G;
-  d.row_tiles = d.rows > 16 ? 2 : 1;
+  // More than 16 rows: two tiles of them share what a wave reads, unless there is little to read in all (by the width of the table):
+  // then a second workgroup finds it in the L2, and the first is done sooner.  64 / 2 heads of 128, us, two tiles and one: one request of
+  // 4096 tokens 14.6 and 12.5, of 16384 18.9 and 19.5; 8 of up to 1024 15.9 and 13.5, of up to 4096 18.9 and 23.5.  32 / 1 heads: one
+  // request of 16384 tokens 18.1 and 16.0, 8 of up to 4096 16.6 and 16.4, 64 of up to 1024 19.2 and 16.6, of up to 4096 32.6 and 43.7.
+  const int64_t longest = (int64_t)(n_keep && n_keep < c.max_pages ? n_keep : c.max_pages) * c.page_size;
+  const int64_t read = (int64_t)d.contexts * longest * L.n_kv_heads * 2 * L.head_dim * (L.dtype == QCF_DTYPE_BF16 ? 2 : 4);
+  d.row_tiles = d.rows > 16 && read > (int64_t)kShared ? 2 : 1;
   d.row_blocks = (d.rows + 16 * d.row_tiles - 1) / (16 * d.row_tiles);
   d.inner = L.n_kv_heads * d.row_blocks;
   d.slots = (d.row_tiles == 1 || L.head_dim == 64 ? 2 : 1) * compute_unit_count() / d.inner;       // (two waves to a SIMD, or one)
   if (d.slots < 1) d.slots = 1;
-  const int64_t longest = (int64_t)(n_keep && n_keep < c.max_pages ? n_keep : c.max_pages) * c.page_size;
   d.most = (int64_t)d.contexts * ((longest + kGrain - 1) / kGrain);
   d.least = least_range(L);
   // (four drafts of 8 requests of 2K to 6K tokens, 32 rows: 53.0 us without, 48.1 with 12, 47.1 with 18, 50.0 with 28; two workgroups on

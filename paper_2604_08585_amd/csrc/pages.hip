@@ -259,10 +259,11 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int head
 // and so are their sums where the terms are within 2^37 of each other: the order of the sum does not decide between pages.
 // Bound by memory (512 bytes to a page and KV head of 128) and, close behind, by its float64 work, a conversion and a product to
 // each value: 32 contexts of 1024 pages on average, 8 KV heads, 41.6 us with the queries in registers, two waves to a SIMD (30 of
-// it without the products, with more chains of sums no change), 38.9 with the queries in LDS, four waves (3.5 TB/s).  A lane has page
+// it without the products, with more chains of sums no change), 38.9 with the queries in LDS, four waves, 35.1 (3.8 TB/s) with a wave's
+// table entries asked for at once.  A lane has page
 // lane % 16 and every fourth 16-byte vector of its bounds; of the result, query lane % 4 and page 4 (lane / 4 % 4) + lane / 16.
-constexpr int kScorePages = 16;
-template <typename T, int D>
+constexpr int kScorePages = 16, kScoreTiles = 4;          // of a wave, and tiles of them that it has at most
+template <typename T, int D, int TILES>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_kernel(
     qcf_page_cache c, const T* __restrict__ q, const int32_t* __restrict__ seen, int n_q, int H, int Hkv, int log2_page, int chunks,
     int chunk, float* __restrict__ score) {
@@ -277,7 +278,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_k
   const int first = (int)(rest - row * chunks) * chunk, p0 = first + kScorePages * __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* table = c.table + b * c.max_pages;
   auto entry = [&](int p) { return p + col < c.max_pages ? table[p + col] : -1; };
-  const int phys0 = entry(p0);                          // (asked for with the count, not behind it)
+  // (all of them are asked for with the count: behind a tile's bounds, one would wait for those)
+  int phys[TILES];
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) phys[i] = entry(p0 + i * STEP);
   const int count = (int)min(((int64_t)max(seen[row], 0) + c.page_size - 1) >> log2_page, (int64_t)c.max_pages);
   const int end = min(count, first + chunk);
   if (first >= end) return;                             // (the workgroup)
@@ -292,9 +296,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_k
     }
   };
   for (int h0 = 0; h0 < G; h0 += 4) {                   // four queries at a time
-    int phys = phys0, next = entry(p0 + STEP);
-    u32x4 lo[LOADS], hi[LOADS], next_lo[LOADS], next_hi[LOADS];
-    if (p0 < end) load(phys, lo, hi);
+    u32x4 lo[2][LOADS], hi[2][LOADS];
+    if (p0 < end) load(phys[0], lo[0], hi[0]);
     if (h0 > 0) __syncthreads();
     for (int i = tid; i < 4 * D; i += kThreads) {
       const int h = i / D, e = i % D;                   // element e is in vector e / VEC: load vector / 4, quad vector % 4
@@ -304,17 +307,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_k
       s_q[1][at][lanes][e & 1] = v < 0.f ? 0.0 : (double)v;
     }
     __syncthreads();
-    for (int p = p0; p < end; p += STEP) {
-      const uint64_t mask = __ballot(phys >= 0 && phys < c.n_pages);
-      if (p + STEP < end) load(next, next_lo, next_hi);
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      const int p = p0 + i * STEP;
+      if (p >= end) break;
+      const uint64_t mask = __ballot(phys[i] >= 0 && phys[i] < c.n_pages);
+      if (i + 1 < TILES && p + STEP < end) load(phys[i + 1 < TILES ? i + 1 : i], lo[(i + 1) & 1], hi[(i + 1) & 1]);
       double a0 = 0.0, a1 = 0.0;
       int query = 4 * quad + j;
       asm volatile("" : "+v"(query));                   // (read from LDS for every tile: kept, they would be spilled)
 #pragma unroll
       for (int f = 0; f < LOADS; ++f) {
         float l[VEC], h[VEC];
-        Vec16<T>::unpack(lo[f], l);
-        Vec16<T>::unpack(hi[f], h);
+        Vec16<T>::unpack(lo[i & 1][f], l);
+        Vec16<T>::unpack(hi[i & 1][f], h);
 #pragma unroll
         for (int e = 0; e < VEC; e += 2) {
           const pair_t down = s_q[0][(f * VEC + e) / 2][query], up = s_q[1][(f * VEC + e) / 2][query];
@@ -334,10 +340,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_k
         s = mask >> mine & 1 ? s : -INFINITY;
         out[p + mine] = h0 > 0 ? fmaxf(out[p + mine], s) : s;           // (written by this lane)
       }
-      phys = next;
-      next = entry(p + 2 * STEP);
-#pragma unroll
-      for (int f = 0; f < LOADS; ++f) { lo[f] = next_lo[f]; hi[f] = next_hi[f]; }
     }
   }
 }
@@ -394,18 +396,20 @@ qcf_status launch_page_select(const qcf_layer_desc& L, const qcf_page_cache& c, 
   // out once for them).  32 contexts of 512 to 1536 pages, 8 KV heads: 39.0 us with up to four, 39.2 with up to eight; one context of
   // 8192 pages: 12.1, 12.9 with two workgroups to a compute unit.
   int64_t each = rows * L.n_kv_heads * tiles / (4 * compute_unit_count());
-  each = std::min<int64_t>(std::max<int64_t>(each, 1), 4);
+  each = std::min<int64_t>(std::max<int64_t>(each, 1), kScoreTiles);
   const int64_t chunks = (tiles + each - 1) / each, blocks = rows * L.n_kv_heads * chunks;
   if (blocks > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page select: too many rows");
   const int log2_page = __builtin_ctz((unsigned)c.page_size), chunk = (int)(each * 4 * kScorePages);
-#define QCF_LAUNCH(T, D)                                                                                              \
-  page_score_kernel<T, D><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(c, static_cast<const T*>(q), seen, n_q,  \
-                                                                             L.n_q_heads, L.n_kv_heads, log2_page, (int)chunks, chunk, score)
+#define QCF_TILES(T, D, TILES)                                                                                               \
+  page_score_kernel<T, D, TILES><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(c, static_cast<const T*>(q), seen, n_q,  \
+                                                                                    L.n_q_heads, L.n_kv_heads, log2_page, (int)chunks, chunk, score)
+#define QCF_LAUNCH(T, D) do { if (each == 1) QCF_TILES(T, D, 1); else QCF_TILES(T, D, kScoreTiles); } while (0)
   if (L.dtype == QCF_DTYPE_BF16) {
     if (L.head_dim == 128) QCF_LAUNCH(bf16_t, 128); else QCF_LAUNCH(bf16_t, 64);
   } else {
     if (L.head_dim == 128) QCF_LAUNCH(float, 128); else QCF_LAUNCH(float, 64);
   }
+#undef QCF_TILES
 #undef QCF_LAUNCH
   QCF_TRY_LAUNCH("page scores");
   return launch_page_top(score, seen, rows, L.n_kv_heads, c.page_size, c.max_pages, n_keep, n_first, n_last, pages, st);

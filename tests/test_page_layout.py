@@ -89,4 +89,4 @@ def test_short_contexts_are_taken_whole_by_the_rule():
     assert whole(64, 16) and not whole(128, 16)                       # of 16
     assert whole(128, 64) and not whole(512, 64)
     assert whole(8192, 32, keep=96) and not whole(8192, 1, keep=256)
-    assert not whole(32, 1, n_q=8)                                    # 32 rows: two tiles of rows to a workgroup
+    assert whole(32, 1, n_q=8) and not whole(32, 64, n_q=8)           # 32 rows: two tiles of rows to a workgroup where there is much to read
