@@ -20,7 +20,8 @@ extern "C" {
 /* A layer's cache in pages (host struct).  Token t of request b is in slot t % page_size of page table[b][t / page_size].
  * A table entry outside [0, n_pages) is a page that is not there: what would be written to it is dropped, its tokens are not
  * attended to.  Requests may share pages that none of them writes.
- * Slot s of page p, KV head g: d elements from p * page_stride + s * slot_stride + g * head_stride on, of k and of v.
+ * Slot s of page p, KV head g: d elements from p * page_stride + s * slot_stride + g * head_stride on, of k and of v.  Any order is
+ * taken; pages that keep a head's tokens together are read 4 to 5 % faster than pages that keep a token's heads together.
  * Strides are in elements, multiples of 8, at most 2^24 for slots and heads; rows of a page must not overlap, and page_stride
  * must be at least what a page spans. */
 typedef struct qcf_page_cache {
