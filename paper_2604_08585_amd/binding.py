@@ -486,13 +486,15 @@ def page_cache(k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor],
                                    table.shape[1], 0), (k, v, bounds, table))
 
 
-def _rows(t: Optional[torch.Tensor]):
-    """Pointer and row stride of [rows, heads, d], dense but for the distance of its rows."""
+def _rows(t: Optional[torch.Tensor], rows: int = 0):
+    """Pointer and row stride of [rows, heads, d] or more rows, dense but for the distance of its rows."""
     if t is None:
         return None, 0
     shape, stride = t.shape, t.stride()          # (each attribute once: they are most of what a call takes here)
     if len(stride) != 3 or not t.is_cuda or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2]):
         raise QcfError("rows handed to the library must be CUDA tensors [rows, heads, d] with dense rows")
+    if shape[0] < rows:
+        raise QcfError(f"{shape[0]} rows, {rows} wanted")
     return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1] * shape[2]
 
 
@@ -500,7 +502,7 @@ def qcf_page_append(desc: LayerDesc, cache: PageCache, B: int, q: Optional[torch
                     row_off: torch.Tensor, total_rows: int, lens: torch.Tensor, pos: Optional[torch.Tensor],
                     q_out: Optional[torch.Tensor]) -> None:
     """Rows of k and v behind what their requests hold (lens), keys and queries turned by pos on the way."""
-    (qp, qs), (kp, ks), (vp, vs) = _rows(q), _rows(k), _rows(v)
+    (qp, qs), (kp, ks), (vp, vs) = _rows(q, total_rows), _rows(k, total_rows), _rows(v, total_rows)
     _check(load_library().qcf_page_append(C.byref(desc), cache.of(B), B, qp, qs, kp, ks, vp, vs, _ptr(row_off), total_rows,
                                           _ptr(lens), _ptr(pos), _ptr(q_out), _stream()))
 
@@ -526,6 +528,8 @@ def qcf_page_attn(desc: LayerDesc, cache: PageCache, B: int, n_q: int, q: torch.
                   pages: Optional[torch.Tensor], n_keep: int, o_out: torch.Tensor, lse_out: Optional[torch.Tensor],
                   workspace: Optional[torch.Tensor] = None) -> None:
     """Attention of n_q new rows of each request over all its pages, or over those that `pages` lists for each row and KV head."""
+    if pages is not None and pages.shape[-1] != n_keep:
+        raise QcfError(f"pages lists {pages.shape[-1]} pages to a row, n_keep is {n_keep}")
     if workspace is None:
         workspace = _workspace(qcf_page_attn_workspace_bytes(desc, cache, B, n_q, n_keep), q.device)
     wp, wn = _ws_args(workspace)

@@ -252,8 +252,8 @@ struct Walk {
           const uint32_t x0 = __float_as_uint(p[r][2 * i]), x1 = __float_as_uint(p[r][2 * i + 1]);
           ph[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
           float r0 = p[r][2 * i] - __uint_as_float(x0 & 0xffff0000u), r1 = p[r][2 * i + 1] - __uint_as_float(x1 & 0xffff0000u);
-          r0 = p[r][2 * i] > 0.f ? fmaxf(r0, 1e-30f) : r0;
-          r1 = p[r][2 * i + 1] > 0.f ? fmaxf(r1, 1e-30f) : r1;
+          r0 = p[r][2 * i] > 0.f ? fmaxf(r0, 0x1p-126f) : r0;
+          r1 = p[r][2 * i + 1] > 0.f ? fmaxf(r1, 0x1p-126f) : r1;
           pl[i] = cvt_pk_bf16(r0, r1);
         }
         hi[r] = __builtin_bit_cast(bf16x8, ph);

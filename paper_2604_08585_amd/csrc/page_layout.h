@@ -63,8 +63,8 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   // 4096 tokens 14.6 and 12.5, of 16384 18.9 and 19.5; 8 of up to 1024 15.9 and 13.5, of up to 4096 18.9 and 23.5.  32 / 1 heads: one
   // request of 16384 tokens 18.1 and 16.0, 8 of up to 4096 16.6 and 16.4, 64 of up to 1024 19.2 and 16.6, of up to 4096 32.6 and 43.7.
   const int64_t longest = (int64_t)(n_keep && n_keep < c.max_pages ? n_keep : c.max_pages) * c.page_size;
-  const int64_t read = (int64_t)d.contexts * longest * L.n_kv_heads * 2 * L.head_dim * (L.dtype == QCF_DTYPE_BF16 ? 2 : 4);
-  d.row_tiles = d.rows > 16 && read > (int64_t)kShared ? 2 : 1;
+  const double read = (double)d.contexts * (double)longest * L.n_kv_heads * 2 * L.head_dim * (L.dtype == QCF_DTYPE_BF16 ? 2 : 4);
+  d.row_tiles = d.rows > 16 && read > kShared ? 2 : 1;
   d.row_blocks = (d.rows + 16 * d.row_tiles - 1) / (16 * d.row_tiles);
   d.inner = L.n_kv_heads * d.row_blocks;
   d.slots = (d.row_tiles == 1 || L.head_dim == 64 ? 2 : 1) * compute_unit_count() / d.inner;       // (two waves to a SIMD, or one)

@@ -27,8 +27,8 @@ template <typename T>
 __device__ __forceinline__ float2 turn_at(double positions, double turns) {
   const double t = positions * turns;
   const float f = (float)(t - __builtin_rint(t));
-  // bf16: the hardware's sine and cosine of a fraction of a turn, at most 1.3e-7 off (731
-  // rows with heads of 64, in pages of 64: 10.8 us with sincospif and rounding by integers, 8.1 with both in hardware)
+  // bf16: the hardware's sine and cosine of a fraction of a turn, at most 1.3e-7 off (731 rows with heads of 64, in pages of 64:
+  // 10.8 us with sincospif and rounding by integers, 8.1 with both in hardware)
   if constexpr (sizeof(T) == 2) return make_float2(__builtin_amdgcn_cosf(f), __builtin_amdgcn_sinf(f));
   float sn, cn;
   sincospif(2.f * f, &sn, &cn);
@@ -90,10 +90,10 @@ __device__ __forceinline__ Request request_of(const AppendArgs& a, int64_t unit,
 }
 
 // One workgroup per (page that gets rows, `heads` KV heads of it): their keys, turned and rounded, the bounds, the values, and the
-// queries of the heads' groups.  A thread takes VEC rotary pairs of a row, two 16-byte vectors.  The (cos, sin) of kRows rows are
+// queries of the heads' groups.  A thread takes VEC rotary pairs of a row, two 16-byte vectors.  The (cos, sin) of ROWS rows are
 // kept in LDS for all heads: formed for every vector anew they took the vector unit longer than the rows took memory (32K rows, 8
-// KV heads of 128: 238 us, 190 with them).  Bound by memory there, and by the chain offsets -> rows, page and positions -> factors
-// -> stores where few rows come: what needs no factors is asked for in front of them.
+// KV heads of 128: 238 us, 190 with them, 181 or 4.95 TB/s now).  Bound by memory there, and by the chain offsets -> rows, page and
+// positions -> factors -> stores where few rows come (8 rows 5.2 us): what needs no factors is asked for in front of them.
 template <typename T, int D, int STYLE>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int heads, int log2_lanes) {
   constexpr int VEC = Elem<T>::kVec, TPR = D / 2 / VEC, WAVES = kThreads / 64, PAIRS = D / 2, ROWS = 4096 / D, AHEAD = 2;
@@ -256,12 +256,12 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int head
 
 // Scores of pages (the definition is in qcf_pages.h), 16 pages to a wave, in float64 products of 4 pages x 4 queries x 4 elements,
 // four of them side by side: score = sum of min(q, 0) lo + max(q, 0) hi.  Products of two stored bf16 values are exact in float64,
-// and so are their sums where the terms are within 2^37 of each other: the order of the sum does not decide between pages.
+// and so are their sums where the terms are within 2^29 of each other: the order of the sum does not decide between pages.
 // Bound by memory (512 bytes to a page and KV head of 128) and, close behind, by its float64 work, a conversion and a product to
 // each value: 32 contexts of 1024 pages on average, 8 KV heads, 41.6 us with the queries in registers, two waves to a SIMD (30 of
-// it without the products, with more chains of sums no change), 38.9 with the queries in LDS, four waves, 35.1 (3.8 TB/s) with a wave's
-// table entries asked for at once.  A lane has page
-// lane % 16 and every fourth 16-byte vector of its bounds; of the result, query lane % 4 and page 4 (lane / 4 % 4) + lane / 16.
+// it without the products, with more chains of sums no change), 38.9 with the queries in LDS, four waves, 35.1 (3.8 TB/s) with a
+// wave's table entries asked for at once.  A lane has page lane % 16 and every fourth 16-byte vector of its bounds; of the result,
+// query lane % 4 and page 4 (lane / 4 % 4) + lane / 16.
 constexpr int kScorePages = 16, kScoreTiles = 4;          // of a wave, and tiles of them that it has at most
 template <typename T, int D, int TILES>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_kernel(

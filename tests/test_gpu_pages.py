@@ -609,6 +609,34 @@ def test_two_graphs_that_share_a_workspace_take_turns():
             assert torch.equal(calls[1 - i][1], want[1 - i][0]), (turn, i)
 
 
+def test_calls_on_two_streams_at_once():
+    """Divided attention over two caches, each with a workspace of its own, on two streams: the bits of the calls alone."""
+    rng = np.random.default_rng(22)
+    sh = shape(32, 8, 128, "bf16")
+    jobs = []
+    for lens in ([9000, 4000, 77], [15000]):
+        p = Paged(rng, sh, 16, lens, width=2048)
+        q = torch.from_numpy(normal(rng, (len(lens), 1, 32, 128), "bf16")).to(device=DEV, dtype=p.dt)
+        ws = torch.empty(qb.qcf_page_attn_workspace_bytes(p.desc, p.cache, len(lens), 1, 0), dtype=torch.uint8, device=DEV)
+        o, lse = torch.empty_like(q), torch.empty(len(lens), 1, 32, device=DEV)
+        jobs.append((p, q, i32(lens), o, lse, ws, torch.cuda.Stream()))
+    run = lambda j: qb.qcf_page_attn(j[0].desc, j[0].cache, len(j[1]), 1, j[1], j[2], None, 0, j[3], j[4], j[5])
+    alone = []
+    for j in jobs:
+        run(j)
+        torch.cuda.synchronize()
+        alone.append((j[3].clone(), j[4].clone()))
+        j[3].fill_(0.0)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for j in jobs:
+            with torch.cuda.stream(j[6]):
+                run(j)
+    torch.cuda.synchronize()
+    for j, (o, lse) in zip(jobs, alone):
+        assert torch.equal(j[3], o) and torch.equal(j[4], lse)
+
+
 def test_append_of_many_requests():
     """More requests than a wave has lanes, some without rows, lengths all over a page."""
     for dtype, B in [("bf16", 300), ("f32", 65), ("bf16", 64), ("f32", 4097), ("bf16", 4500)]:

@@ -113,3 +113,8 @@ def test_binding_refuses_what_it_cannot_describe():
         qb.page_cache(pool.transpose(2, 3), pool.transpose(2, 3), None, table)
     with pytest.raises(qb.QcfError):
         qb._rows(torch.zeros(4, 2, 64).transpose(0, 1))
+    cache = qb.PageCache(_cache(), (pool, pool, None, table))
+    with pytest.raises(qb.QcfError, match="2 requests, 1 rows"):
+        cache.of(2)
+    with pytest.raises(qb.QcfError, match="n_keep"):
+        qb.qcf_page_attn(_desc(), cache, 1, 1, pool, table, torch.zeros(1, 1, 2, 3, dtype=torch.int32), 4, pool, None)
