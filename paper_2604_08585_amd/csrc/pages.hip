@@ -257,34 +257,31 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int head
 // Scores of pages (the definition is in qcf_pages.h), 16 pages to a wave, in float64 products of 4 pages x 4 queries x 4 elements,
 // four of them side by side: score = sum of min(q, 0) lo + max(q, 0) hi.  Products of two stored bf16 values are exact in float64,
 // and so are their sums where the terms are within 2^29 of each other: the order of the sum does not decide between pages.
-// Bound by memory (512 bytes to a page and KV head of 128) and, close behind, by its float64 work, a conversion and a product to
-// each value: 32 contexts of 1024 pages on average, 8 KV heads, 41.6 us with the queries in registers, two waves to a SIMD (30 of
-// it without the products, with more chains of sums no change), 38.9 with the queries in LDS, four waves, 35.1 (3.8 TB/s) with a
-// wave's table entries asked for at once.  A lane has page lane % 16 and every fourth 16-byte vector of its bounds; of the result,
-// query lane % 4 and page 4 (lane / 4 % 4) + lane / 16.
-constexpr int kScorePages = 16, kScoreTiles = 4;          // of a wave, and tiles of them that it has at most
-template <typename T, int D, int TILES>
+// Bound by memory (512 bytes to a page and KV head of 128) and by its float64 work, a conversion and a product to each value: 32
+// contexts of 1024 pages on average, 8 KV heads, 41.6 us with the queries in registers, two waves to a SIMD (30 of it without the
+// products, with more chains of sums no change), 38.9 with the queries in LDS, four waves of up to four tiles, the next on its way,
+// 35.7 with their table entries asked for at once, 31.4 (4.3 TB/s) with one tile at a time, six waves.  A lane has page lane % 16 and
+// every fourth 16-byte vector of its bounds; of the result, query lane % 4 and page 4 (lane / 4 % 4) + lane / 16.
+constexpr int kScorePages = 16, kScoreStep = kScorePages * kThreads / 64;           // pages of a wave, of a workgroup
+template <typename T, int D>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_kernel(
-    qcf_page_cache c, const T* __restrict__ q, const int32_t* __restrict__ seen, int n_q, int H, int Hkv, int log2_page, int chunks,
-    int chunk, float* __restrict__ score) {
-  constexpr int VEC = Elem<T>::kVec, LOADS = D / (4 * VEC), STEP = kScorePages * kThreads / 64;
+    qcf_page_cache c, const T* __restrict__ q, const int32_t* __restrict__ seen, int n_q, int H, int Hkv, int log2_page, int parts,
+    float* __restrict__ score) {
+  constexpr int VEC = Elem<T>::kVec, LOADS = D / (4 * VEC);
   typedef double pair_t __attribute__((ext_vector_type(2)));
   // min(q, 0) and max(q, 0) of two elements of four queries, in the order in which the lanes read them
   __shared__ pair_t s_q[2][D / 8][16];
   const int tid = threadIdx.x, lane = tid & 63, quad = lane >> 4, col = lane & 15, j = lane & 3;
   const int g = (int)(blockIdx.x % Hkv), G = H / Hkv;
-  const int64_t rest = blockIdx.x / Hkv, row = rest / chunks;           // (request, new row)
+  const int64_t rest = blockIdx.x / Hkv, row = rest / parts;            // (request, new row)
   const int64_t b = row / n_q;
-  const int first = (int)(rest - row * chunks) * chunk, p0 = first + kScorePages * __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int first = (int)(rest - row * parts) * kScoreStep, p0 = first + kScorePages * __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int step = parts * kScoreStep;                  // (at most max_pages and 64 more)
   const int32_t* table = c.table + b * c.max_pages;
   auto entry = [&](int p) { return p + col < c.max_pages ? table[p + col] : -1; };
-  // (all of them are asked for with the count: behind a tile's bounds, one would wait for those)
-  int phys[TILES];
-#pragma unroll
-  for (int i = 0; i < TILES; ++i) phys[i] = entry(p0 + i * STEP);
+  const int phys0 = entry(p0);                          // (asked for with the count)
   const int count = (int)min(((int64_t)max(seen[row], 0) + c.page_size - 1) >> log2_page, (int64_t)c.max_pages);
-  const int end = min(count, first + chunk);
-  if (first >= end) return;                             // (the workgroup)
+  if (first >= count) return;                           // (the workgroup)
   float* out = score + (row * Hkv + g) * c.max_pages;
   const T* bounds = static_cast<const T*>(c.bounds);
   auto load = [&](int phys, u32x4 (&l)[LOADS], u32x4 (&h)[LOADS]) {
@@ -296,8 +293,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_k
     }
   };
   for (int h0 = 0; h0 < G; h0 += 4) {                   // four queries at a time
-    u32x4 lo[2][LOADS], hi[2][LOADS];
-    if (p0 < end) load(phys[0], lo[0], hi[0]);
+    u32x4 lo[LOADS], hi[LOADS];
+    int phys = phys0;
+    if (p0 < count) load(phys, lo, hi);
     if (h0 > 0) __syncthreads();
     for (int i = tid; i < 4 * D; i += kThreads) {
       const int h = i / D, e = i % D;                   // element e is in vector e / VEC: load vector / 4, quad vector % 4
@@ -307,20 +305,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_k
       s_q[1][at][lanes][e & 1] = v < 0.f ? 0.0 : (double)v;
     }
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < TILES; ++i) {
-      const int p = p0 + i * STEP;
-      if (p >= end) break;
-      const uint64_t mask = __ballot(phys[i] >= 0 && phys[i] < c.n_pages);
-      if (i + 1 < TILES && p + STEP < end) load(phys[i + 1 < TILES ? i + 1 : i], lo[(i + 1) & 1], hi[(i + 1) & 1]);
+    for (int p = p0; p < count;) {
+      const uint64_t mask = __ballot(phys >= 0 && phys < c.n_pages);
+      const int next = p + step;
+      if (next < count) phys = entry(next);
       double a0 = 0.0, a1 = 0.0;
       int query = 4 * quad + j;
       asm volatile("" : "+v"(query));                   // (read from LDS for every tile: kept, they would be spilled)
 #pragma unroll
       for (int f = 0; f < LOADS; ++f) {
         float l[VEC], h[VEC];
-        Vec16<T>::unpack(lo[i & 1][f], l);
-        Vec16<T>::unpack(hi[i & 1][f], h);
+        Vec16<T>::unpack(lo[f], l);
+        Vec16<T>::unpack(hi[f], h);
 #pragma unroll
         for (int e = 0; e < VEC; e += 2) {
           const pair_t down = s_q[0][(f * VEC + e) / 2][query], up = s_q[1][(f * VEC + e) / 2][query];
@@ -330,16 +326,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_k
           a1 = __builtin_amdgcn_mfma_f64_4x4x4f64((double)h[e + 1], up[1], a1, 0, 0, 0);
         }
       }
+      if (next < count) load(phys, lo, hi);
       const float sum = (float)(a0 + a1);
       float s = sum == sum ? fmaxf(sum, -3.402823466e38f) : INFINITY;   // (the least float: above pages that are not there)
       if (h0 + j >= G) s = -INFINITY;
       s = fmaxf(s, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(s), 0xb1, 0xf, 0xf, false)));    // the four queries
       s = fmaxf(s, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(s), 0x4e, 0xf, 0xf, false)));
       const int mine = 4 * (lane >> 2 & 3) + quad;
-      if (j == 0 && p + mine < end) {
+      if (j == 0 && p + mine < count) {
         s = mask >> mine & 1 ? s : -INFINITY;
         out[p + mine] = h0 > 0 ? fmaxf(out[p + mine], s) : s;           // (written by this lane)
       }
+      p = next;
     }
   }
 }
@@ -394,25 +392,23 @@ qcf_status launch_page_select(const qcf_layer_desc& L, const qcf_page_cache& c, 
                               const int32_t* seen, int32_t n_keep, int32_t n_first, int32_t n_last, int32_t* pages, void* ws,
                               hipStream_t st) {
   float* score = static_cast<float*>(ws);
-  const int64_t rows = (int64_t)B * n_q, tiles = ((int64_t)c.max_pages + 4 * kScorePages - 1) / (4 * kScorePages);
-  // Tiles of 4 waves x 16 pages of a workgroup: up to four, as long as every compute unit has four workgroups (the queries are laid
-  // out once for them).  32 contexts of 512 to 1536 pages, 8 KV heads: 39.0 us with up to four, 39.2 with up to eight; one context of
-  // 8192 pages: 12.1, 12.9 with two workgroups to a compute unit.
-  int64_t each = rows * L.n_kv_heads * tiles / (4 * compute_unit_count());
-  each = std::min<int64_t>(std::max<int64_t>(each, 1), kScoreTiles);
-  const int64_t chunks = (tiles + each - 1) / each, blocks = rows * L.n_kv_heads * chunks;
+  // A workgroup to every 64 pages of a table's row, but not more than the GPU holds at a time (six to a compute unit, bf16, heads of 128): these take
+  // turns.  Scores and choice, us, with four / six / eight / sixteen / any number to a compute unit: 32 contexts of 512 to 1536
+  // pages 39.3, 38.7, 38.9, 39.8, 42.0; 64 of 1024 to 2048 pages 43.5, 42.5, 42.7, 43.1, 44.8; 32 of 94 to 188 pages in a table of
+  // 8192 15.1, 13.9, 17.4, 17.9, 24.8 (64).
+  const int64_t rows = (int64_t)B * n_q, steps = ((int64_t)c.max_pages + kScoreStep - 1) / kScoreStep;
+  const int64_t most = 6 * (int64_t)compute_unit_count() / (rows * L.n_kv_heads);
+  const int64_t parts = std::min(steps, std::max<int64_t>(most, 1)), blocks = rows * L.n_kv_heads * parts;
   if (blocks > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page select: too many rows");
-  const int log2_page = __builtin_ctz((unsigned)c.page_size), chunk = (int)(each * 4 * kScorePages);
-#define QCF_TILES(T, D, TILES)                                                                                               \
-  page_score_kernel<T, D, TILES><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(c, static_cast<const T*>(q), seen, n_q,  \
-                                                                                    L.n_q_heads, L.n_kv_heads, log2_page, (int)chunks, chunk, score)
-#define QCF_LAUNCH(T, D) do { if (each == 1) QCF_TILES(T, D, 1); else QCF_TILES(T, D, kScoreTiles); } while (0)
+  const int log2_page = __builtin_ctz((unsigned)c.page_size);
+#define QCF_LAUNCH(T, D)                                                                                              \
+  page_score_kernel<T, D><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(c, static_cast<const T*>(q), seen, n_q,  \
+                                                                             L.n_q_heads, L.n_kv_heads, log2_page, (int)parts, score)
   if (L.dtype == QCF_DTYPE_BF16) {
     if (L.head_dim == 128) QCF_LAUNCH(bf16_t, 128); else QCF_LAUNCH(bf16_t, 64);
   } else {
     if (L.head_dim == 128) QCF_LAUNCH(float, 128); else QCF_LAUNCH(float, 64);
   }
-#undef QCF_TILES
 #undef QCF_LAUNCH
   QCF_TRY_LAUNCH("page scores");
   return launch_page_top(score, seen, rows, L.n_kv_heads, c.page_size, c.max_pages, n_keep, n_first, n_last, pages, st);

@@ -494,6 +494,28 @@ def test_selection(dtype, H, Hkv, D, page, lens, n_q, keep, first, last):
             assert np.array_equal(got[b, i], orc.page_select(s, keep, first, last)), (b, i)
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,D,B,n_q", [
+    ("bf16", 64, 8, 128, 20, 16),                                            # a workgroup takes all pages of its row
+    ("bf16", 12, 2, 64, 25, 12), ("f32", 6, 3, 64, 40, 6), ("f32", 10, 2, 128, 21, 9)])     # two or four share them
+def test_selection_where_workgroups_take_turns(dtype, H, Hkv, D, B, n_q):
+    rng = np.random.default_rng(21)
+    p = Paged(rng, shape(H, Hkv, D, dtype), 16, [16 * 350])
+    p.table = np.stack([rng.permutation(350) for _ in range(B)]).astype(np.int32)        # (pages may be shared by requests)
+    p.upload()
+    counts = np.array([0, 1, 63, 64, 65, 127, 128, 129, 200, 256, 257, 320, 321, 349, 350])[rng.integers(0, 15, (B, n_q))]
+    seen = np.maximum(16 * counts - rng.integers(0, 16, (B, n_q)), 0).astype(np.int32)
+    q = normal(rng, (B, n_q, H, D), dtype)
+    pages = torch.full((B, n_q, Hkv, 9), 99, dtype=torch.int32, device=DEV)
+    say("selection in turns", dtype, H, Hkv, D, B, n_q)
+    qb.qcf_page_select(p.desc, p.cache, B, n_q, torch.from_numpy(q).to(device=DEV, dtype=p.dt), i32(seen), 9, 1, 2, pages)
+    torch.cuda.synchronize()
+    got = pages.cpu().numpy()
+    for b in range(B):
+        for i in range(n_q):
+            s = orc.page_scores(q[b, i], p.bounds.astype(np.float64), p.table[b, :counts[b, i]])
+            assert np.array_equal(got[b, i], orc.page_select(s, 9, 1, 2)), (b, i, counts[b, i])
+
+
 def test_selection_of_ties_absent_pages_and_values_that_are_not_finite():
     rng = np.random.default_rng(13)
     for dtype in ("bf16", "f32"):
