@@ -392,10 +392,10 @@ qcf_status launch_page_select(const qcf_layer_desc& L, const qcf_page_cache& c, 
                               const int32_t* seen, int32_t n_keep, int32_t n_first, int32_t n_last, int32_t* pages, void* ws,
                               hipStream_t st) {
   float* score = static_cast<float*>(ws);
-  // A workgroup to every 64 pages of a table's row, but not more than the GPU holds at a time (six to a compute unit, bf16, heads of 128): these take
-  // turns.  Scores and choice, us, with four / six / eight / sixteen / any number to a compute unit: 32 contexts of 512 to 1536
-  // pages 39.3, 38.7, 38.9, 39.8, 42.0; 64 of 1024 to 2048 pages 43.5, 42.5, 42.7, 43.1, 44.8; 32 of 94 to 188 pages in a table of
-  // 8192 15.1, 13.9, 17.4, 17.9, 24.8 (64).
+  // A workgroup to every 64 pages of a table's row, but not more than the GPU holds at a time (six to a compute unit with bf16 heads
+  // of 128): these take turns.  Scores and choice, us, with four / six / eight / sixteen / any number to a compute unit: 32 contexts
+  // of 512 to 1536 pages 39.3, 38.7, 38.9, 39.8, 42.0; 64 of 1024 to 2048 pages 43.5, 42.5, 42.7, 43.1, 44.8; 32 of 94 to 188 pages
+  // in a table of 8192 15.1, 13.9, 17.4, 17.9, 24.8 (64 to a compute unit).
   const int64_t rows = (int64_t)B * n_q, steps = ((int64_t)c.max_pages + kScoreStep - 1) / kScoreStep;
   const int64_t most = 6 * (int64_t)compute_unit_count() / (rows * L.n_kv_heads);
   const int64_t parts = std::min(steps, std::max<int64_t>(most, 1)), blocks = rows * L.n_kv_heads * parts;
