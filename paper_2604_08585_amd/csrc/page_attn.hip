@@ -41,7 +41,9 @@ struct PageAttnArgs {
   float2* part_ml;
 };
 
-// Tokens that context x covers: what its rows see, or its listed pages.
+// Tokens that context x covers: what its rows see, or as many entries of its list as the row sees pages.  What a list has behind
+// these is mostly empty; the last part of a context looks through it (list_end).  16 rows of 32 to 3000 tokens with lists of 256
+// pages of 16: selection and attention 37.4 us without that, 39.6 with it, 47.5 with the lists divided as a whole.
 __device__ __forceinline__ int64_t context_tokens(const PageAttnArgs& a, int x) {
   const int64_t most = (int64_t)a.c.max_pages << a.log2_page;
   if (a.list) {
@@ -53,6 +55,12 @@ __device__ __forceinline__ int64_t context_tokens(const PageAttnArgs& a, int x) 
 #pragma unroll
     for (int i = 0; i < 4; ++i) seen = max(seen, a.seen[(int64_t)x * a.n_q + min(i0 + i, a.n_q - 1)]);
   return min((int64_t)seen, most);
+}
+
+// The end of the last part of a context of `tokens`.
+template <int MODE>
+__device__ __forceinline__ int64_t list_end(const PageAttnArgs& a, int64_t tokens) {
+  return MODE == kList && tokens > 0 ? (int64_t)a.n_keep << a.log2_page : tokens;
 }
 
 template <int CTRL, int ROWS = 0xf>
@@ -164,7 +172,7 @@ struct Walk {
   const int lane, quad, col, g;
   int x, b;                                              // context, request
   int64_t end;                                           // of the workgroup's part, in the context's order
-  int count;                                             // pages that a row sees (listed pages from there on are none)
+  int count;                                             // pages that a row sees (listed pages of higher numbers are none)
   Window w;
   u32x4 q[RT][kLoads];
   int lim[RT];                                           // tokens that the lane's row sees
@@ -235,6 +243,16 @@ struct Walk {
     const Where r = find(at);
     load_keys(t, r);
     load_values(t, r);
+  }
+
+  // The wave's tile at `at`; of a list, the next one before `stop` that has a page.
+  __device__ __forceinline__ int64_t tile_at(int64_t at, int64_t stop) {
+    if constexpr (MODE == kList)
+      for (; at < stop; at += kStep) {
+        const Where r = find(at);
+        if (r.base[0] >= 0 || r.base[kSub - 1] >= 0) break;
+      }
+    return at;
   }
 
   // products of the tile's values with the weights, added to c
@@ -405,17 +423,19 @@ struct Walk {
   __device__ __forceinline__ void run(int64_t at) {
     const int64_t shared = MODE == kSeveral && lim_lo < lim_hi ? min(end, (int64_t)(lim_lo & -kTokens)) : end;
     auto nothing = [] {};
+    at = tile_at(at, shared);
     if constexpr (RT == 2 && D == 128) {
       // (no registers for a second tile: the next keys are asked for once the logits are there, the next values after the products)
       if (at < shared) {
         Tile t;
         load(t, at);
-        for (; at < shared; at += kStep) {
+        while (at < shared) {
           Where next;
-          const bool more = at + kStep < shared;
+          at = tile_at(at + kStep, shared);
+          const bool more = at < shared;
           step<false>(t, [&] {
             if (more) {
-              next = find(at + kStep);
+              next = find(at);
               load_keys(t, next);
             }
           });
@@ -426,11 +446,11 @@ struct Walk {
       Tile t0, t1;
       load(t0, at);
       while (true) {
-        at += kStep;
+        at = tile_at(at + kStep, shared);
         if (at < shared) load(t1, at);
         step<false>(t0, nothing);
         if (at >= shared) break;
-        at += kStep;
+        at = tile_at(at + kStep, shared);
         if (at < shared) load(t0, at);
         step<false>(t1, nothing);
         if (at >= shared) break;
@@ -571,7 +591,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 || D == 64 ? 2 : 1) void page_a
   const int in = (int)(blockIdx.x - r * a.inner), g = in % a.Hkv, row0 = in / a.Hkv * kRows;
   W w(a, lane, g);
   if constexpr (WHOLE) {
-    w.start((int)r, row0, 0, context_tokens(a, (int)r));
+    w.start((int)r, row0, 0, list_end<MODE>(a, context_tokens(a, (int)r)));
     w.run(wave * W::kTokens);
     finish(a, w, s_o, s_m, s_l, in, row0, -1);
     return;
@@ -585,7 +605,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 || D == 64 ? 2 : 1) void page_a
     const int64_t g0 = max(from - here.start, (int64_t)0), g1 = min(to - here.start, here.grains);
     if (g1 > g0) {
       const int64_t tokens = here.x < 64 ? from_lane(all.tokens, here.x) : context_tokens(a, here.x);
-      w.start(here.x, row0, g0 * pages::kGrain, min(g1 * pages::kGrain, tokens));
+      w.start(here.x, row0, g0 * pages::kGrain, g1 == here.grains ? list_end<MODE>(a, tokens) : g1 * pages::kGrain);
       w.run(g0 * pages::kGrain + wave * W::kTokens);
       finish(a, w, s_o, s_m, s_l, in, row0, g1 - g0 == here.grains ? -1 : 2 * r + (g0 == 0));
     }

@@ -386,6 +386,29 @@ def test_attention_over_listed_pages(dtype, H, Hkv, D, page, keep):
     _attend_and_check(p, rng, seen, pages)
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,D,page,keep,width", [
+    ("bf16", 32, 8, 128, 16, 30, None), ("f32", 4, 2, 64, 32, 12, None), ("bf16", 8, 2, 64, 64, 700, 1024),
+    ("bf16", 32, 8, 128, 16, 1500, 2048), ("f32", 4, 2, 64, 16, 1100, 2048), ("bf16", 24, 1, 128, 32, 2000, 2048)])
+def test_listed_pages_behind_more_entries_than_the_row_has_pages(dtype, H, Hkv, D, page, keep, width):
+    """Entries that are no page of the row, before and between those that are, and pages listed again, in lists wider than the row."""
+    rng = np.random.default_rng(22)
+    lens = [page * 2 - 3, 5, page * 4, page * 7 + 1]
+    p = Paged(rng, shape(H, Hkv, D, dtype), page, lens, width=width)
+    pages = np.full((4, 2, Hkv, keep), -1, dtype=np.int32)
+    for b, n in enumerate(lens):
+        count = -(-n // page)
+        for i in range(2):
+            for g in range(Hkv):
+                at = rng.permutation(keep)[:min(10, keep // 2)]
+                pages[b, i, g, at] = rng.integers(0, count + 2, len(at))        # (pages of the row, some again, and pages behind it)
+                pages[b, i, g, -1] = count - 1
+    pages[1, 1, :, :-1], pages[1, 1, :, -1] = 9, 0                      # the last entry alone
+    pages[2, 0] = -1                                                    # none
+    pages[3, 1, 0, -1] = -1
+    _attend_and_check(p, rng, np.array([[n - 1, n] for n in lens], dtype=np.int32), pages)
+    _attend_and_check(p, rng, np.array([[0, n] for n in lens], dtype=np.int32), pages)
+
+
 def test_a_list_of_all_pages_is_no_list():
     rng = np.random.default_rng(11)
     p = Paged(rng, shape(8, 2, 128, "bf16"), 16, [16 * 40 - 5])
