@@ -447,7 +447,10 @@ def decode_step(P: PagedLayer, x: torch.Tensor, w_qkv: torch.Tensor) -> torch.Te
     """One layer's attention for `new` tokens behind each request: x [B * new, d_model] (normed hidden states) is projected, keys and
     values go into the cache, rotated on the way, and the queries attend.  Returns o [B, new, H, d].  Lengths and positions live
     on the device and are not moved: call `advance` after a step's last layer, or to accept fewer tokens than were drafted."""
-    rows, dm = x.shape
+    rows, dm = P.B * P.new, P.desc.d_model
+    if x.shape != (rows, dm) or w_qkv.shape != (P.qkv.shape[1], dm) or x.dtype != P.qkv.dtype or w_qkv.dtype != P.qkv.dtype:
+        raise ValueError(f"x {tuple(x.shape)} and w_qkv {tuple(w_qkv.shape)} for {P.B} requests of {P.new} rows of {dm}, "
+                         f"{P.qkv.shape[1]} columns, {P.qkv.dtype}")
     qb.qcf_linear(P.desc, x, rows, dm, w_qkv, P.qkv.shape[1], None, P.qkv, P.ws_linear)
     q, k, v = P.parts
     qb.qcf_page_append(P.desc, P.cache, P.B, q, k, v, P.row_off, rows, P.held, P.pos, P.q.flatten(0, 1))

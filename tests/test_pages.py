@@ -3,11 +3,13 @@ import ctypes as C
 import os
 import re
 import subprocess
+import types
 
 import pytest
 import torch
 
 from paper_2604_08585_amd import binding as qb
+from paper_2604_08585_amd import pipeline
 from paper_2604_08585_amd.inputs import LayerShape
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -118,3 +120,11 @@ def test_binding_refuses_what_it_cannot_describe():
         cache.of(2)
     with pytest.raises(qb.QcfError, match="n_keep"):
         qb.qcf_page_attn(_desc(), cache, 1, 1, pool, table, torch.zeros(1, 1, 2, 3, dtype=torch.int32), 4, pool, None)
+
+
+@pytest.mark.parametrize("x,w,dtype", [((7, 256), (512, 256), torch.float32), ((6, 255), (512, 255), torch.float32),
+                                       ((6, 256), (256, 512), torch.float32), ((6, 256), (512, 256), torch.bfloat16)])
+def test_a_step_refuses_rows_weights_and_types_that_do_not_fit(x, w, dtype):
+    P = types.SimpleNamespace(desc=_desc(), B=2, new=3, qkv=torch.zeros(6, 512))
+    with pytest.raises(ValueError, match="2 requests of 3 rows of 256"):
+        pipeline.decode_step(P, torch.zeros(x, dtype=dtype), torch.zeros(w))
