@@ -387,7 +387,7 @@ def test_attention_over_listed_pages(dtype, H, Hkv, D, page, keep):
 
 
 @pytest.mark.parametrize("dtype,H,Hkv,D,page,keep,width", [
-    ("bf16", 32, 8, 128, 16, 30, None), ("f32", 4, 2, 64, 32, 12, None), ("bf16", 8, 2, 64, 64, 700, 1024),
+    ("bf16", 32, 8, 128, 16, 30, None), ("f32", 4, 2, 64, 32, 12, None), ("bf16", 8, 2, 64, 64, 700, 1024), ("bf16", 8, 2, 64, 64, 700, 600),
     ("bf16", 32, 8, 128, 16, 1500, 2048), ("f32", 4, 2, 64, 16, 1100, 2048), ("bf16", 24, 1, 128, 32, 2000, 2048)])
 def test_listed_pages_behind_more_entries_than_the_row_has_pages(dtype, H, Hkv, D, page, keep, width):
     """Entries that are no page of the row, before and between those that are, and pages listed again, in lists wider than the row."""
