@@ -68,7 +68,8 @@ qcf_status qcf_page_select(const qcf_layer_desc* desc, const qcf_page_cache* cac
 /* o[b, i, h] = sum_t softmax_t( q[b, i, h] . k_t / sqrt(d) ) v_t over the tokens t < seen[b, i] of request b whose page is there,
  * k_t and v_t of KV head h / (H / H_kv).  q and o [B, n_q, H, d], seen [B, n_q], 1 <= n_q <= 16, as above; lse (may be NULL)
  * [B, n_q, H] float32, natural-log sum-exp of the scaled logits.  A row that sees nothing gets a zero output row and lse = -inf;
- * what is stored in slots that a row does not see, whatever it is, does not reach it.
+ * what is stored in slots that a row does not see, whatever it is, does not reach it.  A logit of -inf weighs nothing beside others,
+and makes a row that has only such NaN; a logit that is NaN or +inf makes its row NaN.
  * pages (NULL: all pages; n_keep is then 0) [B, n_q, H_kv, n_keep]: only tokens of these pages, in any order; entries that are no
  * page of the row are passed over, a page that is listed twice counts twice.
  * The contexts are divided over the GPU by their lengths; the same call gives the same bits, and the last bits of a row depend on

@@ -543,7 +543,10 @@ __device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MOD
     bool any = w.any[r];
     any = __shfl_xor((int)any, 16, 64) || any;
     any = __shfl_xor((int)any, 32, 64) || any;
-    if (any && w.m[r] == -INFINITY) l = NAN;             // only logits of -inf
+    // without a reference point: only logits of -inf (l is 0), which make the row NaN where no other part has more, or some that are
+    // NaN (l is NaN), which make it NaN whatever the others have: with a finite point the joins take that l with them
+    if (l != l) w.m[r] = w.m[r] == -INFINITY ? 0.f : w.m[r];
+    else if (any && w.m[r] == -INFINITY) l = NAN;
     if (lane < 16) { s_m[wave][16 * r + lane] = w.m[r]; s_l[wave][16 * r + lane] = l; }
     if (row0 + 16 * r + w.col >= a.rows) continue;
 #pragma unroll
