@@ -555,7 +555,7 @@ __device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MOD
       for (int e = 0; e < W::kE; e += 4) {
         const int dim = W::kHalf ? D / 16 * (4 * w.quad + i) + e : 16 * e + 4 * (4 * w.quad + i);
         *reinterpret_cast<floatx4*>(&s_o[wave][16 * r + w.col][dim]) =
-            floatx4{w.acc[r][e][i], w.acc[r][e + 1][i], w.acc[r][e + 2][i], w.acc[r][e + 3][i]};
+            any ? floatx4{w.acc[r][e][i], w.acc[r][e + 1][i], w.acc[r][e + 2][i], w.acc[r][e + 3][i]} : floatx4{0.f, 0.f, 0.f, 0.f};
       }
   }
   __syncthreads();
@@ -570,11 +570,13 @@ __device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MOD
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
       const float mi = s_m[i][r], li = s_l[i][r];
-      // (what saw nothing or only logits of -inf weighs nothing beside others; the latter make a row NaN that has nothing else)
-      if (mi == -INFINITY) { l = top == -INFINITY ? l + li : l; continue; }
+      const floatx4 oi = *reinterpret_cast<const floatx4*>(&s_o[i][r][e]);
+      // (what saw nothing or only logits of -inf weighs nothing beside others; the latter make a row NaN that has nothing else.  Their
+      // sums are 0, or NaN where a value is not finite)
+      if (mi == -INFINITY) { l = top == -INFINITY ? l + li : l; o += oi; continue; }
       const float f = mi == top ? 1.f : __builtin_amdgcn_exp2f(mi - top);
       l += f * li;
-      o += f * *reinterpret_cast<const floatx4*>(&s_o[i][r][e]);
+      o += f * oi;
     }
     if (part >= 0) {
       const int64_t at = (part * a.inner + in) * a.part_rows + r;
@@ -650,7 +652,7 @@ __global__ __launch_bounds__(256) void page_join_kernel(PageAttnArgs a, int row_
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
   // part j: (ml, v) beside what there is; what has only logits of -inf weighs nothing beside others, and makes a row NaN alone
   auto add = [&](float2 ml, floatx4 v) {
-    if (ml.x == -INFINITY) { l = top == -INFINITY ? l + ml.y : l; return; }
+    if (ml.x == -INFINITY) { l = top == -INFINITY ? l + ml.y : l; o += v; return; }
     if (top == -INFINITY) l = 0.f;
     const float next = fmaxf(top, ml.x);
     const float f = top == next ? 1.f : __builtin_amdgcn_exp2f(top - next), g = ml.x == next ? 1.f : __builtin_amdgcn_exp2f(ml.x - next);

@@ -75,3 +75,25 @@ def test_a_key_that_is_not_a_number_makes_its_rows_not_numbers(case):
             else:
                 assert torch.equal(o[i, :G], base[i, :G]) and torch.equal(lse[i, :G], base_lse[i, :G])
         assert torch.equal(o[:, G:], base[:, G:]) and torch.equal(lse[:, G:], base_lse[:, G:])
+
+
+@pytest.mark.parametrize("case", CASES)
+def test_values_that_are_not_finite_beside_logits_of_minus_infinity(case):
+    """0 times such a value is not 0: the row is NaN, as it is where other tokens of the same tile have finite logits."""
+    c = Context(*case)
+    seen, G = case[4], case[2]
+    c.q.abs_()                                                 # a key of -inf makes its logit -inf
+    n = case[3]
+    for tokens in [[n - 1], [n // 2], list(range(n // 3, 2 * n // 3)), list(range(16 * (n // 16), n))]:
+        k = c.changed(c.k, tokens, -float("inf"))
+        base, base_lse = c.run(k=k)
+        assert torch.isfinite(base.float()).all()
+        for value in (float("nan"), float("inf")):
+            print("values", value, case, len(tokens), "from", tokens[0], flush=True)
+            o, lse = c.run(k=k, v=c.changed(c.v, tokens[-1:], value))
+            for i, s in enumerate(seen):
+                if s > tokens[-1]:
+                    assert torch.isnan(o[i, :G]).all(), (tokens[0], len(tokens), i)
+                else:
+                    assert torch.equal(o[i, :G], base[i, :G])
+            assert torch.equal(o[:, G:], base[:, G:]) and torch.equal(lse, base_lse)
