@@ -58,8 +58,9 @@ qcf_status qcf_page_append(const qcf_layer_desc* desc, const qcf_page_cache* cac
  * with lo and hi the bounds of page p of request b: no key of the page has a larger product with any of these queries.  The sum
  * is taken in 64 bits and rounded once to 32.  pages [B, n_q, H_kv, n_keep] gets the n_keep pages of the largest scores among
  * the ceil(seen / page_size) that the row sees, ascending, ties to the lower page, -1 behind the last.  The first n_first and
- * the last n_last of them rank before all others (n_first + n_last <= n_keep), then pages whose score is not a number or
- * infinite (a key that is not finite makes it so), and pages that are not in the table behind all others. */
+ * the last n_last of them rank before all others (n_first + n_last <= n_keep), then pages with a sum that is infinite or not a
+ * number, of either sign (a key or a query that is not finite makes it so), and pages that are not in the table behind all
+ * others.  A finite sum beyond the range of 32 bits counts as the largest or the least float. */
 size_t qcf_page_select_workspace_bytes(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, int32_t n_keep);
 qcf_status qcf_page_select(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, const void* q,
                            const int32_t* seen_dev, int32_t n_keep, int32_t n_first, int32_t n_last, int32_t* pages,

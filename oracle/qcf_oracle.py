@@ -416,12 +416,12 @@ def page_scores(q: np.ndarray, bounds: np.ndarray, pages: np.ndarray) -> np.ndar
 
 def page_select(score: np.ndarray, n_keep: int, n_first: int, n_last: int) -> np.ndarray:
     """Pages [H_kv, n_keep] of score [H_kv, P], ascending, -1 behind the last: the first and the last ones, then the largest
-    scores (as float32), ties to the lower page."""
+    scores (as float32; finite ones beyond its range as its largest or least value), ties to the lower page."""
     n_kv, P = score.shape
+    top = float(np.finfo(np.float32).max)
     out = np.full((n_kv, n_keep), -1, dtype=np.int64)
     for g in range(n_kv):
-        with np.errstate(over="ignore"):
-            s = score[g].astype(np.float32)
+        s = np.where(np.isfinite(score[g]), np.clip(score[g], -top, top), score[g]).astype(np.float32)
         always = [p for p in range(P) if p < n_first or p >= P - n_last]
         rest = sorted((p for p in range(P) if p not in always), key=lambda p: -s[p])
         kept = list(range(P)) if P <= n_keep else sorted(always + rest[:n_keep - len(always)])

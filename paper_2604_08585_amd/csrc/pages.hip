@@ -327,8 +327,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) void page_score_k
         }
       }
       if (next < count) load(phys, lo, hi);
-      const float sum = (float)(a0 + a1);
-      float s = sum == sum ? fmaxf(sum, -3.402823466e38f) : INFINITY;   // (the least float: above pages that are not there)
+      // (a sum that is not finite ranks first; what is beyond the floats stays above pages that are not there, and below those)
+      const double sum = a0 + a1;
+      float s = __builtin_isfinite(sum) ? __builtin_amdgcn_fmed3f((float)sum, -3.402823466e38f, 3.402823466e38f) : INFINITY;
       if (h0 + j >= G) s = -INFINITY;
       s = fmaxf(s, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(s), 0xb1, 0xf, 0xf, false)));    // the four queries
       s = fmaxf(s, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(s), 0x4e, 0xf, 0xf, false)));

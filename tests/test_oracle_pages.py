@@ -72,3 +72,14 @@ def test_selection_by_hand():
     assert orc.page_select(s, 2, 1, 1).tolist() == [[0, 6]]
     assert orc.page_select(s, 9, 1, 1).tolist() == [[0, 1, 2, 3, 4, 5, 6, -1, -1]]
     assert orc.page_select(np.zeros((1, 5)), 2, 0, 0).tolist() == [[0, 1]]
+
+
+def test_scores_that_are_not_finite_or_beyond_32_bits():
+    q = np.array([[np.inf, 1.0]])
+    bounds = np.zeros((3, 1, 2, 2))
+    bounds[0, 0, :, 0] = [-2.0, -1.0]                           # inf * -1: a sum of -inf
+    bounds[1, 0, :, 0] = [1.0, 2.0]                             # +inf
+    assert orc.page_scores(q, bounds, [0, 1, 2, 9])[0].tolist() == [np.inf, np.inf, np.inf, -np.inf]      # (inf * 0: not a number)
+    s = np.array([[-np.inf, -1e300, 1e39, 3.0, 1e300, np.inf, -3e38]])
+    order = [orc.page_select(s, n, 0, 0)[0].tolist() for n in range(1, 7)]
+    assert order == [[5], [2, 5], [2, 4, 5], [2, 3, 4, 5], [2, 3, 4, 5, 6], [1, 2, 3, 4, 5, 6]]
