@@ -177,6 +177,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _stream() -> int:
@@ -451,19 +452,34 @@ def qcf_gather(desc: LayerDesc, k_src: torch.Tensor, v_src: Optional[torch.Tenso
                                      _ptr(k_out), _ptr(v_out), _stream()))
 
 
+_PAGE_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
 class PageCache:
     """A layer's cache in pages: the descriptor that the calls take, and the tensors that it points into."""
 
     def __init__(self, desc: PageCacheDesc, tensors: tuple):
         self.desc, self.tensors = desc, tensors
-        self.requests = tensors[3].shape[0]        # rows of the table
+        k, _, _, table = tensors
+        self.requests = table.shape[0]             # rows of the table
+        self.dtype, self.device = k.dtype, k.get_device()
+        self.fits = (k.shape[2], k.shape[3], _PAGE_DTYPES.get(k.dtype))
         self.ref = C.byref(desc)
 
-    def of(self, B: int):
-        """The descriptor for a call over B requests."""
+    def of(self, B: int, desc: Optional[LayerDesc] = None):
+        """The descriptor for a call over B requests of a layer."""
         if B > self.requests:
             raise QcfError(f"{B} requests, {self.requests} rows in the table of pages")
+        if desc is not None and (desc.n_kv_heads, desc.head_dim, desc.dtype) != self.fits:
+            raise QcfError(f"pages of {self.fits[0]} heads of {self.fits[1]} in {self.dtype} for a layer of {desc.n_kv_heads} heads of "
+                           f"{desc.head_dim}, dtype {desc.dtype}")
         return self.ref
+
+    def stream(self) -> int:
+        """Handle of the current stream, if it is one of the device that has the pages."""
+        if self.device < 0 or _current_device() != self.device:
+            raise QcfError("tensors handed to the library must be CUDA tensors of the current device")
+        return _stream() if _raw_stream is None else _raw_stream(self.device)
 
 
 def page_cache(k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor], table: torch.Tensor) -> PageCache:
@@ -475,6 +491,10 @@ def page_cache(k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor],
         raise QcfError("tensors handed to the library must be CUDA tensors")
     if table.dim() != 2 or table.dtype != torch.int32:
         raise QcfError("table must be an int32 tensor [B, max_pages]")
+    if k.dtype not in _PAGE_DTYPES:
+        raise QcfError("pages of float32 or bfloat16 elements")
+    if any(t is not None and t.device != k.device for t in (v, bounds, table)):
+        raise QcfError("k, v, bounds and table must be on one device")
     n_pages, page_size, n_kv, d = k.shape
     if bounds is not None and (bounds.shape != (n_pages, n_kv, 2, d) or bounds.dtype != k.dtype):
         raise QcfError("bounds must have the shape [n_pages, H_kv, 2, d] and the type of the keys")
@@ -486,25 +506,49 @@ def page_cache(k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor],
                                    table.shape[1], 0), (k, v, bounds, table))
 
 
-def _rows(t: Optional[torch.Tensor], rows: int = 0):
+def _dense(name: str, t: Optional[torch.Tensor], count: int, dtype: torch.dtype, device: int) -> Optional[int]:
+    """Pointer of a contiguous tensor of `count` elements or more."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < count or t.get_device() != device or not t.is_contiguous():
+        raise QcfError(f"{name}: {count} contiguous elements of {dtype} on the device of the pages wanted, got {tuple(t.shape)}, "
+                       f"{t.dtype}, {t.device}")
+    return t.data_ptr()
+
+
+def _rows(t: Optional[torch.Tensor], rows: int = 0, heads: int = 0, cache: Optional[PageCache] = None):
     """Pointer and row stride of [rows, heads, d] or more rows, dense but for the distance of its rows."""
     if t is None:
         return None, 0
     shape, stride = t.shape, t.stride()          # (each attribute once: they are most of what a call takes here)
-    if len(stride) != 3 or not t.is_cuda or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2]):
+    if len(stride) != 3 or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2]) or (cache is None and not t.is_cuda):
         raise QcfError("rows handed to the library must be CUDA tensors [rows, heads, d] with dense rows")
     if shape[0] < rows:
         raise QcfError(f"{shape[0]} rows, {rows} wanted")
+    if cache is not None and (shape[1] != heads or shape[2] != cache.fits[1] or t.dtype is not cache.dtype or t.get_device() != cache.device):
+        raise QcfError(f"rows of {shape[1]} heads of {shape[2]} in {t.dtype} on {t.device}: {heads} heads of {cache.fits[1]} in "
+                       f"{cache.dtype} on the device of the pages wanted")
     return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1] * shape[2]
+
+
+def _page_ws(workspace: Optional[torch.Tensor], device: int):
+    if workspace is None:
+        return None, 0
+    return _dense("workspace", workspace, 0, workspace.dtype, device), workspace.nbytes
 
 
 def qcf_page_append(desc: LayerDesc, cache: PageCache, B: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
                     row_off: torch.Tensor, total_rows: int, lens: torch.Tensor, pos: Optional[torch.Tensor],
                     q_out: Optional[torch.Tensor]) -> None:
     """Rows of k and v behind what their requests hold (lens), keys and queries turned by pos on the way."""
-    (qp, qs), (kp, ks), (vp, vs) = _rows(q, total_rows), _rows(k, total_rows), _rows(v, total_rows)
-    _check(load_library().qcf_page_append(C.byref(desc), cache.of(B), B, qp, qs, kp, ks, vp, vs, _ptr(row_off), total_rows,
-                                          _ptr(lens), _ptr(pos), _ptr(q_out), _stream()))
+    ref, dev, H, Hkv = cache.of(B, desc), cache.device, desc.n_q_heads, cache.fits[0]
+    (qp, qs), (kp, ks), (vp, vs) = _rows(q, total_rows, H, cache), _rows(k, total_rows, Hkv, cache), _rows(v, total_rows, Hkv, cache)
+    status = (_lib or load_library()).qcf_page_append(
+        C.byref(desc), ref, B, qp, qs, kp, ks, vp, vs, _dense("row_off", row_off, B + 1, torch.int64, dev), total_rows,
+        _dense("lens", lens, B, torch.int32, dev), _dense("pos", pos, total_rows, torch.int32, dev),
+        _dense("q_out", q_out, total_rows * H * cache.fits[1], cache.dtype, dev), cache.stream())
+    if status:
+        _check(status)
 
 
 def qcf_page_select_workspace_bytes(desc: LayerDesc, cache: PageCache, B: int, n_q: int, n_keep: int) -> int:
@@ -513,11 +557,18 @@ def qcf_page_select_workspace_bytes(desc: LayerDesc, cache: PageCache, B: int, n
 
 def qcf_page_select(desc: LayerDesc, cache: PageCache, B: int, n_q: int, q: torch.Tensor, seen: torch.Tensor, n_keep: int,
                     n_first: int, n_last: int, pages: torch.Tensor, workspace: Optional[torch.Tensor] = None) -> None:
+    """The pages that attention of n_q new rows of each request is cut down to, for each row and KV head."""
+    if pages is not None and pages.shape[-1] != n_keep:
+        raise QcfError(f"pages has room for {pages.shape[-1]} pages to a row, n_keep is {n_keep}")
+    ref, dev, rows = cache.of(B, desc), cache.device, B * n_q
+    qp, sp = _dense("q", q, rows * desc.n_q_heads * cache.fits[1], cache.dtype, dev), _dense("seen", seen, rows, torch.int32, dev)
+    pp = _dense("pages", pages, rows * cache.fits[0] * n_keep, torch.int32, dev)
     if workspace is None:
         workspace = _workspace(qcf_page_select_workspace_bytes(desc, cache, B, n_q, n_keep), q.device)
-    wp, wn = _ws_args(workspace)
-    _check(load_library().qcf_page_select(C.byref(desc), cache.of(B), B, n_q, _ptr(q), _ptr(seen), n_keep, n_first, n_last,
-                                          _ptr(pages), wp, wn, _stream()))
+    wp, wn = _page_ws(workspace, dev)
+    status = (_lib or load_library()).qcf_page_select(C.byref(desc), ref, B, n_q, qp, sp, n_keep, n_first, n_last, pp, wp, wn, cache.stream())
+    if status:
+        _check(status)
 
 
 def qcf_page_attn_workspace_bytes(desc: LayerDesc, cache: PageCache, B: int, n_q: int, n_keep: int) -> int:
@@ -530,8 +581,14 @@ def qcf_page_attn(desc: LayerDesc, cache: PageCache, B: int, n_q: int, q: torch.
     """Attention of n_q new rows of each request over all its pages, or over those that `pages` lists for each row and KV head."""
     if pages is not None and pages.shape[-1] != n_keep:
         raise QcfError(f"pages lists {pages.shape[-1]} pages to a row, n_keep is {n_keep}")
+    ref, dev, rows = cache.of(B, desc), cache.device, B * n_q
+    heads = rows * desc.n_q_heads
+    qp, sp = _dense("q", q, heads * cache.fits[1], cache.dtype, dev), _dense("seen", seen, rows, torch.int32, dev)
+    pp = _dense("pages", pages, rows * cache.fits[0] * n_keep, torch.int32, dev)
+    op, zp = _dense("o_out", o_out, heads * cache.fits[1], cache.dtype, dev), _dense("lse_out", lse_out, heads, torch.float32, dev)
     if workspace is None:
         workspace = _workspace(qcf_page_attn_workspace_bytes(desc, cache, B, n_q, n_keep), q.device)
-    wp, wn = _ws_args(workspace)
-    _check(load_library().qcf_page_attn(C.byref(desc), cache.of(B), B, n_q, _ptr(q), _ptr(seen), _ptr(pages), n_keep, _ptr(o_out),
-                                        _ptr(lse_out), wp, wn, _stream()))
+    wp, wn = _page_ws(workspace, dev)
+    status = (_lib or load_library()).qcf_page_attn(C.byref(desc), ref, B, n_q, qp, sp, pp, n_keep, op, zp, wp, wn, cache.stream())
+    if status:
+        _check(status)
