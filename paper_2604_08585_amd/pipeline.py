@@ -393,6 +393,7 @@ class PagedLayer:
     first: int                     # of them, always kept: the first pages of a request
     last: int                      # and its last ones
     cache: qb.PageCache
+    room: List[int]                # tokens that each request can still take (counted by advance)
     held: torch.Tensor             # [B] int32: tokens that a request holds
     seen: torch.Tensor             # [B, new] int32: tokens that each new row sees
     pos: torch.Tensor              # [B * new] int32: absolute positions of the new rows
@@ -430,7 +431,7 @@ def paged_layer(L: DeviceLayer, more: int, page_size: int = 16, new: int = 1, ke
     step = torch.arange(new, dtype=torch.int32, device=dev)
     qkv = empty(rows, (H + 2 * Hkv) * d)
     P = PagedLayer(
-        desc=desc, B=L.B, new=new, keep=keep, first=first, last=last, cache=cache, held=held, seen=held[:, None] + 1 + step,
+        desc=desc, B=L.B, new=new, keep=keep, first=first, last=last, cache=cache, room=[more] * L.B, held=held, seen=held[:, None] + 1 + step,
         pos=(held[:, None] + step).flatten(), row_off=torch.arange(L.B + 1, dtype=torch.int64, device=dev) * new, qkv=qkv,
         parts=tuple(t.unflatten(1, (-1, d)) for t in qkv.split([H * d, Hkv * d, Hkv * d], 1)), q=empty(L.B, new, H, d),
         pages=empty(L.B, new, Hkv, keep, dtype=torch.int32) if keep else None, o=empty(L.B, new, H, d),
@@ -446,11 +447,15 @@ def paged_layer(L: DeviceLayer, more: int, page_size: int = 16, new: int = 1, ke
 def decode_step(P: PagedLayer, x: torch.Tensor, w_qkv: torch.Tensor) -> torch.Tensor:
     """One layer's attention for `new` tokens behind each request: x [B * new, d_model] (normed hidden states) is projected, keys and
     values go into the cache, rotated on the way, and the queries attend.  Returns o [B, new, H, d].  Lengths and positions live
-    on the device and are not moved: call `advance` after a step's last layer, or to accept fewer tokens than were drafted."""
+    on the device and are not moved: call `advance` after a step's last layer, or to accept fewer tokens than were drafted.  A step
+    for which a request has no room is refused; steps that a captured graph replays are not, so who replays them counts."""
     rows, dm = P.B * P.new, P.desc.d_model
     if x.shape != (rows, dm) or w_qkv.shape != (P.qkv.shape[1], dm) or x.dtype != P.qkv.dtype or w_qkv.dtype != P.qkv.dtype:
         raise ValueError(f"x {tuple(x.shape)} and w_qkv {tuple(w_qkv.shape)} for {P.B} requests of {P.new} rows of {dm}, "
                          f"{P.qkv.shape[1]} columns, {P.qkv.dtype}")
+    room = min(P.room, default=P.new)
+    if P.new > room:
+        raise ValueError(f"a step of {P.new} tokens to a request, room for {room} more behind request {P.room.index(room)}")
     qb.qcf_linear(P.desc, x, rows, dm, w_qkv, P.qkv.shape[1], None, P.qkv, P.ws_linear)
     q, k, v = P.parts
     qb.qcf_page_append(P.desc, P.cache, P.B, q, k, v, P.row_off, rows, P.held, P.pos, P.q.flatten(0, 1))
@@ -461,7 +466,13 @@ def decode_step(P: PagedLayer, x: torch.Tensor, w_qkv: torch.Tensor) -> torch.Te
 
 
 def advance(P: PagedLayer, tokens: int) -> None:
-    """Every request holds `tokens` tokens more (fewer than were appended: the others' slots are written again)."""
+    """Every request holds `tokens` tokens more, at most the `new` of a step (fewer: the others' slots are written again).  (Recorded
+    into a graph it moves lengths and positions at every replay, and what is left of the room not at all.)"""
+    room = min(P.room, default=tokens)
+    if not 0 <= tokens <= P.new or tokens > room:
+        raise ValueError(f"{tokens} tokens more to a request, {P.new} in a step, room for {room}")
+    if not (P.held.is_cuda and torch.cuda.is_current_stream_capturing()):
+        P.room = [r - tokens for r in P.room]
     P.held += tokens
     P.seen += tokens
     P.pos += tokens
