@@ -6,7 +6,8 @@ offset tables, and enqueues the calls of binding.py on the current stream.
 from __future__ import annotations
 
 import dataclasses
-from typing import Dict, List, Optional
+import operator
+from typing import Dict, List, Optional, Sequence, Union
 
 import numpy as np
 import torch
@@ -465,14 +466,29 @@ def decode_step(P: PagedLayer, x: torch.Tensor, w_qkv: torch.Tensor) -> torch.Te
     return P.o
 
 
-def advance(P: PagedLayer, tokens: int) -> None:
-    """Every request holds `tokens` tokens more, at most the `new` of a step (fewer: the others' slots are written again).  (Recorded
-    into a graph it moves lengths and positions at every replay, and what is left of the room not at all.)"""
-    room = min(P.room, default=tokens)
-    if not 0 <= tokens <= P.new or tokens > room:
-        raise ValueError(f"{tokens} tokens more to a request, {P.new} in a step, room for {room}")
-    if not (P.held.is_cuda and torch.cuda.is_current_stream_capturing()):
-        P.room = [r - tokens for r in P.room]
-    P.held += tokens
-    P.seen += tokens
-    P.pos += tokens
+def advance(P: PagedLayer, tokens: Union[int, Sequence[int], torch.Tensor]) -> None:
+    """Every request holds `tokens` tokens more, at most the `new` of a step (fewer: the others' slots are written again); a
+    sequence of one number for each request where they accept different ones.  The numbers are the host's, which counts the room.
+    (One number recorded into a graph moves lengths and positions at every replay, and what is left of the room not at all.)"""
+    if isinstance(tokens, torch.Tensor) and tokens.is_cuda:
+        raise ValueError("advance counts the room on the host: pass the accepted tokens as numbers, not as a CUDA tensor")
+    several = np.ndim(tokens) > 0
+    taken = [operator.index(t) for t in tokens] if several else [operator.index(tokens)] * P.B
+    if len(taken) != P.B:
+        raise ValueError(f"{len(taken)} numbers of tokens for {P.B} requests")
+    for t, room in zip(taken, P.room):
+        if not 0 <= t <= P.new or t > room:
+            raise ValueError(f"{t} tokens more to a request, {P.new} in a step, room for {room}")
+    capturing = P.held.is_cuda and torch.cuda.is_current_stream_capturing()
+    if several:
+        if capturing:
+            raise ValueError("the numbers of several requests come from the host and cannot be recorded into a graph")
+        more = torch.tensor(taken, dtype=torch.int32, device=P.held.device)
+        P.held += more
+        P.seen += more[:, None]
+        P.pos += more.repeat_interleave(P.new)
+    else:
+        for t in (P.held, P.seen, P.pos):
+            t += operator.index(tokens)
+    if not capturing:
+        P.room = [room - t for t, room in zip(taken, P.room)]

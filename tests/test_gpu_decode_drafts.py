@@ -1,0 +1,45 @@
+"""Decoding steps in which requests accept different numbers of their drafts, against the oracle's attention over what each holds."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import qcf_oracle as orc
+from paper_2604_08585_amd import inputs, pipeline
+from gpu_util import DEV, quantizer, to_np
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("batch,new,accepted", [
+    (3, 3, [[3, 0, 1], [2, 3, 1], [0, 1, 3]]), (2, 4, [[4, 1], [0, 3]]), (4, 2, [[2, 1, 0, 2], [1, 1, 2, 0], [2, 2, 2, 2]])])
+def test_requests_accept_different_numbers_of_drafts(batch, new, accepted):
+    sh = inputs.LayerShape(256, 4, 2, 64, 10000.0, "f32")
+    wl = inputs.make_config(4, orc.PlantOps(), scale=1 / 16, batch=batch, shape=sh)
+    L = pipeline.upload(wl, DEV)
+    pipeline.fuse_layer(L)
+    P = pipeline.paged_layer(L, more=new * len(accepted), new=new)
+    rng = np.random.default_rng(71)
+    quant = quantizer("f32")
+    off = np.concatenate([[0], np.cumsum(L.ctx_lens)])
+    k_ctx, v_ctx, w = to_np(L.k_fused), to_np(L.v_fused), np.asarray(wl.w_qkv, dtype=np.float64)
+    keys = [k_ctx[off[b]:off[b + 1]] for b in range(batch)]
+    values = [v_ctx[off[b]:off[b + 1]] for b in range(batch)]
+    for step, taken in enumerate(accepted):
+        x = quant(rng.standard_normal((batch * new, sh.d_model)))
+        o = to_np(pipeline.decode_step(P, torch.from_numpy(x).to(device=DEV, dtype=torch.float32), L.w_qkv))
+        y = quant(x @ w.T).reshape(batch, new, 8, 64)
+        for b in range(batch):
+            n = len(keys[b])
+            pos = n + np.arange(new)
+            q, k = (orc.rope_at(t, pos, sh.rope_base) for t in (y[b, :, :4], y[b, :, 4:6]))
+            k, v = np.concatenate([keys[b], k]), np.concatenate([values[b], y[b, :, 6:]])
+            ref, _ = orc.recompute_attn(q, pos, k, v)
+            print(f"step {step} request {b}: {n} + {new} tokens, worst {np.abs(o[b] - ref).max():.2e}", flush=True)
+            assert np.abs(o[b] - ref).max() <= 1e-4
+            keys[b], values[b] = k[:n + taken[b]], v[:n + taken[b]]
+        pipeline.advance(P, taken if step % 2 else torch.tensor(taken))
+    held = [n + sum(t[b] for t in accepted) for b, n in enumerate(L.ctx_lens)]
+    assert P.held.tolist() == held and P.pos.tolist() == [h + i for h in held for i in range(new)]
+    assert P.seen.tolist() == [[h + 1 + i for i in range(new)] for h in held]
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        pipeline.advance(P, torch.zeros(batch, dtype=torch.int32, device=DEV))

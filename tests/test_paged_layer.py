@@ -49,3 +49,33 @@ def test_advance_moves_lengths_and_positions():
     pipeline.advance(P, 2)
     pipeline.advance(P, 0)
     assert P.room == [7, 7] and _state(P) == _state(_layer(2, 3, 9, held=[12, 22]))
+
+
+@pytest.mark.parametrize("kind", [list, tuple, lambda t: torch.tensor(t), lambda t: torch.tensor(t, dtype=torch.int32).numpy()])
+def test_requests_accept_different_numbers(kind):
+    for B, new, taken in [(3, 3, [3, 0, 2]), (2, 3, [1, 3]), (1, 4, [2])]:        # (as many requests as rows, and not)
+        P = _layer(B, new, 9)
+        pipeline.advance(P, kind(taken))
+        assert P.room == [9 - t for t in taken]
+        assert _state(P) == _state(_layer(B, new, 9, held=[10 * (b + 1) + t for b, t in enumerate(taken)]))
+
+
+@pytest.mark.parametrize("taken,word", [([1, 2], "2 numbers"), ([1, 2, 3, 0], "4 numbers"), ([1, 4, 0], "4 tokens more"), ([1, -1, 0], "-1 tokens more"),
+                                        ([0, 3, 2], "room for 2")])
+def test_numbers_that_do_not_fit_change_nothing(taken, word):
+    P = _layer(3, 3, 2)
+    before = _state(P)
+    with pytest.raises(ValueError, match=word):
+        pipeline.advance(P, taken)
+    with pytest.raises(TypeError):
+        pipeline.advance(P, [0.5, 1, 1])
+    assert _state(P) == before and P.room == [2, 2, 2]
+
+
+def test_the_request_with_the_least_room_stops_a_step():
+    P = _layer(2, 2, 4)
+    pipeline.advance(P, [1, 2])
+    pipeline.advance(P, [0, 1])
+    assert P.room == [3, 1]
+    with pytest.raises(ValueError, match="room for 1 more behind request 1"):
+        pipeline.decode_step(P, torch.zeros(4, 256), torch.zeros(512, 256))
