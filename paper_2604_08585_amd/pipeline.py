@@ -415,6 +415,10 @@ def paged_layer(L: DeviceLayer, more: int, page_size: int = 16, new: int = 1, ke
     """The fused cache of a layer in pages, with room for `more` tokens behind every request's context (which begins at position
     0).  keep > 0: each new row's attention is cut down to that many pages for each KV head, the first `first` and the last `last`
     among them; the pages' bounds are kept for that."""
+    if more < 0 or not 0 <= new <= 16:
+        raise ValueError(f"room for {more} tokens, steps of {new} (at most 16)")
+    if keep < 0 or min(first, last) < 0 or (keep and first + last > keep):
+        raise ValueError(f"{keep} pages kept, the first {first} and the last {last} among them")
     desc, dev, dt = L.desc, L.k_fused.device, L.k_fused.dtype
     H, Hkv, d = desc.n_q_heads, desc.n_kv_heads, desc.head_dim
     counts = [-(-(n + more) // page_size) for n in L.ctx_lens]

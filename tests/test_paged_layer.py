@@ -79,3 +79,10 @@ def test_the_request_with_the_least_room_stops_a_step():
     assert P.room == [3, 1]
     with pytest.raises(ValueError, match="room for 1 more behind request 1"):
         pipeline.decode_step(P, torch.zeros(4, 256), torch.zeros(512, 256))
+
+
+@pytest.mark.parametrize("kw", [dict(more=-1), dict(more=4, new=17), dict(more=4, new=-1), dict(more=4, keep=1), dict(more=4, keep=-3),
+                                dict(more=4, keep=8, first=-1), dict(more=4, keep=8, first=4, last=5)])
+def test_layers_whose_steps_would_fail_are_refused_before_anything_is_appended(kw):
+    with pytest.raises(ValueError, match="room for|pages kept"):
+        pipeline.paged_layer(None, **kw)
