@@ -1,4 +1,4 @@
-// How the attention over a cache in pages divides its contexts: plain code of the host and the device, which tests compile.
+// How the calls over a cache in pages divide their work: plain code of the host and the device, which tests compile.
 #pragma once
 
 #include <stdint.h>
@@ -97,6 +97,27 @@ inline size_t sums_bytes(const qcf_layer_desc& L, const Division& d) { return pa
 inline bool divides(const Division& d) { return !d.whole && d.slots > 1; }
 inline size_t workspace(const qcf_layer_desc& L, const Division& d) {
   return divides(d) ? sums_bytes(L, d) + parts(d) * 2 * sizeof(float) : 0;
+}
+
+// Units of an append, one to each page that gets rows: those of request b start at row_off[b] / page + 2 b, which leaves room for
+// every page that its rows can touch (n rows touch at most floor((n - 1) / page) + 2).
+inline int64_t append_units(const qcf_page_cache& c, int32_t B, int64_t total_rows) { return total_rows / c.page_size + 2 * (int64_t)B; }
+
+// KV heads of an append's workgroup: a power of two of them, whose vectors of a row fill a wave at most, as long as every compute
+// unit has a workgroup (two where a page has 256 rows).  More share their (cos, sin) and whole rows, fewer give a short call more
+// workgroups: 8 KV heads of 128, us, with one head, by this rule and with all eight: 500 rows 7.9, 8.1 and 14.8, 8000 in pages of 64
+// 53.1, 43.8 and 80.8, 256 requests of one row 20.0, 8.7 and 9.4; 16 requests of 1000 to 2000 in pages of 256 163 (208 with one workgroup
+// to a compute unit), in pages of 128 143 (156 with two).  About three workgroups to a compute unit, which fill it once, are slower
+// than twice as many: 4 requests of 2000 to 4000 rows in pages of 16 84 and 75, 32 of 1000 to 2000 in pages of 64 303 and 270.
+inline int append_heads(const qcf_layer_desc& L, const qcf_page_cache& c, int64_t units) {
+  const int per_row = L.head_dim / 2 / (L.dtype == QCF_DTYPE_BF16 ? 8 : 4);            // 16-byte vectors of half a row
+  const int cus = compute_unit_count(), wanted = (c.page_size >= 256 ? 2 : 1) * cus;
+  int heads = 1;
+  while (L.n_kv_heads % (2 * heads) == 0 && 2 * heads * per_row <= 64 && units * (L.n_kv_heads / (2 * heads)) >= wanted)
+    heads *= 2;
+  const int64_t groups = units * (L.n_kv_heads / heads);
+  if (heads > 1 && 2 * groups > 5 * cus && groups < 4 * cus) heads /= 2;
+  return heads;
 }
 
 }  // namespace pages

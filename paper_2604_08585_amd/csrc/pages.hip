@@ -1,5 +1,6 @@
 // Decoding over a cache in pages: new rows into their pages, and the scores of a request's pages for its new queries.
 #include "qcf_internal.h"
+#include "page_layout.h"
 
 namespace qcf {
 namespace {
@@ -46,9 +47,9 @@ __device__ __forceinline__ u32x4 rounded(const float* f) {
 __device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 __device__ __forceinline__ float largest(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// Request of a unit: units of request b start at row_off[b] / page + 2 b, which leaves room for every page that its rows can touch
-// (n rows touch at most floor((n - 1) / page) + 2), so that no sum over the requests stands in front of the rows.  Every wave
-// looks for the last request that starts at or before the unit; offsets and lengths of the first 64 are on their way together.
+// Request of a unit: units of request b start at row_off[b] / page + 2 b (pages::append_units), so that no sum over the requests
+// stands in front of the rows.  Every wave looks for the last request that starts at or before the unit; offsets and lengths of the
+// first 64 are on their way together.
 struct Request {
   int b;
   int64_t r0, r1, len, unit0;     // its rows, the tokens that it holds, its first unit
@@ -356,20 +357,9 @@ qcf_status launch_page_append(const qcf_layer_desc& L, const qcf_page_cache& c, 
   a.B = B; a.H = L.n_q_heads; a.Hkv = L.n_kv_heads;
   a.log2_page = __builtin_ctz((unsigned)c.page_size);
   a.neg2_over_d_log2base = -2.0 / L.head_dim * std::log2(L.rope_base);
-  // KV heads of a workgroup: a power of two of them, whose vectors of a row fill a wave at most, as long as every compute unit
-  // has a workgroup (two where a page has 256 rows).  More share their (cos, sin) and whole rows, fewer give a short call more
-  // workgroups: 8 KV heads of 128, us, with one head, by this rule and with all eight: 500 rows 7.9, 8.1 and 14.8, 8000 in pages of 64
-  // 53.1, 43.8 and 80.8, 256 requests of one row 20.0, 8.7 and 9.4; 16 requests of 1000 to 2000 in pages of 256 163 (208 with one workgroup
-  // to a compute unit), in pages of 128 143 (156 with two).  About three workgroups to a compute unit, which fill it once, are slower
-  // than twice as many: 4 requests of 2000 to 4000 rows in pages of 16 84 and 75, 32 of 1000 to 2000 in pages of 64 303 and 270.
-  const int64_t units = (total_rows >> a.log2_page) + 2 * (int64_t)B;
+  const int64_t units = pages::append_units(c, B, total_rows);
+  const int heads = pages::append_heads(L, c, units);
   const int per_row = L.head_dim / 2 / (16 / elem_size(L.dtype));
-  const int cus = compute_unit_count(), wanted = (c.page_size >= 256 ? 2 : 1) * cus;
-  int heads = 1;
-  while (L.n_kv_heads % (2 * heads) == 0 && 2 * heads * per_row <= 64 && units * (L.n_kv_heads / (2 * heads)) >= wanted)
-    heads *= 2;
-  const int64_t groups = units * (L.n_kv_heads / heads);
-  if (heads > 1 && 2 * groups > 5 * cus && groups < 4 * cus) heads /= 2;
   const int log2_lanes = __builtin_ctz((unsigned)(heads * per_row));
   const int64_t blocks = units * (L.n_kv_heads / heads);
   if (blocks > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page append: too many rows");

@@ -43,3 +43,35 @@ def test_requests_accept_different_numbers_of_drafts(batch, new, accepted):
     assert P.seen.tolist() == [[h + 1 + i for i in range(new)] for h in held]
     with pytest.raises(ValueError, match="CUDA tensor"):
         pipeline.advance(P, torch.zeros(batch, dtype=torch.int32, device=DEV))
+
+
+@pytest.mark.parametrize("cfg,kw", [(0, dict(keep=9)), (0, dict(keep=5, first=0, last=2, new=2)), (4, dict(keep=6, new=3))])
+def test_the_pages_of_a_step_are_the_best_of_the_bounds_that_append_kept(cfg, kw):
+    """The bounds after the fused cache went into pages, unrotated, and steps behind it: those of the stored keys, page by page."""
+    if cfg:
+        wl = inputs.make_config(4, orc.PlantOps(), scale=1 / 8, batch=40, shape=inputs.LayerShape(512, 8, 8, 64, 10000.0, "bf16"))
+    else:
+        wl = inputs.make_config(0, orc.PlantOps())
+    L = pipeline.upload(wl, DEV)
+    pipeline.fuse_layer(L)
+    new = kw.get("new", 1)
+    P = pipeline.paged_layer(L, more=2 * new, **kw)
+    rng = np.random.default_rng(72)
+    k_ctx = to_np(L.k_fused)
+    off = np.concatenate([[0], np.cumsum(L.ctx_lens)])
+    for step in range(2):
+        x = torch.from_numpy(rng.standard_normal((L.B * new, P.desc.d_model)).astype(np.float32)).to(device=DEV, dtype=L.k_fused.dtype)
+        pipeline.decode_step(P, x, L.w_qkv)
+        k, bounds, table = to_np(P.cache.tensors[0]), to_np(P.cache.tensors[2]), P.cache.tensors[3].cpu().numpy()
+        q, seen, pages = to_np(P.q), P.seen.cpu().numpy(), P.pages.cpu().numpy()
+        for b in range(L.B):
+            held = L.ctx_lens[b] + (step + 1) * new
+            for pg in range(-(-held // 16)):
+                rows = k[table[b, pg], :min(16, held - 16 * pg)]
+                if 16 * (pg + 1) <= L.ctx_lens[b]:
+                    assert np.array_equal(rows, k_ctx[off[b] + 16 * pg:off[b] + 16 * (pg + 1)])
+                assert np.array_equal(bounds[table[b, pg], :, 0], rows.min(0)) and np.array_equal(bounds[table[b, pg], :, 1], rows.max(0))
+            for i in range(new):
+                s = orc.page_scores(q[b, i], bounds, table[b, :-(-seen[b, i] // 16)])
+                assert np.array_equal(pages[b, i], orc.page_select(s, P.keep, P.first, P.last)), (step, b, i)
+        pipeline.advance(P, new)
