@@ -7,6 +7,7 @@
  *   call order for one layer and one step:
  *     qcf_page_append -> [qcf_page_select ->] qcf_page_attn
  *   (all on one stream; the fused cache itself goes into pages with qcf_page_append, unrotated)
+ *   (B is at most 65535 in each; a launch takes 2^32 threads at most, so selections of B * n_q * H_kv beyond 2^22 are refused)
  */
 #ifndef QCF_PAGES_H
 #define QCF_PAGES_H

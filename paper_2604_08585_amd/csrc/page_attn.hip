@@ -691,7 +691,8 @@ qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t s
   const bool shared = (int64_t)d.contexts * 4 < d.slots;
   const int row_steps = shared ? a.part_rows : (a.part_rows + 1024 / D - 1) / (1024 / D);
   const int64_t joins = (int64_t)std::min(d.contexts, d.slots) * d.inner * row_steps;
-  if (blocks > 0x7fffffff || joins > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page attention: too many rows");
+  if (blocks > pages::kThreadsAtMost / (64 * (d.whole ? pages::kWholeWaves : pages::kWaves)) || joins > pages::kThreadsAtMost / 256)
+    return fail(QCF_ERR_UNSUPPORTED, "page attention: too many rows");
   const dim3 grid((unsigned)blocks);
 #define QCF_LAUNCH(RT, MODE, WAVES, WHOLE) page_attn_kernel<T, D, RT, MODE, WAVES, WHOLE><<<grid, dim3(64 * WAVES), 0, st>>>(a)
 #define QCF_ROWS(MODE)                                                                          \

@@ -20,6 +20,8 @@ namespace pages {
 constexpr int kWaves = 4;                 // of a workgroup; each takes every fourth tile of its part of a context
 constexpr int kWholeWaves = 8;            // of a workgroup that has a context as a whole
 constexpr int kGrain = 32;                // contexts are divided at multiples of this many tokens
+constexpr int64_t kThreadsAtMost = 0xffffffff;               // of a launch: a dispatch counts them in 32 bits
+constexpr int kTopThreads = 1024;         // of a workgroup that chooses a row's pages
 constexpr int kShared = 16 << 20;         // bytes of keys and values from which on two tiles of rows share a workgroup
 
 // Grains of a range: a tile of 32 tokens (bf16) or 16 for every wave.

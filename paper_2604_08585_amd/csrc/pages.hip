@@ -362,7 +362,7 @@ qcf_status launch_page_append(const qcf_layer_desc& L, const qcf_page_cache& c, 
   const int per_row = L.head_dim / 2 / (16 / elem_size(L.dtype));
   const int log2_lanes = __builtin_ctz((unsigned)(heads * per_row));
   const int64_t blocks = units * (L.n_kv_heads / heads);
-  if (blocks > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page append: too many rows");
+  if (blocks > pages::kThreadsAtMost / kThreads) return fail(QCF_ERR_UNSUPPORTED, "page append: too many rows");
 #define QCF_LAUNCH(T, D, S) append_kernel<T, D, S><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, heads, log2_lanes)
 #define QCF_STYLE(T, D) do { if (L.rope_style == 0) QCF_LAUNCH(T, D, 0); else QCF_LAUNCH(T, D, 1); } while (0)
   if (L.dtype == QCF_DTYPE_BF16) {
@@ -390,7 +390,8 @@ qcf_status launch_page_select(const qcf_layer_desc& L, const qcf_page_cache& c, 
   const int64_t rows = (int64_t)B * n_q, steps = ((int64_t)c.max_pages + kScoreStep - 1) / kScoreStep;
   const int64_t most = 6 * (int64_t)compute_unit_count() / (rows * L.n_kv_heads);
   const int64_t parts = std::min(steps, std::max<int64_t>(most, 1)), blocks = rows * L.n_kv_heads * parts;
-  if (blocks > 0x7fffffff) return fail(QCF_ERR_UNSUPPORTED, "page select: too many rows");
+  if (blocks > pages::kThreadsAtMost / kThreads || rows * L.n_kv_heads > pages::kThreadsAtMost / pages::kTopThreads)
+    return fail(QCF_ERR_UNSUPPORTED, "page select: too many rows");
   const int log2_page = __builtin_ctz((unsigned)c.page_size);
 #define QCF_LAUNCH(T, D)                                                                                              \
   page_score_kernel<T, D><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(c, static_cast<const T*>(q), seen, n_q,  \

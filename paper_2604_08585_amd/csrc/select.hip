@@ -12,6 +12,7 @@
 
 #include "qcf_internal.h"
 #include "score_layout.h"
+#include "page_layout.h"
 
 namespace qcf {
 namespace {
@@ -21,6 +22,7 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kDigitBits = 10;               // bits resolved per histogram (8192 keys: 9 bits 6.8 us, 10 6.4)
 constexpr int kBins = 1 << kDigitBits;
 static_assert(kBins == kThreads && kWaves == 16, "a thread has one bin, a row of lanes the waves' sums");
+static_assert(kThreads == pages::kTopThreads);
 constexpr int kRanked = 128;                 // keys of one bin that are ranked against each other, and not split further (64 and 256 alike)
 constexpr int kListed = kThreads;            // keys of one bin that are listed, one to a thread, and not looked for again
 constexpr int kStage = 8192;                 // outputs that leave together
