@@ -45,14 +45,16 @@ struct Division {
 
 // Whether workgroups of eight waves take whole contexts, in one launch, or four waves each range of them, in two.  The second launch
 // takes 4 to 5 us, a compute unit reads 50 to 60 GB/s at most; what is saved by dividing shrinks as more workgroups share the
-// memory.  Heads of 128 in bf16, whole and divided, us: 8 workgroups (a request, 8 KV heads) of 512 tokens 9.9 and 10.8, 1024 14.8 and
-// 11.7; 64 of up to 1024 tokens 15.9 and 14.8; 128 of up to 1536 21.2 and 23.6, 2048 36.5 and 30.9; 512 of up to 1024 49 and 55, 4096
-// 159 and 161, 8192 313 and 302.  Heads of 64: 16 of 1536 tokens 12.4 and 13.4, 2048 15.7 and 11.8; 512 of up to 4096 97 and 103.
-// In float32, heads of 64: 2 of 512 tokens 10.4 and 10.8, 768 13.6 and 11.2; 16 of up to 512 10.9 and 10.8.
+// memory.  us on the GPU, whole and divided.  Heads of 128 in bf16: 8 workgroups (a request, 8 KV heads) of 512 tokens 10.0 and 9.5, of
+// 1024 15.3 and 10.3; 64 of up to 768 12.8 and 12.5, 1024 16.0 and 13.4; 128 of up to 1024 17.6 and 20.6, 1536 21.4 and 23.5, 2048 27.9 and
+// 28.7, 4096 48.1 and 42.1; 512 of up to 1024 40.0 and 42.7, 4096 161 and 159.  Heads of 64: 16 of up to 1024 11.0 and 12.9, 1536 12.8 and
+// 13.1, 2048 16.3 and 11.1.  In float32, heads of 64: 2 of 512 10.8 and 9.7, 4 of up to 512 10.9 and 12.3, 1024 15.9 and 10.5.  Over eight
+// shapes, 1 to 64 requests and 256 to 8192 tokens the rule is 0.5 % behind the better of the two on average (272 KB in place of 290:
+// 0.6 %, 350: 0.9 %); at its border it takes the worse one by up to 11 % (19 % in float32), and by 25 % for 2048 workgroups of up to 256 tokens.
 inline bool takes_whole(const qcf_layer_desc& L, int64_t workgroups, int64_t longest) {
   const int64_t bytes = longest * 2 * L.head_dim * (L.dtype == QCF_DTYPE_BF16 ? 2 : 4);
   const int64_t alone = std::max<int64_t>(30, 200 - workgroups * 256 / compute_unit_count());      // of 200
-  return bytes * alone <= (int64_t)((L.dtype == QCF_DTYPE_BF16 ? 272 : 240) << 10) * 200;
+  return bytes * alone <= (int64_t)((L.dtype == QCF_DTYPE_BF16 ? 290 : 240) << 10) * 200;
 }
 
 inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, int32_t n_keep) {
