@@ -23,6 +23,8 @@ extern "C" {
  * attended to.  Requests may share pages that none of them writes.
  * Slot s of page p, KV head g: d elements from p * page_stride + s * slot_stride + g * head_stride on, of k and of v.  Any order is
  * taken; pages that keep a head's tokens together are read 4 to 5 % faster than pages that keep a token's heads together.
+ * The calls read lengths on the device and divide their work by max_pages: one request of 256 tokens is attended to in 7.0 us with a
+ * table of 16 pages, 9.9 with one of 512 or 8192 (two launches); where contexts are long it makes no difference.
  * Strides are in elements, multiples of 8, at most 2^24 for slots and heads; rows of a page must not overlap, and page_stride
  * must be at least what a page spans. */
 typedef struct qcf_page_cache {

@@ -4,7 +4,8 @@
 // equal ranges, as many as the GPU holds at once; a second launch joins the partial results of contexts that several ranges have.
 // Bound by memory: 4 d operations to a token and row against 4 d bytes (bf16) to a token and KV head, which is an operation a byte for
 // each row, 4 to 32 of them.  32 / 8 heads of 128, 64 requests of 4K to 12K tokens: 395 us, 5.5 TB/s, the bytes of the keys and values
-// and no more (counters; a copy of 1 GiB reaches 5.05 TB/s); one of 128K 101 us; one of 731 tokens 10.5 us, 6.8 and 4.6 of it in two launches.
+// and no more (counters; a copy of 1 GiB reaches 5.05 TB/s); one of 128K 101 us; one of 731 tokens 10.4 us, in two launches that depend on
+// each other (6.9 and 4.5 us where a profiler keeps them apart).
 //
 // A wave takes 32 tokens (16 in float32) at a time, without LDS: the logits are products K Q^T of 16 tokens x 16 rows, so a lane
 // owns a row and four tokens; the outputs are V^T P^T of 16 elements x 16 rows, in which the order of the tokens is free.  It

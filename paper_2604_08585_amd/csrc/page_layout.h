@@ -29,7 +29,8 @@ inline int least_range(const qcf_layer_desc& L) { return L.dtype == QCF_DTYPE_BF
 
 // The contexts, laid end to end in grains (one at least for each), are cut into equal ranges, one to a workgroup, as many as the
 // GPU holds at once: a range may end inside a context, and may hold several.  (Units of equal length within each context, the last
-// one shorter, left the workgroups unequal where lengths differ: 64 requests of 4K to 12K 480 us, 16 of 1K to 8K 84; 399 and 71 so.)
+// one shorter, left the workgroups unequal where lengths differ: 64 requests of 4K to 12K 480 us, 16 of 1K to 8K 84; 399 and 71
+// with ranges when they came in, 395 and 70 now.)
 struct Division {
   int contexts;                           // B, or B * n_q where every row has pages of its own
   int rows;                               // rows of a context and KV head: (new rows) * heads of the group
@@ -75,8 +76,8 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   if (d.slots < 1) d.slots = 1;
   d.most = (int64_t)d.contexts * ((longest + kGrain - 1) / kGrain);
   d.least = least_range(L);
-  // (four drafts of 8 requests of 2K to 6K tokens, 32 rows: 53.0 us without, 48.1 with 12, 47.1 with 18, 50.0 with 28; two workgroups on
-  // a compute unit cover for each other, 0 to 9 are the same there)
+  // (four drafts of 8 requests of 2K to 6K tokens, 32 rows, before later steps, which brought 47 to 44 us: 53.0 us without, 48.1 with 12,
+  // 47.1 with 18, 50.0 with 28; two workgroups on a compute unit cover for each other, 0 to 9 are the same there)
   d.pad = d.contexts > 1 && d.row_tiles == 2 ? 16 : 0;
   d.whole = d.row_tiles == 1 && takes_whole(L, (int64_t)d.contexts * d.inner, longest);
   const int64_t ranges = (d.most + d.least - 1) / d.least;
