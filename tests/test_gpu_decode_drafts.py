@@ -76,3 +76,37 @@ def test_the_pages_of_a_step_are_the_best_of_the_bounds_that_append_kept(cfg, kw
                 s = orc.page_scores(q[b, i], bounds, table[b, :-(-seen[b, i] // 16)])
                 assert np.array_equal(pages[b, i], orc.page_select(s, P.keep, P.first, P.last)), (step, b, i)
         pipeline.advance(P, new)
+
+
+@pytest.mark.parametrize("inside", [True, False])                # advance recorded with the step, or called between replays
+def test_steps_replayed_from_a_graph(inside):
+    wl = inputs.make_config(0, orc.PlantOps())
+    L = pipeline.upload(wl, DEV)
+    pipeline.fuse_layer(L)
+    x = torch.from_numpy(np.random.default_rng(73).standard_normal((5, 2 * L.B, 256)).astype(np.float32)).to(DEV)
+    eager = pipeline.paged_layer(L, more=12, new=2)
+    want = []
+    for i in range(5):
+        want.append(pipeline.decode_step(eager, x[i], L.w_qkv).clone())
+        pipeline.advance(eager, 2)
+    P = pipeline.paged_layer(L, more=12, new=2)
+    now = torch.empty_like(x[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pipeline.decode_step(P, now, L.w_qkv)
+        if inside:
+            pipeline.advance(P, 2)
+            with pytest.raises(ValueError, match="recorded"):
+                pipeline.advance(P, [2] * P.B)
+    assert P.room == [12] * P.B
+    for i in range(5):
+        now.copy_(x[i])
+        P.o.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(P.o, want[i]), i
+        if not inside:
+            pipeline.advance(P, 2)
+    assert P.held.tolist() == eager.held.tolist() and P.seen.tolist() == eager.seen.tolist() and P.pos.tolist() == eager.pos.tolist()
+    assert P.room == ([12] if inside else [2]) * P.B and eager.room == [2] * P.B
