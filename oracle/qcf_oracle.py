@@ -449,3 +449,101 @@ def page_attn(q: np.ndarray, k_pool: np.ndarray, v_pool: np.ndarray, table_row: 
         o[h] = e @ v_pool[at, slot, g].astype(F64) / e.sum()
         lse[h] = top + math.log(e.sum())
     return o, lse
+
+
+# --------------------------------------------------------------------------
+# 8-bit pages; accumulated attention weights and eviction
+# --------------------------------------------------------------------------
+
+def e4m3(x: np.ndarray) -> np.ndarray:
+    """The nearest e4m3 value (three bits behind the first one, steps of 2^-9 at the least, ties to even); |x| <= 448 or NaN."""
+    x = np.asarray(x, dtype=F64)
+    _, e = np.frexp(np.where(np.isfinite(x), x, 0.0))
+    step = np.ldexp(1.0, np.maximum(e - 1, -6) - 3)
+    return np.round(x / step) * step
+
+
+def page8_scale(x: np.ndarray) -> float:
+    """The least power of two s >= 2^-100 with |x| <= 448 s for every element up to 2^100."""
+    a = np.abs(np.asarray(x, dtype=F64))
+    a = a[a <= 2.0 ** 100]
+    amax, s = (a.max() if a.size else 0.0), 2.0 ** -100
+    while amax > 448.0 * s:
+        s *= 2.0
+    return s
+
+
+def page8_values(codes: np.ndarray, scales: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
+    """Elements of pools (k, v) of code values [n_pages, page, H_kv, d] with scales [n_pages, H_kv, 2, page / 16]."""
+    per_slot = np.repeat(np.asarray(scales, dtype=F64), 16, axis=3).transpose(2, 0, 3, 1)[..., None]      # [2, n_pages, page, H_kv, 1]
+    return codes[0] * per_slot[0], codes[1] * per_slot[1]
+
+
+def page8_append(codes: Sequence[np.ndarray], scales: np.ndarray, bounds: np.ndarray, table: np.ndarray, lens: Sequence[int],
+                 row_off: Sequence[int], k: np.ndarray, v: np.ndarray, pos: Optional[np.ndarray], base: float, style: int = 0):
+    """page_append into pools of code values with scales: rows of a block are rounded with one scale, the block's tokens in front of
+    them again where it grows.  Returns (k codes, v codes), scales, bounds."""
+    out, scales, bounds = [np.array(c, dtype=F64) for c in codes], np.array(scales, dtype=F64), np.array(bounds, dtype=F64)
+    k = np.asarray(k, dtype=F64) if pos is None else rope_at(k, pos, base, style)
+    n_pages, page, n_kv, _ = out[0].shape
+    for b in range(len(lens)):
+        t, end = lens[b], lens[b] + row_off[b + 1] - row_off[b]
+        while t < end:
+            n = min(end, (t // 16 + 1) * 16) - t
+            p = table[b, t // page] if 0 <= t // page < table.shape[1] else -1
+            m, slot = row_off[b] + t - lens[b], t % page
+            t += n
+            if not 0 <= p < n_pages:
+                continue
+            front, blk = slot // 16 * 16, slot // 16
+            for g in range(n_kv):
+                for which, x in enumerate((k, v)):
+                    rows = np.where(np.abs(x[m:m + n, g]) <= 2.0 ** 100, x[m:m + n, g], np.nan)
+                    s, pool = page8_scale(rows), out[which]
+                    again = slice(slot, slot)
+                    if slot > front:
+                        s = max(s, scales[p, g, which, blk])
+                        if s > scales[p, g, which, blk]:
+                            again = slice(front, slot)
+                            pool[p, again, g] = e4m3(pool[p, again, g] * (scales[p, g, which, blk] / s))
+                    scales[p, g, which, blk] = s
+                    pool[p, slot:slot + n, g] = e4m3(rows / s)
+                    if which == 0:
+                        new = pool[p, again.start:slot + n, g] * s
+                        lo, hi = new.min(0), new.max(0)
+                        if slot > 0:
+                            lo, hi = np.minimum(lo, bounds[p, g, 0]), np.maximum(hi, bounds[p, g, 1])
+                        bounds[p, g, 0], bounds[p, g, 1] = lo, hi
+    return out, scales, bounds
+
+
+def page_weigh(weights: np.ndarray, q: np.ndarray, k_pool: np.ndarray, table_row: np.ndarray, seen: Sequence[int], lse: np.ndarray,
+               old: int, alpha: float, beta: float) -> np.ndarray:
+    """One request: weights [H_kv, tokens], q [n_q, H, d], seen [n_q], lse [n_q, H]."""
+    n_pages, page, n_kv, d = k_pool.shape
+    group = q.shape[1] // n_kv
+    w = np.array(weights, dtype=F64)
+    most = min(max(max(seen), 0), len(table_row) * page)
+    w[:, min(max(old, 0), most):most] = 0.0
+    w[:, :most] *= alpha
+    for i, n in enumerate(seen):
+        for t in range(min(max(n, 0), most)):
+            p = table_row[t // page]
+            if not 0 <= p < n_pages:
+                continue
+            for g in range(n_kv):
+                z = np.asarray(q[i, g * group:(g + 1) * group], dtype=F64) @ np.asarray(k_pool[p, t % page, g], dtype=F64) / math.sqrt(d)
+                w[g, t] += beta * np.exp(z - lse[i, g * group:(g + 1) * group]).sum()
+    return w
+
+
+def page_evict(weights: np.ndarray, length: int, n_keep: int, n_first: int, n_last: int) -> np.ndarray:
+    """Tokens that stay [H_kv, n_keep] of one request, ascending, -1 behind the last; NaN ranks first."""
+    out = np.full((weights.shape[0], n_keep), -1, dtype=np.int64)
+    for g, w in enumerate(np.asarray(weights, dtype=F64)):
+        always = [t for t in range(length) if t < n_first or t >= length - n_last]
+        forced = set(always)
+        rest = sorted((t for t in range(length) if t not in forced), key=lambda t: (not np.isnan(w[t]), 0.0 if np.isnan(w[t]) else -w[t]))
+        kept = list(range(length)) if length <= n_keep else sorted(always + rest[:n_keep - len(always)])
+        out[g, :len(kept)] = kept
+    return out

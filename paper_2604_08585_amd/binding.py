@@ -44,6 +44,10 @@ FUSE_EXPORTS = ["qcf_fuse_layer"]
 PAGES_EXPORTS = ["qcf_page_append", "qcf_page_select_workspace_bytes", "qcf_page_select", "qcf_page_attn_workspace_bytes",
                  "qcf_page_attn"]
 
+# declared in qcf_pages8.h and qcf_evict.h
+PAGES8_EXPORTS = ["qcf_page8_append", "qcf_page8_attn_workspace_bytes", "qcf_page8_attn"]
+EVICT_EXPORTS = ["qcf_page_weigh", "qcf_page_evict_workspace_bytes", "qcf_page_evict"]
+
 
 class QcfError(RuntimeError):
     pass
@@ -153,6 +157,18 @@ def load_library() -> C.CDLL:
     lib.qcf_page_select.argtypes = [dp, cp, i32, i32, vp, vp, i32, i32, i32, vp, vp, sz, vp]
     lib.qcf_page_attn.restype = C.c_int
     lib.qcf_page_attn.argtypes = [dp, cp, i32, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.qcf_page8_append.restype = C.c_int
+    lib.qcf_page8_append.argtypes = [dp, cp, vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]
+    lib.qcf_page8_attn_workspace_bytes.restype = sz
+    lib.qcf_page8_attn_workspace_bytes.argtypes = [dp, cp, i32, i32, i32]
+    lib.qcf_page8_attn.restype = C.c_int
+    lib.qcf_page8_attn.argtypes = [dp, cp, vp, i32, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.qcf_page_weigh.restype = C.c_int
+    lib.qcf_page_weigh.argtypes = [dp, cp, vp, i32, i32, vp, vp, vp, vp, C.c_float, C.c_float, vp, vp]
+    lib.qcf_page_evict_workspace_bytes.restype = sz
+    lib.qcf_page_evict_workspace_bytes.argtypes = [dp, cp, i32, i32]
+    lib.qcf_page_evict.restype = C.c_int
+    lib.qcf_page_evict.argtypes = [dp, cp, vp, i32, vp, vp, i32, i32, i32, cp, vp, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -475,11 +491,69 @@ class PageCache:
                            f"{desc.head_dim}, dtype {desc.dtype}")
         return self.ref
 
+    of_any = of                                    # (for calls that take 8-bit pages too)
+    scales = scales_ptr = None
+
+    @property
+    def tokens(self) -> int:
+        """Tokens that a row of the table has room for."""
+        return self.desc.max_pages * self.desc.page_size
+
     def stream(self) -> int:
         """Handle of the current stream, if it is one of the device that has the pages."""
         if self.device < 0 or _current_device() != self.device:
             raise QcfError("tensors handed to the library must be CUDA tensors of the current device")
         return _stream() if _raw_stream is None else _raw_stream(self.device)
+
+
+class Page8Cache(PageCache):
+    """A layer's cache in 8-bit pages: `dtype` is the type of the layer's rows."""
+
+    def __init__(self, desc: PageCacheDesc, tensors: tuple, scales: torch.Tensor, dtype: torch.dtype):
+        super().__init__(desc, tensors)
+        self.dtype, self.scales, self.scales_ptr = dtype, scales, scales.data_ptr()
+        self.fits = self.fits[:2] + (_PAGE_DTYPES[dtype],)
+
+    def of(self, B: int, desc: Optional[LayerDesc] = None):
+        raise QcfError("8-bit pages: qcf_page8_append and qcf_page8_attn take them")
+
+    def of_any(self, B: int, desc: Optional[LayerDesc] = None):
+        return PageCache.of(self, B, desc)
+
+
+def _page_strides(k: torch.Tensor):
+    """Distances of pages, slots and heads of [n_pages, page_size, H_kv, d], in elements."""
+    n_pages, page_size, n_kv, d = k.shape
+    # (the stride of an axis of one entry says nothing: one that fits takes its place)
+    head = k.stride(2) if n_kv > 1 else d
+    slot = k.stride(1) if page_size > 1 else n_kv * d
+    return k.stride(0) if n_pages > 1 else (page_size - 1) * slot + (n_kv - 1) * head + d, slot, head
+
+
+def page8_cache(k: torch.Tensor, v: torch.Tensor, scales: torch.Tensor, bounds: Optional[torch.Tensor], table: torch.Tensor,
+                dtype: torch.dtype) -> Page8Cache:
+    """k and v [n_pages, page_size, H_kv, d] of float8_e4m3fn, as in page_cache; scales [n_pages, H_kv, 2, page_size / 16] float32: those of
+    a page's keys and of its values; bounds [n_pages, H_kv, 2, d] of `dtype`, the type of the layer's rows, or None."""
+    if dtype not in _PAGE_DTYPES:
+        raise QcfError("layers of float32 or bfloat16 elements")
+    if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(3) != 1:
+        raise QcfError("k and v must have the shape [n_pages, page_size, H_kv, d], one type, equal strides and dense rows")
+    if k.dtype != torch.float8_e4m3fn:
+        raise QcfError("8-bit pages of float8_e4m3fn elements")
+    if not k.is_cuda or not v.is_cuda:
+        raise QcfError("tensors handed to the library must be CUDA tensors")
+    if table.dim() != 2 or table.dtype != torch.int32:
+        raise QcfError("table must be an int32 tensor [B, max_pages]")
+    if any(t is not None and t.device != k.device for t in (v, scales, bounds, table)):
+        raise QcfError("k, v, scales, bounds and table must be on one device")
+    n_pages, page_size, n_kv, d = k.shape
+    if scales.shape != (n_pages, n_kv, 2, page_size // 16) or scales.dtype != torch.float32:
+        raise QcfError("scales must have the shape [n_pages, H_kv, 2, page_size / 16] and the type float32")
+    if bounds is not None and (bounds.shape != (n_pages, n_kv, 2, d) or bounds.dtype != dtype):
+        raise QcfError("bounds must have the shape [n_pages, H_kv, 2, d] and the type of the layer")
+    _ptr(scales)
+    return Page8Cache(PageCacheDesc(k.data_ptr(), v.data_ptr(), _ptr(bounds), _ptr(table), *_page_strides(k), n_pages, page_size,
+                                    table.shape[1], 0), (k, v, bounds, table), scales, dtype)
 
 
 def page_cache(k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor], table: torch.Tensor) -> PageCache:
@@ -498,11 +572,7 @@ def page_cache(k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor],
     n_pages, page_size, n_kv, d = k.shape
     if bounds is not None and (bounds.shape != (n_pages, n_kv, 2, d) or bounds.dtype != k.dtype):
         raise QcfError("bounds must have the shape [n_pages, H_kv, 2, d] and the type of the keys")
-    # (the stride of an axis of one entry says nothing: one that fits takes its place)
-    head = k.stride(2) if n_kv > 1 else d
-    slot = k.stride(1) if page_size > 1 else n_kv * d
-    page = k.stride(0) if n_pages > 1 else (page_size - 1) * slot + (n_kv - 1) * head + d
-    return PageCache(PageCacheDesc(k.data_ptr(), v.data_ptr(), _ptr(bounds), _ptr(table), page, slot, head, n_pages, page_size,
+    return PageCache(PageCacheDesc(k.data_ptr(), v.data_ptr(), _ptr(bounds), _ptr(table), *_page_strides(k), n_pages, page_size,
                                    table.shape[1], 0), (k, v, bounds, table))
 
 
@@ -560,7 +630,7 @@ def qcf_page_select(desc: LayerDesc, cache: PageCache, B: int, n_q: int, q: torc
     """The pages that attention of n_q new rows of each request is cut down to, for each row and KV head."""
     if pages is not None and pages.shape[-1] != n_keep:
         raise QcfError(f"pages has room for {pages.shape[-1]} pages to a row, n_keep is {n_keep}")
-    ref, dev, rows = cache.of(B, desc), cache.device, B * n_q
+    ref, dev, rows = cache.of_any(B, desc), cache.device, B * n_q
     qp, sp = _dense("q", q, rows * desc.n_q_heads * cache.fits[1], cache.dtype, dev), _dense("seen", seen, rows, torch.int32, dev)
     pp = _dense("pages", pages, rows * cache.fits[0] * n_keep, torch.int32, dev)
     if workspace is None:
@@ -590,5 +660,96 @@ def qcf_page_attn(desc: LayerDesc, cache: PageCache, B: int, n_q: int, q: torch.
         workspace = _workspace(qcf_page_attn_workspace_bytes(desc, cache, B, n_q, n_keep), q.device)
     wp, wn = _page_ws(workspace, dev)
     status = (_lib or load_library()).qcf_page_attn(C.byref(desc), ref, B, n_q, qp, sp, pp, n_keep, op, zp, wp, wn, cache.stream())
+    if status:
+        _check(status)
+
+
+def _eight(cache: PageCache) -> int:
+    if cache.scales_ptr is None:
+        raise QcfError("8-bit pages wanted (page8_cache)")
+    return cache.scales_ptr
+
+
+def qcf_page8_append(desc: LayerDesc, cache: Page8Cache, B: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                     row_off: torch.Tensor, total_rows: int, lens: torch.Tensor, pos: Optional[torch.Tensor],
+                     q_out: Optional[torch.Tensor]) -> None:
+    """Rows of k and v behind what their requests hold (lens), keys and queries turned by pos, keys and values rounded to 8 bits."""
+    sp = _eight(cache)
+    ref, dev, H, Hkv = cache.of_any(B, desc), cache.device, desc.n_q_heads, cache.fits[0]
+    (qp, qs), (kp, ks), (vp, vs) = _rows(q, total_rows, H, cache), _rows(k, total_rows, Hkv, cache), _rows(v, total_rows, Hkv, cache)
+    status = (_lib or load_library()).qcf_page8_append(
+        C.byref(desc), ref, sp, B, qp, qs, kp, ks, vp, vs, _dense("row_off", row_off, B + 1, torch.int64, dev), total_rows,
+        _dense("lens", lens, B, torch.int32, dev), _dense("pos", pos, total_rows, torch.int32, dev),
+        _dense("q_out", q_out, total_rows * H * cache.fits[1], cache.dtype, dev), cache.stream())
+    if status:
+        _check(status)
+
+
+def qcf_page8_attn_workspace_bytes(desc: LayerDesc, cache: Page8Cache, B: int, n_q: int, n_keep: int) -> int:
+    return int(load_library().qcf_page8_attn_workspace_bytes(C.byref(desc), cache.ref, B, n_q, n_keep))
+
+
+def qcf_page8_attn(desc: LayerDesc, cache: Page8Cache, B: int, n_q: int, q: torch.Tensor, seen: torch.Tensor,
+                   pages: Optional[torch.Tensor], n_keep: int, o_out: torch.Tensor, lse_out: Optional[torch.Tensor],
+                   workspace: Optional[torch.Tensor] = None) -> None:
+    """Attention of n_q new rows of each request over all its 8-bit pages, or over those that `pages` lists for each row and KV head."""
+    if pages is not None and pages.shape[-1] != n_keep:
+        raise QcfError(f"pages lists {pages.shape[-1]} pages to a row, n_keep is {n_keep}")
+    sp = _eight(cache)
+    ref, dev, rows = cache.of_any(B, desc), cache.device, B * n_q
+    heads = rows * desc.n_q_heads
+    qp, np_ = _dense("q", q, heads * cache.fits[1], cache.dtype, dev), _dense("seen", seen, rows, torch.int32, dev)
+    pp = _dense("pages", pages, rows * cache.fits[0] * n_keep, torch.int32, dev)
+    op, zp = _dense("o_out", o_out, heads * cache.fits[1], cache.dtype, dev), _dense("lse_out", lse_out, heads, torch.float32, dev)
+    if workspace is None:
+        workspace = _workspace(qcf_page8_attn_workspace_bytes(desc, cache, B, n_q, n_keep), q.device)
+    wp, wn = _page_ws(workspace, dev)
+    status = (_lib or load_library()).qcf_page8_attn(C.byref(desc), ref, sp, B, n_q, qp, np_, pp, n_keep, op, zp, wp, wn, cache.stream())
+    if status:
+        _check(status)
+
+
+def _weights(name: str, t: Optional[torch.Tensor], B: int, cache: PageCache) -> Optional[int]:
+    """Pointer of [B or more, H_kv, tokens of a row of the table]."""
+    if t is not None and (t.dim() != 3 or tuple(t.shape[1:]) != (cache.fits[0], cache.tokens)):
+        raise QcfError(f"{name}: [B, {cache.fits[0]}, {cache.tokens}] wanted, got {tuple(t.shape)}")
+    return _dense(name, t, B * cache.fits[0] * cache.tokens, torch.float32, cache.device)
+
+
+def qcf_page_weigh(desc: LayerDesc, cache: PageCache, B: int, n_q: int, q: torch.Tensor, seen: torch.Tensor, lse: torch.Tensor,
+                   old: Optional[torch.Tensor], alpha: float, beta: float, weights: torch.Tensor) -> None:
+    """weights [B, H_kv, max_pages * page_size] = alpha * weights + beta * the attention weights that n_q new rows of each request give
+    its tokens (lse: what qcf_page_attn or qcf_page8_attn over all pages said); old [B]: tokens weighed before, None: all."""
+    ref, dev, rows = cache.of_any(B, desc), cache.device, B * n_q
+    qp = _dense("q", q, rows * desc.n_q_heads * cache.fits[1], cache.dtype, dev)
+    np_, zp = _dense("seen", seen, rows, torch.int32, dev), _dense("lse", lse, rows * desc.n_q_heads, torch.float32, dev)
+    op, wp = _dense("old", old, B, torch.int32, dev), _weights("weights", weights, B, cache)
+    status = (_lib or load_library()).qcf_page_weigh(C.byref(desc), ref, cache.scales_ptr, B, n_q, qp, np_, zp, op, alpha, beta, wp,
+                                                     cache.stream())
+    if status:
+        _check(status)
+
+
+def qcf_page_evict_workspace_bytes(desc: LayerDesc, cache: PageCache, B: int, n_keep: int) -> int:
+    return int(load_library().qcf_page_evict_workspace_bytes(C.byref(desc), cache.ref, B, n_keep))
+
+
+def qcf_page_evict(desc: LayerDesc, cache: PageCache, B: int, lens: torch.Tensor, weights: torch.Tensor, n_keep: int, n_first: int,
+                   n_last: int, to: PageCache, kept: torch.Tensor, to_weights: Optional[torch.Tensor], to_lens: torch.Tensor,
+                   workspace: Optional[torch.Tensor] = None) -> None:
+    """The first n_first, the last n_last and the heaviest other tokens of each KV head, n_keep in all, move into the pages of `to`; kept
+    [B, H_kv, n_keep] gets their numbers, to_weights their weights, to_lens (may be lens) how many they are."""
+    if kept.shape[-1] != n_keep:
+        raise QcfError(f"kept has room for {kept.shape[-1]} tokens to a head, n_keep is {n_keep}")
+    if to.device != cache.device or (to.scales_ptr is None) != (cache.scales_ptr is None):
+        raise QcfError("tokens move between pages of one type on one device")
+    ref, to_ref, dev = cache.of_any(B, desc), to.of_any(B, desc), cache.device
+    if workspace is None:
+        workspace = _workspace(qcf_page_evict_workspace_bytes(desc, cache, B, n_keep), lens.device)
+    wp, wn = _page_ws(workspace, dev)
+    status = (_lib or load_library()).qcf_page_evict(
+        C.byref(desc), ref, cache.scales_ptr, B, _dense("lens", lens, B, torch.int32, dev), _weights("weights", weights, B, cache), n_keep,
+        n_first, n_last, to_ref, to.scales_ptr, _dense("kept", kept, B * cache.fits[0] * n_keep, torch.int32, dev),
+        _weights("to_weights", to_weights, B, to), _dense("to_lens", to_lens, B, torch.int32, dev), wp, wn, cache.stream())
     if status:
         _check(status)

@@ -615,14 +615,16 @@ static qcf_status check_row_stride(const char* name, int64_t stride, int64_t row
   return QCF_OK;
 }
 
-qcf_status qcf_page_append(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, const void* q, int64_t q_stride,
-                           const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int64_t* row_off_dev,
-                           int64_t total_rows, const int32_t* len_dev, const int32_t* pos_dev, void* q_out, void* stream) {
+// what the appends check; *empty = nothing to do
+static qcf_status check_append(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, const void* q, int64_t q_stride,
+                               const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int64_t* row_off_dev,
+                               int64_t total_rows, const int32_t* len_dev, const int32_t* pos_dev, const void* q_out, bool* empty) {
   QCF_TRY(check_page_cache(desc, cache));
   if (B < 0 || total_rows < 0) return fail(QCF_ERR_INVALID_ARG, "negative size");
   if (B > 65535) return fail(QCF_ERR_UNSUPPORTED, "B %d > 65535", B);
   if (total_rows > kMaxRows) return fail(QCF_ERR_UNSUPPORTED, "too many rows");
-  if (B == 0 || total_rows == 0) return QCF_OK;
+  *empty = B == 0 || total_rows == 0;
+  if (*empty) return QCF_OK;
   QCF_TRY(check_page_pointers(cache, false));
   QCF_TRY(need_ptr(k, "k"));
   QCF_TRY(need_ptr(v, "v"));
@@ -639,6 +641,15 @@ qcf_status qcf_page_append(const qcf_layer_desc* desc, const qcf_page_cache* cac
     if (q == q_out && q_stride != (int64_t)desc->n_q_heads * desc->head_dim)
       return fail(QCF_ERR_INVALID_ARG, "q_out may be q only where its rows are dense");
   }
+  return QCF_OK;
+}
+
+qcf_status qcf_page_append(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, const void* q, int64_t q_stride,
+                           const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int64_t* row_off_dev,
+                           int64_t total_rows, const int32_t* len_dev, const int32_t* pos_dev, void* q_out, void* stream) {
+  bool empty = true;
+  QCF_TRY(check_append(desc, cache, B, q, q_stride, k, k_stride, v, v_stride, row_off_dev, total_rows, len_dev, pos_dev, q_out, &empty));
+  if (empty) return QCF_OK;
   return launch_page_append(*desc, *cache, B, q, q_stride, k, k_stride, v, v_stride, row_off_dev, total_rows, len_dev, pos_dev,
                             q_out, (hipStream_t)stream);
 }
@@ -685,21 +696,127 @@ size_t qcf_page_attn_workspace_bytes(const qcf_layer_desc* desc, const qcf_page_
   return page_attn_workspace(*desc, *cache, B, n_q, n_keep);
 }
 
-qcf_status qcf_page_attn(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, const void* q,
-                         const int32_t* seen_dev, const int32_t* pages, int32_t n_keep, void* o_out, float* lse_out,
-                         void* workspace, size_t workspace_bytes, void* stream) {
-  bool empty = true;
-  QCF_TRY(check_page_rows(desc, cache, B, n_q, n_keep, &empty));
+// what the attentions check; *empty = nothing to do
+static qcf_status check_page_attn(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, const void* q,
+                                  const int32_t* seen_dev, const int32_t* pages, int32_t n_keep, const void* o_out, const float* lse_out,
+                                  bool* empty) {
+  QCF_TRY(check_page_rows(desc, cache, B, n_q, n_keep, empty));
   if ((pages == nullptr) != (n_keep == 0)) return fail(QCF_ERR_INVALID_ARG, "pages and n_keep must both be given, or NULL and 0");
-  if (empty) return QCF_OK;
+  if (*empty) return QCF_OK;
   QCF_TRY(check_page_pointers(cache, false));
   QCF_TRY(need_ptr(q, "q"));
   QCF_TRY(need_idx_ptr(seen_dev, "seen_dev"));
   if (pages) QCF_TRY(need_idx_ptr(pages, "pages"));
   QCF_TRY(need_ptr(o_out, "o_out"));
   if (lse_out) QCF_TRY(need_idx_ptr(lse_out, "lse_out"));
+  return QCF_OK;
+}
+
+qcf_status qcf_page_attn(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, const void* q,
+                         const int32_t* seen_dev, const int32_t* pages, int32_t n_keep, void* o_out, float* lse_out,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  bool empty = true;
+  QCF_TRY(check_page_attn(desc, cache, B, n_q, q, seen_dev, pages, n_keep, o_out, lse_out, &empty));
+  if (empty) return QCF_OK;
   QCF_TRY(need_ws(workspace, workspace_bytes, page_attn_workspace(*desc, *cache, B, n_q, n_keep)));
   return launch_page_attn(*desc, *cache, B, n_q, q, seen_dev, pages, n_keep, o_out, lse_out, workspace, (hipStream_t)stream);
+}
+
+// ---- 8-bit pages ---------------------------------------------------------------------
+// `scales` of a cache, and what its codes ask of the strides
+static qcf_status check_eight(const qcf_page_cache* c, const float* scales, const char* name) {
+  QCF_TRY(need_idx_ptr(scales, name));
+  if ((c->page_stride | c->slot_stride | c->head_stride) & 15)
+    return fail(QCF_ERR_INVALID_ARG, "page, slot and head strides of 8-bit pages must be multiples of 16");
+  return QCF_OK;
+}
+
+qcf_status qcf_page8_append(const qcf_layer_desc* desc, const qcf_page_cache* cache, float* scales, int32_t B, const void* q,
+                            int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            const int64_t* row_off_dev, int64_t total_rows, const int32_t* len_dev, const int32_t* pos_dev, void* q_out,
+                            void* stream) {
+  bool empty = true;
+  QCF_TRY(check_append(desc, cache, B, q, q_stride, k, k_stride, v, v_stride, row_off_dev, total_rows, len_dev, pos_dev, q_out, &empty));
+  if (empty) return QCF_OK;
+  QCF_TRY(check_eight(cache, scales, "scales"));
+  return launch_page8_append(*desc, *cache, scales, B, q, q_stride, k, k_stride, v, v_stride, row_off_dev, total_rows, len_dev, pos_dev,
+                             q_out, (hipStream_t)stream);
+}
+
+size_t qcf_page8_attn_workspace_bytes(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, int32_t n_keep) {
+  bool empty = true;
+  if (check_page_rows(desc, cache, B, n_q, n_keep, &empty) != QCF_OK || empty) return 0;
+  return page8_attn_workspace(*desc, *cache, B, n_q, n_keep);
+}
+
+qcf_status qcf_page8_attn(const qcf_layer_desc* desc, const qcf_page_cache* cache, const float* scales, int32_t B, int32_t n_q,
+                          const void* q, const int32_t* seen_dev, const int32_t* pages, int32_t n_keep, void* o_out, float* lse_out,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  bool empty = true;
+  QCF_TRY(check_page_attn(desc, cache, B, n_q, q, seen_dev, pages, n_keep, o_out, lse_out, &empty));
+  if (empty) return QCF_OK;
+  QCF_TRY(check_eight(cache, scales, "scales"));
+  QCF_TRY(need_ws(workspace, workspace_bytes, page8_attn_workspace(*desc, *cache, B, n_q, n_keep)));
+  return launch_page8_attn(*desc, *cache, scales, B, n_q, q, seen_dev, pages, n_keep, o_out, lse_out, workspace, (hipStream_t)stream);
+}
+
+// ---- fewer tokens -----------------------------------------------------------------------
+qcf_status qcf_page_weigh(const qcf_layer_desc* desc, const qcf_page_cache* cache, const float* scales, int32_t B, int32_t n_q,
+                          const void* q, const int32_t* seen_dev, const float* lse, const int32_t* old_dev, float alpha, float beta,
+                          float* weights, void* stream) {
+  bool empty = true;
+  QCF_TRY(check_page_rows(desc, cache, B, n_q, 0, &empty));
+  if (!std::isfinite(alpha) || !std::isfinite(beta)) return fail(QCF_ERR_INVALID_ARG, "alpha and beta must be finite");
+  if (empty) return QCF_OK;
+  QCF_TRY(check_page_pointers(cache, false));
+  if (scales) QCF_TRY(check_eight(cache, scales, "scales"));
+  QCF_TRY(need_ptr(q, "q"));
+  QCF_TRY(need_idx_ptr(seen_dev, "seen_dev"));
+  QCF_TRY(need_idx_ptr(lse, "lse"));
+  if (old_dev) QCF_TRY(need_idx_ptr(old_dev, "old_dev"));
+  QCF_TRY(need_ptr(weights, "weights"));
+  return launch_page_weigh(*desc, *cache, scales, B, n_q, q, seen_dev, lse, old_dev, alpha, beta, weights, (hipStream_t)stream);
+}
+
+static qcf_status check_evict(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_keep) {
+  QCF_TRY(check_page_cache(desc, cache));
+  if (B < 0) return fail(QCF_ERR_INVALID_ARG, "negative size");
+  if (B > 65535) return fail(QCF_ERR_UNSUPPORTED, "B %d > 65535", B);
+  if (n_keep <= 0) return fail(QCF_ERR_INVALID_ARG, "n_keep %d must be positive", n_keep);
+  if (n_keep > kMaxRows) return fail(QCF_ERR_UNSUPPORTED, "n_keep %d: more than 2^30 tokens", n_keep);
+  return QCF_OK;
+}
+
+size_t qcf_page_evict_workspace_bytes(const qcf_layer_desc*, const qcf_page_cache*, int32_t, int32_t) { return 0; }
+
+qcf_status qcf_page_evict(const qcf_layer_desc* desc, const qcf_page_cache* cache, const float* scales, int32_t B,
+                          const int32_t* len_dev, const float* weights, int32_t n_keep, int32_t n_first, int32_t n_last,
+                          const qcf_page_cache* to, float* to_scales, int32_t* kept, float* to_weights, int32_t* to_len_dev,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  (void)workspace; (void)workspace_bytes;
+  QCF_TRY(check_evict(desc, cache, B, n_keep));
+  QCF_TRY(check_page_cache(desc, to));
+  if (n_first < 0 || n_last < 0) return fail(QCF_ERR_INVALID_ARG, "negative size");
+  if ((int64_t)n_first + n_last > n_keep)
+    return fail(QCF_ERR_INVALID_ARG, "n_first %d + n_last %d > n_keep %d", n_first, n_last, n_keep);
+  if (n_keep > (int64_t)to->max_pages * to->page_size)
+    return fail(QCF_ERR_INVALID_ARG, "n_keep %d, room for %lld tokens in the new table", n_keep, (long long)to->max_pages * to->page_size);
+  if ((scales == nullptr) != (to_scales == nullptr)) return fail(QCF_ERR_INVALID_ARG, "scales and to_scales must both be given, or both be NULL");
+  if (B == 0) return QCF_OK;
+  QCF_TRY(check_page_pointers(cache, false));
+  QCF_TRY(check_page_pointers(to, false));
+  if (scales) {
+    QCF_TRY(check_eight(cache, scales, "scales"));
+    QCF_TRY(check_eight(to, to_scales, "to_scales"));
+  }
+  QCF_TRY(need_idx_ptr(len_dev, "len_dev"));
+  QCF_TRY(need_ptr(weights, "weights"));
+  QCF_TRY(need_idx_ptr(kept, "kept"));
+  if (to_weights) QCF_TRY(need_ptr(to_weights, "to_weights"));
+  if (to_weights == weights) return fail(QCF_ERR_INVALID_ARG, "to_weights must be other memory than weights");
+  QCF_TRY(need_idx_ptr(to_len_dev, "to_len_dev"));
+  return launch_page_evict(*desc, *cache, scales, B, len_dev, weights, n_keep, n_first, n_last, *to, to_scales, kept, to_weights,
+                           to_len_dev, (hipStream_t)stream);
 }
 
 }  // extern "C"

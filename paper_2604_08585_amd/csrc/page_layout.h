@@ -24,6 +24,9 @@ constexpr int64_t kThreadsAtMost = 0xffffffff;               // of a launch: a d
 constexpr int kTopThreads = 1024;         // of a workgroup that chooses a row's pages
 constexpr int kShared = 16 << 20;         // bytes of keys and values from which on two tiles of rows share a workgroup
 
+// Bytes of an element of the layer; the pages' own may be smaller.
+inline int layer_elem(const qcf_layer_desc& L) { return L.dtype == QCF_DTYPE_BF16 ? 2 : 4; }
+
 // Grains of a range: a tile of 32 tokens (bf16) or 16 for every wave.
 inline int least_range(const qcf_layer_desc& L) { return L.dtype == QCF_DTYPE_BF16 ? 4 : 2; }
 
@@ -52,13 +55,14 @@ struct Division {
 // 13.1, 2048 16.3 and 11.1.  In float32, heads of 64: 2 of 512 10.8 and 9.7, 4 of up to 512 10.9 and 12.3, 1024 15.9 and 10.5.  Over eight
 // shapes, 1 to 64 requests and 256 to 8192 tokens the rule is 0.5 % behind the better of the two on average (272 KB in place of 290:
 // 0.6 %, 350: 0.9 %); at its border it takes the worse one by up to 11 % (19 % in float32), and by 25 % for 2048 workgroups of up to 256 tokens.
-inline bool takes_whole(const qcf_layer_desc& L, int64_t workgroups, int64_t longest) {
-  const int64_t bytes = longest * 2 * L.head_dim * (L.dtype == QCF_DTYPE_BF16 ? 2 : 4);
+inline bool takes_whole(const qcf_layer_desc& L, int64_t workgroups, int64_t longest, int elem) {
+  const int64_t bytes = longest * 2 * L.head_dim * elem;
   const int64_t alone = std::max<int64_t>(30, 200 - workgroups * 256 / compute_unit_count());      // of 200
   return bytes * alone <= (int64_t)((L.dtype == QCF_DTYPE_BF16 ? 290 : 240) << 10) * 200;
 }
 
-inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, int32_t n_keep) {
+// elem: bytes of a stored element
+inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, int32_t n_keep, int elem) {
   Division d;
   const int G = L.n_q_heads / L.n_kv_heads;
   d.contexts = n_keep ? B * n_q : B;
@@ -68,7 +72,7 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   // 4096 tokens 14.6 and 12.5, of 16384 18.9 and 19.5; 8 of up to 1024 15.9 and 13.5, of up to 4096 18.9 and 23.5.  32 / 1 heads: one
   // request of 16384 tokens 18.1 and 16.0, 8 of up to 4096 16.6 and 16.4, 64 of up to 1024 19.2 and 16.6, of up to 4096 32.6 and 43.7.
   const int64_t longest = (int64_t)(n_keep && n_keep < c.max_pages ? n_keep : c.max_pages) * c.page_size;
-  const double read = (double)d.contexts * (double)longest * L.n_kv_heads * 2 * L.head_dim * (L.dtype == QCF_DTYPE_BF16 ? 2 : 4);
+  const double read = (double)d.contexts * (double)longest * L.n_kv_heads * 2 * L.head_dim * elem;
   d.row_tiles = d.rows > 16 && read > kShared ? 2 : 1;
   d.row_blocks = (d.rows + 16 * d.row_tiles - 1) / (16 * d.row_tiles);
   d.inner = L.n_kv_heads * d.row_blocks;
@@ -79,10 +83,13 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   // (four drafts of 8 requests of 2K to 6K tokens, 32 rows, before later steps, which brought 47 to 44 us: 53.0 us without, 48.1 with 12,
   // 47.1 with 18, 50.0 with 28; two workgroups on a compute unit cover for each other, 0 to 9 are the same there)
   d.pad = d.contexts > 1 && d.row_tiles == 2 ? 16 : 0;
-  d.whole = d.row_tiles == 1 && takes_whole(L, (int64_t)d.contexts * d.inner, longest);
+  d.whole = d.row_tiles == 1 && takes_whole(L, (int64_t)d.contexts * d.inner, longest, elem);
   const int64_t ranges = (d.most + d.least - 1) / d.least;
   if (d.slots > ranges) d.slots = (int)ranges;
   return d;
+}
+inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, int32_t n_keep) {
+  return divide(L, c, B, n_q, n_keep, layer_elem(L));
 }
 
 // Grains of a context and of a range, where there are `total` of them in all.

@@ -1,0 +1,176 @@
+// What the tokens of a cache in pages get of their requests' attention, added up step by step.
+//
+// The softmax's sums are known (lse), so a token's weights need its logits and nothing of other tokens: one pass over the keys.  A wave
+// takes 32 tokens (16 in float32) at a time as in the attention, whose division of the contexts this has too; a lane owns a row and four
+// tokens of each 16, the sum over the rows goes over the 16 lanes of a quad.  Bound by memory: the keys, and 8 bytes of weights to a token
+// and KV head.
+#include "page_walk.h"
+
+namespace qcf {
+namespace {
+
+struct WeighArgs {
+  PageAttnArgs a;
+  const float* lse;
+  const int32_t* old;
+  float alpha, beta;
+  float* weights;
+  int64_t stride;                                        // tokens of a head's weights
+  int row_blocks;
+};
+
+template <typename T, int D, int RT, bool EIGHT>
+struct Weigher : Walk<T, D, RT, kSeveral, pages::kWaves, EIGHT> {
+  typedef Walk<T, D, RT, kSeveral, pages::kWaves, EIGHT> W;
+  typedef typename W::Tile Tile;
+  static constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.925963033500e-8f;
+  const WeighArgs& w_;
+  float ref[RT], ref_low[RT];                            // lse in powers of two, as two floats
+  floatx4* out;                                          // weights of token 0 of this lane's four
+  int known;                                             // tokens weighed before
+
+  __device__ __forceinline__ Weigher(const WeighArgs& args, int lane, int g) : W(args.a, lane, g), w_(args) {}
+
+  __device__ __forceinline__ void prepare(int context, int row0, int64_t begin, int64_t end) {
+    this->start(context, row0, begin, end);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const int row = this->row_of(r);
+      const bool there = row < this->a.rows;
+      const int i = there ? row / this->a.G : 0;
+      const float l = there ? w_.lse[((int64_t)context * this->a.n_q + i) * this->a.H + this->g * this->a.G + (row - i * this->a.G)] : 0.f;
+      ref[r] = l * kLog2e;
+      ref_low[r] = __builtin_isfinite(ref[r]) ? __builtin_fmaf(l, kLog2e, -ref[r]) + l * kLog2eLow : 0.f;
+    }
+    known = w_.old ? w_.old[context] : 0x7fffffff;
+    out = reinterpret_cast<floatx4*>(w_.weights + ((int64_t)context * this->a.Hkv + this->g) * w_.stride) + this->quad + 4 * this->col;
+  }
+
+  // (lanes 0 and 1 of each 16 have the weights of a tile's parts)
+  __device__ __forceinline__ bool mine(int64_t at) const { return this->col < W::kSub && at + 16 * this->col < this->lim_hi; }
+  __device__ __forceinline__ void load(Tile& t, floatx4& was, int64_t at, bool first) {
+    const typename W::Where r = this->find(at);
+    this->load_keys(t, r);
+#pragma unroll
+    for (int h = 0; h < W::kSub; ++h) t.base[h] = r.base[h];
+    was = floatx4{0.f, 0.f, 0.f, 0.f};
+    if ((!first || w_.alpha != 0.f) && mine(at)) was = out[at / 4];
+  }
+  __device__ __forceinline__ void weigh(const Tile& t, floatx4 was, int64_t at, bool first) {
+    float s[RT][W::kS], sum[W::kS];
+    this->logits(t, s);
+#pragma unroll
+    for (int i = 0; i < W::kS; ++i) {
+      sum[i] = 0.f;
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const float x = __builtin_fmaf(s[r][i], this->a.scale, -ref[r]) + __builtin_fmaf(s[r][i], this->a.scale_low, -ref_low[r]);
+        const bool ok = t.base[i >> 2] >= 0 && this->token(t, i) < this->lim[r];
+        sum[i] += ok ? __builtin_amdgcn_exp2f(x) : 0.f;
+      }
+      sum[i] = row_sum(sum[i]);
+    }
+    if (!mine(at)) return;
+    const int64_t token = at + 16 * this->col + 4 * this->quad;
+    floatx4 now;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float mine = sum[i];
+#pragma unroll
+      for (int h = 1; h < W::kSub; ++h) mine = this->col == h ? sum[4 * h + i] : mine;
+      const float before = !first ? was[i] : token + i < known && w_.alpha != 0.f ? w_.alpha * was[i] : 0.f;
+      now[i] = before + w_.beta * mine;
+      if (now[i] != now[i]) now[i] = NAN;
+    }
+    if (token + 4 <= this->lim_hi) {
+      out[at / 4] = now;
+    } else {
+      float* w = reinterpret_cast<float*>(out + at / 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (token + i < this->lim_hi) w[i] = now[i];
+    }
+  }
+  __device__ __forceinline__ void run(int64_t at, bool first) {
+    if (at >= this->end) return;
+    Tile t0, t1;
+    floatx4 w0, w1;
+    load(t0, w0, at, first);
+    while (true) {
+      int64_t next = at + W::kStep;
+      if (next < this->end) load(t1, w1, next, first);
+      weigh(t0, w0, at, first);
+      if (next >= this->end) return;
+      at = next + W::kStep;
+      if (at < this->end) load(t0, w0, at, first);
+      weigh(t1, w1, next, first);
+      if (at >= this->end) return;
+    }
+  }
+};
+
+template <typename T, int D, int RT, bool EIGHT>
+__global__ __launch_bounds__(64 * pages::kWaves, 2) void page_weigh_kernel(WeighArgs args) {
+  typedef Weigher<T, D, RT, EIGHT> W;
+  const PageAttnArgs& a = args.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t r = blockIdx.x / a.inner;
+  const int g = (int)(blockIdx.x - r * a.inner);
+  W w(args, lane, g);
+  const Contexts all = contexts_of(a, lane);
+  const int64_t from = r * all.range, to = from + all.range;
+  Place here = place_of<false>(a, all, from, 0, lane);
+  if (here.x < 0) return;
+  while (true) {
+    const int64_t g0 = max(from - here.start, (int64_t)0), g1 = min(to - here.start, here.grains);
+    if (g1 > g0) {
+      const int64_t tokens = here.x < 64 ? from_lane(all.tokens, here.x) : context_tokens(a, here.x);
+      const int64_t begin = g0 * pages::kGrain, end = g1 == here.grains ? tokens : g1 * pages::kGrain;
+      // (each wave's tokens are its own, and so are their weights: the second block of rows finds what the first one stored)
+      for (int block = 0; block < args.row_blocks; ++block) {
+        w.prepare(here.x, block * 16 * RT, begin, end);
+        w.lim_hi = (int)tokens;                          // (of all rows)
+        w.run(begin + wave * W::W::kTokens, block == 0);
+      }
+    }
+    here.start += here.grains + all.pad;
+    if (here.start >= to || all.apart || ++here.x >= a.contexts) return;
+    here.grains = here.x < 64 ? (int64_t)from_lane(all.grains, here.x) : pages::grains_of(context_tokens(a, here.x));
+  }
+}
+
+}  // namespace
+
+qcf_status launch_page_weigh(const qcf_layer_desc& L, const qcf_page_cache& c, const float* scales, int32_t B, int32_t n_q, const void* q,
+                             const int32_t* seen, const float* lse, const int32_t* old, float alpha, float beta, float* weights,
+                             hipStream_t st) {
+  WeighArgs w;
+  const int rows = n_q * (L.n_q_heads / L.n_kv_heads), row_tiles = rows > 16 ? 2 : 1;
+  fill_args(w.a, L, c, scales, n_q, q, seen);
+  w.a.contexts = B;
+  w.a.rows = rows;
+  w.a.inner = L.n_kv_heads;
+  w.a.least = pages::least_range(L);
+  w.a.pad = 0;
+  w.lse = lse; w.old = old; w.alpha = alpha; w.beta = beta;
+  w.weights = weights;
+  w.stride = (int64_t)c.max_pages * c.page_size;
+  w.row_blocks = (rows + 16 * row_tiles - 1) / (16 * row_tiles);
+  const int64_t ranges = ((int64_t)B * ((w.stride + pages::kGrain - 1) / pages::kGrain) + w.a.least - 1) / w.a.least;
+  w.a.slots = (int)std::min<int64_t>(ranges, std::max(1, 2 * compute_unit_count() / L.n_kv_heads));
+  const dim3 grid((unsigned)((int64_t)w.a.slots * w.a.inner)), block(64 * pages::kWaves);
+#define QCF_LAUNCH(T, D, RT, EIGHT) page_weigh_kernel<T, D, RT, EIGHT><<<grid, block, 0, st>>>(w)
+#define QCF_ROWS(T, D, EIGHT) do { if (row_tiles == 1) QCF_LAUNCH(T, D, 1, EIGHT); else QCF_LAUNCH(T, D, 2, EIGHT); } while (0)
+#define QCF_PAGES(T, D) do { if (scales) QCF_ROWS(T, D, true); else QCF_ROWS(T, D, false); } while (0)
+  if (L.dtype == QCF_DTYPE_BF16) {
+    if (L.head_dim == 128) QCF_PAGES(bf16_t, 128); else QCF_PAGES(bf16_t, 64);
+  } else {
+    if (L.head_dim == 128) QCF_PAGES(float, 128); else QCF_PAGES(float, 64);
+  }
+#undef QCF_PAGES
+#undef QCF_ROWS
+#undef QCF_LAUNCH
+  return check_launch("page weights");
+}
+
+}  // namespace qcf

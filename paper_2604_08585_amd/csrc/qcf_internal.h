@@ -14,6 +14,8 @@
 #include "qcf_anchors.h"
 #include "qcf_fuse.h"
 #include "qcf_pages.h"
+#include "qcf_pages8.h"
+#include "qcf_evict.h"
 
 namespace qcf {
 
@@ -361,5 +363,22 @@ size_t page_attn_workspace(const qcf_layer_desc& L, const qcf_page_cache& c, int
 qcf_status launch_page_attn(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, const void* q,
                             const int32_t* seen, const int32_t* pages, int32_t n_keep, void* o, float* lse, void* ws,
                             hipStream_t st);
+
+// the same over 8-bit pages
+qcf_status launch_page8_append(const qcf_layer_desc& L, const qcf_page_cache& c, float* scales, int32_t B, const void* q,
+                               int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                               const int64_t* row_off, int64_t total_rows, const int32_t* len, const int32_t* pos, void* q_out,
+                               hipStream_t st);
+size_t page8_attn_workspace(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int32_t n_q, int32_t n_keep);
+qcf_status launch_page8_attn(const qcf_layer_desc& L, const qcf_page_cache& c, const float* scales, int32_t B, int32_t n_q,
+                             const void* q, const int32_t* seen, const int32_t* pages, int32_t n_keep, void* o, float* lse, void* ws,
+                             hipStream_t st);
+// attention weights of tokens, and the tokens that stay; scales NULL: pages of the layer's type
+qcf_status launch_page_weigh(const qcf_layer_desc& L, const qcf_page_cache& c, const float* scales, int32_t B, int32_t n_q,
+                             const void* q, const int32_t* seen, const float* lse, const int32_t* old, float alpha, float beta,
+                             float* weights, hipStream_t st);
+qcf_status launch_page_evict(const qcf_layer_desc& L, const qcf_page_cache& c, const float* scales, int32_t B, const int32_t* len,
+                             const float* weights, int32_t n_keep, int32_t n_first, int32_t n_last, const qcf_page_cache& to,
+                             float* to_scales, int32_t* kept, float* to_weights, int32_t* to_len, hipStream_t st);
 
 }  // namespace qcf

@@ -1,0 +1,345 @@
+"""GPU parity of weights and eviction (qcf_evict.h) against the float64 oracle on identical inputs.
+
+Tolerances, derived.  A weight exp(z - lse): z of d products in 32 bits is off by at most eps = (d + 5) 2^-24 sum |q k| / sqrt(d), z - lse by
+2^-23 (1 + |z - lse|) more, the exponential by 2^-22: relative to each weight.  The sum of R weights adds R 2^-24, alpha w + beta s two
+roundings, 2^-23.  Kept tokens, lengths, moved rows and moved weights are equal; in 8 bits the codes are the oracle's.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import qcf_oracle as orc
+from paper_2604_08585_amd import binding as qb
+from gpu_pages8 import E4M3, Paged8, normal, say, shape
+from gpu_util import DEV, i32, i64, to_np
+from test_gpu_pages import Paged
+
+pytestmark = pytest.mark.gpu
+
+
+def _paged(eight, *a, **kw):
+    return Paged8(*a, **kw) if eight else Paged(*a, **kw)
+
+
+def _values(p):
+    return p.values() if isinstance(p, Paged8) else (np.asarray(p.k, dtype=np.float64), np.asarray(p.v, dtype=np.float64))
+
+
+def _attn(p):
+    return qb.qcf_page8_attn if isinstance(p, Paged8) else qb.qcf_page_attn
+
+
+# ------------------------------------------------------------------ weights
+
+WEIGHTS = [
+    # dtype, H, Hkv, D, page, order, seen [B][n_q], old
+    ("bf16", 32, 8, 128, 16, "token", [[731]], [730]),
+    ("bf16", 8, 2, 128, 16, "head", [[1], [2], [15], [16], [17], [0], [31], [32], [33]], [0, 2, 9, 16, 3, 0, 40, -1, 32]),
+    ("bf16", 64, 8, 128, 64, "token", [[97, 98, 99, 100], [61, 62, 0, 0], [1, 2, 3, 4]], [96, 60, 0]),
+    ("bf16", 16, 1, 128, 16, "token", [[64 + i for i in range(16)], [0] * 16], [63, 5]),        # 256 rows: several blocks of them
+    ("bf16", 48, 2, 64, 128, "head", [[200], [129]], None),
+    ("bf16", 6, 2, 64, 256, "token", [[500, 3, 0, 257]], [499]),
+    ("f32", 4, 2, 64, 32, "token", [[1], [33], [600], [0], [64]], [0, 32, 599, 0, 63]),
+    ("f32", 20, 1, 64, 16, "head", [[40, 41, 42, 43, 44]], [39]),
+    ("f32", 6, 2, 128, 256, "token", [[700]], [0]),
+    ("bf16", 8, 8, 128, 16, "token", [[97 * i % 700] for i in range(70)], [5 * i for i in range(70)]),
+]
+
+
+def _weigh(p, q, seen, lse, old, alpha, beta, w):
+    qb.qcf_page_weigh(p.desc, p.cache, len(seen), seen.shape[1], torch.from_numpy(q).to(device=DEV, dtype=p.dt), i32(seen), lse,
+                      None if old is None else i32(old), alpha, beta, w)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("case", WEIGHTS)
+def test_weights(case, eight):
+    dtype, H, Hkv, D, page, order, seen, old = case
+    rng = np.random.default_rng(41)
+    seen = np.array(seen, dtype=np.int32)
+    B, n_q = seen.shape
+    p = _paged(eight, rng, shape(H, Hkv, D, dtype), page, np.maximum(seen.max(1), 1).tolist(), order)
+    say("weigh", dtype, H, Hkv, D, "page", page, order, "8 bits" if eight else "", "seen", seen.tolist() if seen.size < 40 else seen.shape)
+    q = normal(rng, (B, n_q, H, D), dtype, 1.5)
+    k, _ = _values(p)
+    lse = np.full((B, n_q, H), -np.inf)
+    for b in range(B):
+        for i in range(n_q):
+            lse[b, i] = orc.page_attn(q[b, i], k, k, p.table[b], seen[b, i])[1]
+    lse = lse.astype(np.float32)
+    tokens = p.table.shape[1] * page
+    was = rng.random((B, Hkv, tokens)).astype(np.float32)
+    for alpha, beta in [(0.75, 2.0), (0.0, 1.0)]:
+        start = was if alpha else np.full_like(was, np.nan)
+        w = torch.from_numpy(start).to(DEV)
+        _weigh(p, q, seen, torch.from_numpy(lse).to(DEV), old, alpha, beta, w)
+        got = w.double().cpu().numpy()
+        for b in range(B):
+            most = max(seen[b].max(), 0)
+            ref = orc.page_weigh(np.nan_to_num(start[b]), q[b], k, p.table[b], seen[b], lse[b].astype(np.float64), 10 ** 9 if old is None else old[b], alpha, beta)
+            terms = np.abs(k[p.table[b, :-(-most // page)]]).sum(-1).max() * np.abs(q[b]).max() if most else 0.0
+            x = max(1.0, np.abs(lse[b][np.isfinite(lse[b])]).max() * 2 if np.isfinite(lse[b]).any() else 1.0)
+            rel = (D + 5) * 2.0 ** -24 * terms / math.sqrt(D) + 2.0 ** -22 * (1 + x) + 2.0 ** -22 + n_q * H // Hkv * 2.0 ** -24 + 2.0 ** -22
+            assert np.all(np.abs(got[b, :, :most] - ref[:, :most]) <= rel * ref[:, :most]), (b, np.abs(got[b, :, :most] / ref[:, :most] - 1).max(), rel)
+            assert np.array_equal(got[b, :, most:], start[b, :, most:], equal_nan=True), b
+
+
+def test_weights_of_one_step_sum_to_the_heads_and_do_not_read_what_is_not_seen():
+    """NaN in keys and scales that no row sees, pages that are not there, lse from the attention itself."""
+    for eight in (False, True):
+        rng = np.random.default_rng(42)
+        p = _paged(eight, rng, shape(12, 2, 128, "bf16"), 16, [75, 33, 20], width=12)
+        pools = p.codes if eight else [p.k, p.v]
+        free = np.setdiff1d(np.arange(len(pools[0])), p.table)
+        pools[0][free] = np.nan
+        pools[0][p.table[0, 4], 11:] = np.nan
+        p.table[1, 1] = -1
+        p.upload(bounds=False)
+        q = torch.from_numpy(normal(rng, (3, 2, 12, 128), "bf16")).to(device=DEV, dtype=p.dt)
+        seen = i32([[74, 75], [32, 33], [0, 0]])
+        o, lse = torch.empty_like(q), torch.empty(3, 2, 12, device=DEV)
+        _attn(p)(p.desc, p.cache, 3, 2, q, seen, None, 0, o, lse)
+        w = torch.full((3, 2, 12 * 16), math.nan, device=DEV)
+        qb.qcf_page_weigh(p.desc, p.cache, 3, 2, q, seen, lse, i32([0, 0, 0]), 1.0, 1.0, w)
+        torch.cuda.synchronize()
+        w = w.cpu()
+        assert (w[0, :, :75].sum(1) - 12.0).abs().max() < 1e-3 and (w[1, :, :16].sum(1) + w[1, :, 32] - 12.0).abs().max() < 1e-3
+        assert (w[1, :, 16:32] == 0).all() and torch.isnan(w[0, :, 75:]).all() and torch.isnan(w[2]).all()
+
+
+def test_a_weight_that_is_not_a_number_is_the_positive_one():
+    rng = np.random.default_rng(43)
+    p = Paged(rng, shape(4, 2, 64, "f32"), 16, [20])
+    p.k[p.table[0, 0], 5, 1] = np.nan
+    p.upload()
+    q = torch.ones(1, 1, 4, 64, device=DEV)
+    w = torch.ones(1, 2, 32, device=DEV)
+    qb.qcf_page_weigh(p.desc, p.cache, 1, 1, -q, i32([[20]]), torch.full((1, 1, 4), 3.0, device=DEV), None, 1.0, -1.0, w)
+    torch.cuda.synchronize()
+    assert w.cpu().isnan().nonzero().tolist() == [[0, 1, 5]]
+    assert (w.view(torch.int32)[0, 1, 5] > 0).item()
+
+
+# ------------------------------------------------------------------ eviction
+
+EVICTIONS = [
+    # dtype, H, Hkv, D, page, new page, order, lens, keep, first, last
+    ("bf16", 8, 2, 128, 16, 16, "token", [200, 47, 48, 49, 0, 1, 16], 48, 4, 8),
+    ("bf16", 8, 8, 128, 64, 16, "head", [700, 100, 64], 101, 0, 0),
+    ("bf16", 4, 2, 64, 16, 256, "token", [900, 257, 600], 300, 1, 100),
+    ("bf16", 4, 1, 64, 128, 128, "head", [1000], 500, 0, 500),
+    ("f32", 4, 2, 64, 32, 32, "token", [100, 33, 5], 33, 2, 2),
+    ("f32", 8, 4, 128, 16, 64, "head", [333, 64, 63], 64, 32, 32),
+    ("f32", 2, 2, 128, 256, 16, "token", [600], 1, 0, 0),
+    ("bf16", 2, 1, 128, 16, 16, "token", [40000], 9000, 4, 64),
+    ("bf16", 32, 8, 128, 16, 16, "token", [100 + 13 * i for i in range(40)], 128, 1, 16),
+]
+
+
+def _evict(p, to, lens, w, keep, first, last, to_len=None):
+    B, Hkv = len(lens), p.sh.n_kv_heads
+    kept = torch.full((B, Hkv, keep), 77, dtype=torch.int32, device=DEV)
+    to_w = torch.full((B, Hkv, to.tokens), 7.0, device=DEV)
+    n = i32(lens)
+    to_len = n if to_len is None else to_len
+    qb.qcf_page_evict(p.desc, p.cache, B, n, w, keep, first, last, to, kept, to_w, to_len)
+    torch.cuda.synchronize()
+    return kept, to_w, to_len
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("case", EVICTIONS)
+def test_eviction(case, eight):
+    dtype, H, Hkv, D, page, new_page, order, lens, keep, first, last = case
+    rng = np.random.default_rng(44)
+    B = len(lens)
+    p = _paged(eight, rng, shape(H, Hkv, D, dtype), page, lens, order)
+    t = _paged(eight, rng, shape(H, Hkv, D, dtype), new_page, [keep] * B, order)              # other pools, for pages of another size
+    say("evict", dtype, H, Hkv, D, page, "->", new_page, "8 bits" if eight else "", "lens", lens[:8], "keep", keep)
+    tokens = p.table.shape[1] * page
+    w = np.exp(2 * rng.standard_normal((B, Hkv, tokens))).astype(np.float32)
+    w[rng.random(w.shape) < 0.3] = 0.0                                                        # ties
+    w[0, 0, 3:5] = np.nan
+    before = t.got() if eight else (to_np(t.kd), to_np(t.vd))
+    b0 = to_np(t.bd)
+    kept, to_w, to_len = _evict(p, t.cache, lens, torch.from_numpy(w).to(DEV), keep, first, last)
+    k, v = _values(p)
+    got = t.got() if eight else (to_np(t.kd), to_np(t.vd))
+    for b in range(B):
+        n = min(lens[b], keep)
+        assert to_len[b].item() == n
+        want = orc.page_evict(w[b], lens[b], keep, first, last)
+        assert np.array_equal(kept[b].cpu().numpy(), want), b
+        for g in range(Hkv):
+            tok = want[g, :n]
+            assert np.array_equal(to_w[b, g, :n].cpu().numpy(), w[b, g, tok], equal_nan=True) and (to_w[b, g, n:] == 7.0).all()
+            src, slot = p.table[b, tok // page], tok % page
+            j = np.arange(n)
+            dst, at = t.table[b, j // new_page], j % new_page
+            for which, x in enumerate((k, v)):
+                rows = x[src, slot, g]
+                if eight:
+                    s = np.array([orc.page8_scale(rows[i:i + 16]) for i in range(0, n, 16)])
+                    assert np.array_equal(got[2][dst[::16], g, which, at[::16] // 16], s)
+                    rows = orc.e4m3(rows / np.repeat(s, 16)[:n, None]) if n else rows
+                assert np.array_equal(got[which][dst, at, g], rows), (b, g, which)
+            stored = got[0][dst, at, g] * (np.repeat(s0, 16)[:n, None] if eight and (s0 := got[2][dst[::16], g, 0, at[::16] // 16]) is not None else 1.0)
+            for page_of in range(-(-n // new_page)):
+                mine = stored[page_of * new_page:(page_of + 1) * new_page]
+                bound = to_np(t.bd)[t.table[b, page_of], g]
+                assert np.array_equal(bound, np.stack([mine.min(0), mine.max(0)])), (b, g, page_of)
+        # slots behind the tokens, and pages that got none, are as they were
+        for j in range(n, t.table.shape[1] * new_page):
+            page_id, at = t.table[b, j // new_page], j % new_page
+            for which in range(2):
+                assert np.array_equal(got[which][page_id, at], before[which][page_id, at])
+        for x in t.table[b, -(-n // new_page):]:
+            assert np.array_equal(to_np(t.bd)[x], b0[x])
+
+
+def test_eviction_within_one_pool_and_what_is_not_there():
+    """A second table of the same pools; pages of the new table that are missing drop what they should get, missing pages give zeros."""
+    for eight in (False, True):
+        rng = np.random.default_rng(45)
+        p = _paged(eight, rng, shape(4, 2, 128, "bf16"), 16, [100, 60], spare=8)
+        free = np.setdiff1d(np.arange(len(p.bounds)), p.table)
+        table = np.array([free[:3], [free[3], -1, free[4]]], dtype=np.int32)
+        p.table[0, 2] = -4
+        p.upload(bounds=False)
+        td = i32(table)
+        to = qb.page8_cache(p.kd, p.vd, p.sd, None, td, p.dt) if eight else qb.page_cache(p.kd, p.vd, None, td)
+        w = rng.random((2, 2, 7 * 16)).astype(np.float32)
+        w[0, :, 32:48] = 9.0                                                # (the missing page's tokens are the heaviest)
+        k, v = _values(p)
+        kept, to_w, to_len = _evict(p, to, [100, 60], torch.from_numpy(w).to(DEV), 40, 0, 0, torch.zeros(2, dtype=torch.int32, device=DEV))
+        assert to_len.cpu().tolist() == [40, 40]
+        if eight:
+            codes = p.got()
+            got = orc.page8_values(codes[:2], codes[2])
+        else:
+            got = to_np(p.kd), to_np(p.vd)
+        for b in range(2):
+            want = orc.page_evict(w[b], [100, 60][b], 40, 0, 0)
+            assert np.array_equal(kept[b].cpu().numpy(), want)
+            for g in range(2):
+                for j, t in enumerate(want[g]):
+                    src, dst = p.table[b, t // 16], table[b, j // 16]
+                    missing = not 0 <= src < len(k)
+                    assert to_w[b, g, j].item() == (0.0 if missing else w[b, g, t])
+                    if dst < 0:
+                        continue
+                    for x, y in zip((k, v), got):
+                        ref = np.zeros(128) if missing else x[src, t % 16, g]
+                        assert np.abs(y[dst, j % 16, g] - ref).max() <= (2.0 ** -4 * np.abs(ref).max() if eight else 0.0)
+
+
+def test_decoding_goes_on_behind_an_eviction():
+    """append, attention, weights and eviction in turn, in both formats: after each eviction attention is that over the kept tokens, each
+    head its own, and the weights of kept tokens go on."""
+    for eight in (False, True):
+        rng = np.random.default_rng(46)
+        H, Hkv, D, page, B = 8, 2, 128, 16, 2
+        sh = shape(H, Hkv, D, "bf16")
+        p = _paged(eight, rng, sh, page, [80, 80], bounds=False)
+        spare = _paged(eight, rng, sh, page, [80, 80], bounds=False)
+        append = qb.qcf_page8_append if eight else qb.qcf_page_append
+        caches = [p.cache, spare.cache]
+        w = [torch.zeros(B, Hkv, caches[0].tokens, device=DEV) for _ in range(2)]
+        lens, off = i32([30, 3]), i64([0, 1, 2])
+        pos = lens.clone()
+        kept = torch.empty(B, Hkv, 40, dtype=torch.int32, device=DEV)
+        mirror = []                                                        # keys, values and weights of each request and head, as a list
+        for b in range(B):
+            mirror.append([None] * Hkv)
+        q, o, lse = (torch.empty(B, H, D, dtype=p.dt, device=DEV), torch.empty(B, 1, H, D, dtype=p.dt, device=DEV), torch.empty(B, 1, H, device=DEV))
+
+        def read(cache, b, g, n):
+            src = p if cache is caches[0] else spare
+            at = src.table[b, np.arange(n) // page], np.arange(n) % page, g
+            if eight:
+                c = src.got()
+                k, v = orc.page8_values(c[:2], c[2])
+            else:
+                k, v = to_np(src.kd), to_np(src.vd)
+            return k[at], v[at]
+
+        now = 0
+        for step in range(30):
+            cache = caches[now]
+            rows = torch.from_numpy(normal(rng, (B, (H + 2 * Hkv) * D), "bf16")).to(device=DEV, dtype=p.dt)
+            parts = [t.unflatten(1, (-1, D)) for t in rows.split([H * D, Hkv * D, Hkv * D], 1)]
+            append(p.desc, cache, B, *parts, off, B, lens, pos, q)
+            _attn(p)(p.desc, cache, B, 1, q, lens[:, None] + 1, None, 0, o, lse)
+            qb.qcf_page_weigh(p.desc, cache, B, 1, q, lens[:, None] + 1, lse, lens, 1.0, 1.0, w[now])
+            lens += 1
+            pos += 1
+            torch.cuda.synchronize()
+            if step % 10 == 9:
+                held = lens.cpu().tolist()
+                before = [[read(cache, b, g, held[b]) for g in range(Hkv)] for b in range(B)]
+                was = w[now].cpu().numpy()
+                qb.qcf_page_evict(p.desc, cache, B, lens, w[now], 20, 2, 6, caches[1 - now], kept[..., :20].contiguous(), w[1 - now], lens)
+                torch.cuda.synchronize()
+                now = 1 - now
+                for b in range(B):
+                    n = min(20, held[b])
+                    assert lens[b].item() == n
+                    want = orc.page_evict(was[b], held[b], 20, 2, 6)
+                    for g in range(Hkv):
+                        k, v = read(caches[now], b, g, n)
+                        tol = 2.0 ** -4 * 2.0 ** -3 if eight else 0.0      # (small elements of a block whose scale is larger now)
+                        for x, y in zip((k, v), before[b][g]):
+                            assert np.abs(x - y[want[g, :n]]).max() <= tol
+                        assert np.array_equal(w[now][b, g, :n].cpu().numpy(), was[b, g, want[g, :n]])
+            held = lens.cpu().tolist()
+        # attention over what is left is that of the formula
+        qd = torch.from_numpy(normal(rng, (B, 1, H, D), "bf16")).to(device=DEV, dtype=p.dt)
+        _attn(p)(p.desc, caches[now], B, 1, qd, lens[:, None].contiguous(), None, 0, o, lse)
+        torch.cuda.synchronize()
+        for b in range(B):
+            for h in range(H):
+                k, v = read(caches[now], b, h // 4, held[b])
+                z = k @ to_np(qd)[b, 0, h] / math.sqrt(D)
+                e = np.exp(z - z.max())
+                ref = e @ v / e.sum()
+                assert np.abs(to_np(o)[b, 0, h] - ref).max() <= 2.0 ** -8 * np.abs(ref).max() + 1e-4 * np.abs(v).max()
+
+
+def test_weights_and_eviction_replay_from_a_captured_graph():
+    rng = np.random.default_rng(47)
+    p = Paged8(rng, shape(8, 2, 128, "bf16"), 16, [300, 90], width=64)
+    t = Paged8(rng, shape(8, 2, 128, "bf16"), 16, [64, 64])
+    q = torch.from_numpy(normal(rng, (2, 1, 8, 128), "bf16")).to(device=DEV, dtype=p.dt)
+    seen, lens = i32([[300], [90]]), i32([300, 90])
+    o, lse = torch.empty_like(q), torch.empty(2, 1, 8, device=DEV)
+    w, to_w, kept, to_len = torch.zeros(2, 2, 1024, device=DEV), torch.zeros(2, 2, 64, device=DEV), torch.zeros(2, 2, 50, dtype=torch.int32, device=DEV), i32([0, 0])
+    ws = torch.empty(max(1, qb.qcf_page8_attn_workspace_bytes(p.desc, p.cache, 2, 1, 0)), dtype=torch.uint8, device=DEV)
+    ev = torch.empty(max(1, qb.qcf_page_evict_workspace_bytes(p.desc, p.cache, 2, 50)), dtype=torch.uint8, device=DEV)
+
+    def step():
+        qb.qcf_page8_attn(p.desc, p.cache, 2, 1, q, seen, None, 0, o, lse, ws)
+        qb.qcf_page_weigh(p.desc, p.cache, 2, 1, q, seen, lse, None, 0.5, 1.0, w)
+        qb.qcf_page_evict(p.desc, p.cache, 2, lens, w, 50, 4, 8, t.cache, kept, to_w, to_len, ev)
+        q.mul_(-0.9)
+
+    results = lambda: [x.clone() for x in (w, kept, to_w, to_len, t.kd.view(torch.uint8), t.vd.view(torch.uint8), t.sd, t.bd)]
+    rows, eager = q.clone(), []
+    for _ in range(4):
+        step()
+        torch.cuda.synchronize()
+        eager.append(results())
+    q.copy_(rows), w.zero_()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        to_w.fill_(0.0) if i == 0 else None
+        kept.fill_(5)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(results(), eager[i]):
+            assert torch.equal(got, want), i
