@@ -787,13 +787,14 @@ static qcf_status check_evict(const qcf_layer_desc* desc, const qcf_page_cache* 
   return QCF_OK;
 }
 
-size_t qcf_page_evict_workspace_bytes(const qcf_layer_desc*, const qcf_page_cache*, int32_t, int32_t) { return 0; }
+size_t qcf_page_evict_workspace_bytes(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_keep) {
+  return check_evict(desc, cache, B, n_keep) == QCF_OK ? page_evict_workspace(*desc, *cache, B) : 0;
+}
 
 qcf_status qcf_page_evict(const qcf_layer_desc* desc, const qcf_page_cache* cache, const float* scales, int32_t B,
                           const int32_t* len_dev, const float* weights, int32_t n_keep, int32_t n_first, int32_t n_last,
                           const qcf_page_cache* to, float* to_scales, int32_t* kept, float* to_weights, int32_t* to_len_dev,
                           void* workspace, size_t workspace_bytes, void* stream) {
-  (void)workspace; (void)workspace_bytes;
   QCF_TRY(check_evict(desc, cache, B, n_keep));
   QCF_TRY(check_page_cache(desc, to));
   if (n_first < 0 || n_last < 0) return fail(QCF_ERR_INVALID_ARG, "negative size");
@@ -815,8 +816,9 @@ qcf_status qcf_page_evict(const qcf_layer_desc* desc, const qcf_page_cache* cach
   if (to_weights) QCF_TRY(need_ptr(to_weights, "to_weights"));
   if (to_weights == weights) return fail(QCF_ERR_INVALID_ARG, "to_weights must be other memory than weights");
   QCF_TRY(need_idx_ptr(to_len_dev, "to_len_dev"));
+  QCF_TRY(need_ws(workspace, workspace_bytes, page_evict_workspace(*desc, *cache, B)));
   return launch_page_evict(*desc, *cache, scales, B, len_dev, weights, n_keep, n_first, n_last, *to, to_scales, kept, to_weights,
-                           to_len_dev, (hipStream_t)stream);
+                           to_len_dev, workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -18,6 +18,206 @@ struct EvictArgs {
   int Hkv, n_keep, log2_from, log2_to, pages;            // pages of `to` that n_keep tokens fill
 };
 
+// ---- the choice among many tokens: all of the GPU on each row ------------------------------------------------------------------------
+// launch_page_top has one workgroup to a row, which reads it again and again (131072 tokens 104 us).  Here a row is cut into segments of
+// kSegment tokens, one workgroup each, and its threshold is found digit by digit: histograms of 11, 11 and 10 bits of the weights' order
+// keys, added up over the segments by integer atomics (sums do not depend on their order), each launch finding the digit of the one
+// before it.  Then the segments' counts, and the tokens in order.  The same tokens as launch_page_top's, bit for bit.
+constexpr int kSegment = 4096, kThreadsOf = 256, kEach = kSegment / kThreadsOf;
+constexpr int kBits[3] = {11, 11, 10}, kShift[3] = {21, 10, 0};
+constexpr int kHist = 2048 + 2048 + 1024, kHistAt[3] = {0, 2048, 4096};
+
+// Per row: the histograms, the digits found so far (prefix, how many of its keys are still wanted), and per segment how many keys are
+// beyond the threshold and how many equal it.
+struct TopArgs {
+  const float* weights;
+  const int32_t* len;
+  int64_t stride;                        // tokens of a row
+  int Hkv, n_keep, n_first, n_last, segments;
+  uint32_t* hist;                        // [rows][kHist]
+  uint2* state;                          // [rows][2]
+  uint2* counts;                         // [rows][segments]
+  int32_t* kept;
+};
+struct TopRow {
+  int count, n;                          // tokens, and how many stay
+  int lo, hi;                            // tokens that are chosen from
+  int wanted;                            // of them
+};
+__device__ __forceinline__ TopRow top_row(const TopArgs& a, int64_t row) {
+  TopRow r;
+  r.count = (int)min((int64_t)max(a.len[row / a.Hkv], 0), a.stride);
+  r.n = min(r.count, a.n_keep);
+  r.lo = a.n_first;
+  r.hi = r.count - a.n_last;
+  r.wanted = r.count > a.n_keep ? r.n - a.n_first - a.n_last : 0;          // (0: nothing is to be found)
+  return r;
+}
+__device__ __forceinline__ uint32_t order_key(float s) {
+  uint32_t u = __float_as_uint(s);
+  if (u == 0x80000000u) u = 0u;          // -0 and +0 are the same weight
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+// This thread's keys, in order; what is not chosen from has none.
+__device__ __forceinline__ uint32_t read_keys(const TopArgs& a, const TopRow& r, int64_t row, int t0, uint32_t (&key)[kEach]) {
+  const float* w = a.weights + row * a.stride;
+  uint32_t there = 0;
+#pragma unroll
+  for (int q = 0; q < kEach; q += 4) {
+    const int t = t0 + q;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (t < r.hi) v = *reinterpret_cast<const float4*>(w + t);             // (rows are multiples of 16 long)
+    const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      key[q + i] = order_key(f[i]);
+      there |= (uint32_t)(t + i >= r.lo && t + i < r.hi) << (q + i);
+    }
+  }
+  return there;
+}
+// Inclusive sum over the threads of a workgroup.
+__device__ __forceinline__ uint32_t block_incl(uint32_t x, uint32_t (&s_wave)[kThreadsOf / 64]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint32_t y = __shfl_up(x, d, 64);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();
+  if (lane == 63) s_wave[wave] = x;
+  __syncthreads();
+  for (int i = 0; i < wave; ++i) x += s_wave[i];
+  return x;
+}
+// The digit, counted from the largest, in which the `wanted`-th largest key lies, and how many keys are wanted of it.
+template <int LEVEL>
+__device__ __forceinline__ uint2 find_digit(const uint32_t* hist, uint32_t wanted, uint32_t (&s_wave)[kThreadsOf / 64], uint2& s_found) {
+  constexpr int kBins = 1 << kBits[LEVEL], kPer = kBins / kThreadsOf;
+  uint32_t n[kPer], sum = 0;
+  const int top = kBins - 1 - (int)threadIdx.x * kPer;                     // this thread's largest digit
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) sum += n[i] = hist[kHistAt[LEVEL] + top - i];
+  uint32_t before = block_incl(sum, s_wave) - sum;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (before < wanted && before + n[i] >= wanted) s_found = make_uint2((uint32_t)(top - i), wanted - before);
+    before += n[i];
+  }
+  __syncthreads();
+  return s_found;
+}
+
+__global__ __launch_bounds__(256) void top_clear_kernel(uint32_t* hist, int64_t n) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i < n) *reinterpret_cast<uint4*>(hist + i) = make_uint4(0u, 0u, 0u, 0u);
+}
+
+template <int LEVEL>
+__global__ __launch_bounds__(kThreadsOf) void top_count_kernel(TopArgs a) {
+  constexpr int kBins = 1 << kBits[LEVEL];
+  __shared__ uint32_t s_hist[kBins], s_wave[kThreadsOf / 64];
+  __shared__ uint2 s_found;
+  const int64_t row = blockIdx.x / a.segments;
+  const int seg = (int)(blockIdx.x - row * a.segments), tid = threadIdx.x;
+  const TopRow r = top_row(a, row);
+  if (r.wanted <= 0 || seg * kSegment >= r.hi) return;
+  uint32_t* hist = a.hist + row * kHist;
+  uint32_t prefix = 0, wanted = (uint32_t)r.wanted;
+  for (int i = tid; i < kBins; i += kThreadsOf) s_hist[i] = 0u;
+  uint32_t key[kEach];
+  const uint32_t there = read_keys(a, r, row, seg * kSegment + tid * kEach, key);
+  if constexpr (LEVEL > 0) {
+    if constexpr (LEVEL > 1) {
+      const uint2 s = a.state[row * 2];
+      prefix = s.x;
+      wanted = s.y;
+    }
+    const uint2 found = find_digit<LEVEL - 1>(hist, wanted, s_wave, s_found);
+    prefix |= found.x << kShift[LEVEL - 1];
+    if (seg == 0 && tid == 0) a.state[row * 2 + LEVEL - 1] = make_uint2(prefix, found.y);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const bool mine = (there >> i & 1) && (LEVEL == 0 || key[i] >> kShift[LEVEL == 0 ? 0 : LEVEL - 1] == prefix >> kShift[LEVEL == 0 ? 0 : LEVEL - 1]);
+    const uint32_t digit = key[i] >> kShift[LEVEL] & (kBins - 1);
+    // (keys that are all alike, weights of 0 above all, are counted at once)
+    const uint64_t all = __ballot(mine);
+    const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)digit, all ? __builtin_ctzll(all) : 0);
+    if (__ballot(mine && digit == first) == all) {
+      if (all && (threadIdx.x & 63) == 0) atomicAdd(&s_hist[first], (uint32_t)__popcll(all));
+    } else if (mine) {
+      atomicAdd(&s_hist[digit], 1u);
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < kBins; i += kThreadsOf)
+    if (s_hist[i]) atomicAdd(hist + kHistAt[LEVEL] + i, s_hist[i]);
+}
+
+// (WRITE: the tokens, after a launch without it has counted each segment's)
+template <bool WRITE>
+__global__ __launch_bounds__(kThreadsOf) void top_keep_kernel(TopArgs a) {
+  __shared__ uint32_t s_wave[kThreadsOf / 64], s_wave2[kThreadsOf / 64];
+  __shared__ uint2 s_found;
+  const int64_t row = blockIdx.x / a.segments;
+  const int seg = (int)(blockIdx.x - row * a.segments), tid = threadIdx.x;
+  const TopRow r = top_row(a, row);
+  int32_t* kept = a.kept + row * a.n_keep;
+  if constexpr (WRITE) {
+    // what needs no choice: all tokens, or the first and the last ones, and nothing behind them
+    const int t0 = seg * kSegment, t1 = seg + 1 == a.segments ? 0x7fffffff : t0 + kSegment;
+    if (r.count <= a.n_keep) {
+      for (int j = t0 + tid; j < min(t1, a.n_keep); j += kThreadsOf) kept[j] = j < r.count ? j : -1;
+      return;
+    }
+    if (seg == 0) {
+      for (int j = tid; j < a.n_first; j += kThreadsOf) kept[j] = j;
+      for (int j = tid; j < a.n_last; j += kThreadsOf) kept[r.n - a.n_last + j] = r.count - a.n_last + j;
+    }
+  }
+  if (r.wanted <= 0 || seg * kSegment >= r.hi) return;
+  uint32_t key[kEach];
+  const int t0 = seg * kSegment + tid * kEach;
+  const uint32_t there = read_keys(a, r, row, t0, key);
+  const uint2 s = a.state[row * 2 + 1];
+  const uint2 found = find_digit<2>(a.hist + row * kHist, s.y, s_wave, s_found);
+  const uint32_t least = s.x | found.x;                                    // the least key that stays, and how many of its kind
+  uint32_t more = 0, same = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    more |= (uint32_t)((there >> i & 1) && key[i] > least) << i;
+    same |= (uint32_t)((there >> i & 1) && key[i] == least) << i;
+  }
+  const uint32_t n_more = block_incl((uint32_t)__popc(more), s_wave), n_same = block_incl((uint32_t)__popc(same), s_wave2);
+  uint2* counts = a.counts + row * a.segments;
+  if constexpr (!WRITE) {
+    if (tid == kThreadsOf - 1) counts[seg] = make_uint2(n_more, n_same);
+    return;
+  }
+  uint32_t before_more = 0, before_same = 0;                               // in the segments in front of this one
+  for (int i = tid; i < seg; i += kThreadsOf) {
+    before_more += counts[i].x;
+    before_same += counts[i].y;
+  }
+  __shared__ uint32_t s_sum[2];
+  if (tid < 2) s_sum[tid] = 0u;
+  __syncthreads();
+  if (before_more) atomicAdd(&s_sum[0], before_more);
+  if (before_same) atomicAdd(&s_sum[1], before_same);
+  __syncthreads();
+  uint32_t at_same = s_sum[1] + n_same - (uint32_t)__popc(same);
+  uint32_t at = (uint32_t)a.n_first + s_sum[0] + n_more - (uint32_t)__popc(more) + min(at_same, found.y);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const bool tie = same >> i & 1;
+    if ((more >> i & 1) || (tie && at_same < found.y)) kept[at++] = t0 + i;
+    at_same += tie;
+  }
+}
+
+// ---- the rows ------------------------------------------------------------------------------------------------------------------------------
 // One workgroup per (request, KV head, page of the new cache), a wave of it to a block of 16 tokens: their numbers, their pages and then
 // the rows, all of a block on their way together.  Bound by memory: every kept row is read and written once.
 template <typename T, int D, bool EIGHT>
@@ -145,11 +345,23 @@ __global__ __launch_bounds__(256) void evict_kernel(EvictArgs a) {
   }
 }
 
+// Whether the choice is divided over the GPU.
+#ifndef EV
+#define EV 32768
+#endif
+bool splits_choice(const qcf_page_cache& c) { return (int64_t)c.max_pages * c.page_size > EV; }
+
 }  // namespace
+
+size_t page_evict_workspace(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B) {
+  if (!splits_choice(c)) return 0;
+  const int64_t heads = (int64_t)B * L.n_kv_heads, segments = ((int64_t)c.max_pages * c.page_size + kSegment - 1) / kSegment;
+  return (size_t)(heads * (kHist * (int64_t)sizeof(uint32_t) + (2 + segments) * (int64_t)sizeof(uint2)));
+}
 
 qcf_status launch_page_evict(const qcf_layer_desc& L, const qcf_page_cache& c, const float* scales, int32_t B, const int32_t* len,
                              const float* weights, int32_t n_keep, int32_t n_first, int32_t n_last, const qcf_page_cache& to,
-                             float* to_scales, int32_t* kept, float* to_weights, int32_t* to_len, hipStream_t st) {
+                             float* to_scales, int32_t* kept, float* to_weights, int32_t* to_len, void* ws, hipStream_t st) {
   EvictArgs a;
   a.from = c; a.to = to; a.scales = scales; a.to_scales = to_scales;
   a.weights = weights; a.to_weights = to_weights; a.kept = kept; a.to_len = to_len;
@@ -161,8 +373,31 @@ qcf_status launch_page_evict(const qcf_layer_desc& L, const qcf_page_cache& c, c
   const int64_t heads = (int64_t)B * L.n_kv_heads, blocks = heads * a.pages;
   if (blocks > pages::kThreadsAtMost / threads || heads > pages::kThreadsAtMost / pages::kTopThreads)
     return fail(QCF_ERR_UNSUPPORTED, "page evict: too many rows");
-  // (a page of one token: the choice between pages is one between tokens)
-  QCF_TRY(launch_page_top(weights, len, B, L.n_kv_heads, 1, c.max_pages * c.page_size, n_keep, n_first, n_last, kept, st));
+  if (splits_choice(c)) {
+    TopArgs t;
+    t.weights = weights; t.len = len;
+    t.stride = (int64_t)c.max_pages * c.page_size;
+    t.Hkv = L.n_kv_heads; t.n_keep = n_keep; t.n_first = n_first; t.n_last = n_last;
+    t.segments = (int)((t.stride + kSegment - 1) / kSegment);
+    t.hist = static_cast<uint32_t*>(ws);
+    t.state = reinterpret_cast<uint2*>(t.hist + heads * kHist);
+    t.counts = t.state + heads * 2;
+    t.kept = kept;
+    const int64_t groups = heads * t.segments;
+    if (groups > pages::kThreadsAtMost / kThreadsOf) return fail(QCF_ERR_UNSUPPORTED, "page evict: too many rows");
+    const dim3 grid((unsigned)groups), block(kThreadsOf);
+    top_clear_kernel<<<dim3((unsigned)((heads * kHist + 1023) / 1024)), dim3(256), 0, st>>>(t.hist, heads * kHist);
+    QCF_TRY_LAUNCH("page evict");
+    top_count_kernel<0><<<grid, block, 0, st>>>(t);
+    top_count_kernel<1><<<grid, block, 0, st>>>(t);
+    top_count_kernel<2><<<grid, block, 0, st>>>(t);
+    top_keep_kernel<false><<<grid, block, 0, st>>>(t);
+    top_keep_kernel<true><<<grid, block, 0, st>>>(t);
+    QCF_TRY_LAUNCH("page evict: tokens");
+  } else {
+    // (a page of one token: the choice between pages is one between tokens)
+    QCF_TRY(launch_page_top(weights, len, B, L.n_kv_heads, 1, c.max_pages * c.page_size, n_keep, n_first, n_last, kept, st));
+  }
 #define QCF_LAUNCH(T, D, EIGHT) evict_kernel<T, D, EIGHT><<<dim3((unsigned)blocks), dim3(threads), 0, st>>>(a)
 #define QCF_PAGES(T, D) do { if (scales) QCF_LAUNCH(T, D, true); else QCF_LAUNCH(T, D, false); } while (0)
   if (L.dtype == QCF_DTYPE_BF16) {

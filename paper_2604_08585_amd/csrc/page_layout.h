@@ -47,6 +47,12 @@ struct Division {
   bool whole;                             // a workgroup to every context, KV head and row block: nothing is divided
 };
 
+// Workgroups of four waves that a compute unit holds at once.  (8-bit heads of 64 leave room for a third: 64 requests of 4K to 12K tokens 111
+// us, 122 with two.  Those of 128 would spill 27 registers: 234 us, 203 with two.)
+constexpr int at_once(int head_dim, int row_tiles, bool eight) {
+  return head_dim == 64 ? (eight && row_tiles == 1 ? 3 : 2) : row_tiles == 1 ? 2 : 1;
+}
+
 // Whether workgroups of eight waves take whole contexts, in one launch, or four waves each range of them, in two.  The second launch
 // takes 4 to 5 us, a compute unit reads 50 to 60 GB/s at most; what is saved by dividing shrinks as more workgroups share the
 // memory.  us on the GPU, whole and divided.  Heads of 128 in bf16: 8 workgroups (a request, 8 KV heads) of 512 tokens 10.0 and 9.5, of
@@ -55,7 +61,16 @@ struct Division {
 // 13.1, 2048 16.3 and 11.1.  In float32, heads of 64: 2 of 512 10.8 and 9.7, 4 of up to 512 10.9 and 12.3, 1024 15.9 and 10.5.  Over eight
 // shapes, 1 to 64 requests and 256 to 8192 tokens the rule is 0.5 % behind the better of the two on average (272 KB in place of 290:
 // 0.6 %, 350: 0.9 %); at its border it takes the worse one by up to 11 % (19 % in float32), and by 25 % for 2048 workgroups of up to 256 tokens.
+// 8-bit pages: a wave's tile takes about as long whatever its width, so that the rule goes by tokens.  us, whole and divided, bf16 heads of
+// 128: 8 workgroups of 1024 tokens 11.2 and 11.9, 2048 12.2 and 11.9; 192 of up to 2048 22.5 and 25.8, 4096 42.2 and 40.6; 512 of up to 2048
+// 50.1 and 52.5, 4096 88.8 and 88.2.  Heads of 64: 8 of 1024 8.8 and 11.1, 2048 12.7 and 11.4; 64 of up to 2048 17.0 and 16.3; 192 of up to 2048
+// 17.8 and 20.5, 4096 30.4 and 26.7, 8192 58.6 and 43.9; 512 of up to 8192 91.3 and 97.4.  float32, heads of 64: 2 of 512 9.2 and 10.9, 1024 13.9
+// and 11.0; 16 of up to 512 10.7 and 11.4, 1024 17.2 and 11.7.
 inline bool takes_whole(const qcf_layer_desc& L, int64_t workgroups, int64_t longest, int elem) {
+  if (elem == 1) {
+    const int64_t alone = std::max<int64_t>(30, 200 - workgroups * 154 / compute_unit_count());
+    return longest * alone <= (L.dtype == QCF_DTYPE_BF16 ? 1400 : 700) * 200;
+  }
   const int64_t bytes = longest * 2 * L.head_dim * elem;
   const int64_t alone = std::max<int64_t>(30, 200 - workgroups * 256 / compute_unit_count());      // of 200
   return bytes * alone <= (int64_t)((L.dtype == QCF_DTYPE_BF16 ? 290 : 240) << 10) * 200;
@@ -73,10 +88,13 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   // request of 16384 tokens 18.1 and 16.0, 8 of up to 4096 16.6 and 16.4, 64 of up to 1024 19.2 and 16.6, of up to 4096 32.6 and 43.7.
   const int64_t longest = (int64_t)(n_keep && n_keep < c.max_pages ? n_keep : c.max_pages) * c.page_size;
   const double read = (double)d.contexts * (double)longest * L.n_kv_heads * 2 * L.head_dim * elem;
-  d.row_tiles = d.rows > 16 && read > kShared ? 2 : 1;
+  // (8-bit heads of 128: one tile always; the registers of two leave a compute unit one workgroup, which waits for its chains of products.
+  // 64 / 8 heads, us, two tiles and one: four drafts of 8 requests of 2K to 6K tokens 36.5 and 35.6, of 64 of 4K to 12K 347 and 300, of one
+  // of 128K 93 and 79; 16 drafts of 4 requests of up to 8K 65 and 60.  Heads of 64, 8 drafts of 32 requests: 63 and 74.)
+  d.row_tiles = d.rows > 16 && read > kShared && !(elem == 1 && L.head_dim == 128) ? 2 : 1;
   d.row_blocks = (d.rows + 16 * d.row_tiles - 1) / (16 * d.row_tiles);
   d.inner = L.n_kv_heads * d.row_blocks;
-  d.slots = (d.row_tiles == 1 || L.head_dim == 64 ? 2 : 1) * compute_unit_count() / d.inner;       // (two waves to a SIMD, or one)
+  d.slots = at_once(L.head_dim, d.row_tiles, elem == 1) * compute_unit_count() / d.inner;       // (two waves to a SIMD, or one)
   if (d.slots < 1) d.slots = 1;
   d.most = (int64_t)d.contexts * ((longest + kGrain - 1) / kGrain);
   d.least = least_range(L);

@@ -13,6 +13,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 // tiles neither exchange their maxima nor scale what has been summed.
 constexpr float kRoom = 8.f;
 
+
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -146,11 +147,11 @@ struct Window {
 };
 
 // T: type of the queries and outputs, and of the pages; EIGHT: the pages have e4m3 codes, and a scale to every 16 tokens of a head.
-template <typename T, int D, int RT, int MODE, int WAVES, bool EIGHT = false>
+template <typename T, int D, int RT, int MODE, int WAVES, bool EIGHT = false, int SUB = sizeof(T) == 2 ? 2 : 1>
 struct Walk {
   static constexpr bool kHalf = sizeof(T) == 2;
   static constexpr int kSize = EIGHT ? 1 : (int)sizeof(T);             // bytes of a stored element
-  static constexpr int kSub = kHalf ? 2 : 1;             // parts of 16 tokens of a tile; a part lies in one page
+  static constexpr int kSub = SUB;             // parts of 16 tokens of a tile; a part lies in one page
   static constexpr int kTokens = 16 * kSub, kS = 4 * kSub;             // tokens of a tile, logits of a lane
   static constexpr int kQ = kHalf ? D / 32 : D / 16;                   // 16-byte vectors of a lane's part of a query
   static constexpr int kLoads = D * kSize / 64;                        // 16-byte loads of a lane for 16 tokens' keys
@@ -259,6 +260,9 @@ struct Walk {
     return at;
   }
 
+  // bf16 terms of a weight in its product with the values (8 bits: two, 2^-17 of it are lost, beside codes that are off by 2^-4 of what was
+  // stored; four drafts of 8 requests of 2K to 6K tokens 38.7 us with three, 36.5 with two)
+  static constexpr int kTerms = EIGHT ? 2 : 3;
   // products of the tile's values with the weights, added to c
   template <int N>
   __device__ __forceinline__ void values(const Tile& t, const float (&p_)[N][kS], floatx4 (&c)[N][kE]) const {
@@ -272,16 +276,16 @@ struct Walk {
       // third term of a weight that is not 0 are kept from being 0, so that an infinite value comes out infinite and not NaN.)  With
       // two terms, 16 bits, five to seventeen times as many results were off the nearest bf16 value (16 requests of 1K to 8K tokens:
       // 0.41 % and 0.04 %, one of 128K 0.42 % and 0.02 %) in 0 to 1 % less time (64 of 4K to 12K 397.3 and 398.1 us).
-      bf16x8 term[3][N];
+      bf16x8 term[kTerms][N];
 #pragma unroll
       for (int r = 0; r < N; ++r) {
-        u32x4 w[3];
+        u32x4 w[kTerms];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float x = p[r][2 * i], y = p[r][2 * i + 1];
           const float least_x = fminf(x, 0x1p-126f), least_y = fminf(y, 0x1p-126f);
 #pragma unroll
-          for (int n = 0; n < 2; ++n) {
+          for (int n = 0; n < kTerms - 1; ++n) {
             w[n][i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
             x = x - __uint_as_float(__float_as_uint(x) & 0xffff0000u);
             y = y - __uint_as_float(__float_as_uint(y) & 0xffff0000u);
@@ -290,10 +294,10 @@ struct Walk {
               y = fmaxf(y, least_y);
             }
           }
-          w[2][i] = cvt_pk_bf16(x, y);
+          w[kTerms - 1][i] = cvt_pk_bf16(x, y);
         }
 #pragma unroll
-        for (int n = 0; n < 3; ++n) term[n][r] = __builtin_bit_cast(bf16x8, w[n]);
+        for (int n = 0; n < kTerms; ++n) term[n][r] = __builtin_bit_cast(bf16x8, w[n]);
       }
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
@@ -313,7 +317,7 @@ struct Walk {
 #pragma unroll
         for (int r = 0; r < N; ++r)
 #pragma unroll
-          for (int n = 0; n < 3; ++n) c[r][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, term[n][r], c[r][e], 0, 0, 0);
+          for (int n = 0; n < kTerms; ++n) c[r][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, term[n][r], c[r][e], 0, 0, 0);
       }
     } else if constexpr (EIGHT) {
 #pragma unroll
@@ -355,8 +359,16 @@ struct Walk {
     }
   }
 
-  // products of the tile's keys with the queries
+  // products of the tile's keys with the queries: of row col and tokens 4 quad to 4 quad + 3 of each part, or (TOKENS) of token col
+  // and rows 4 quad to 4 quad + 3
+  template <bool TOKENS = false>
   __device__ __forceinline__ void logits(const Tile& t, float (&s)[RT][kS]) const {
+    auto wide = [](bf16x8 k, bf16x8 q, floatx4 z) {
+      return TOKENS ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, k, z, 0, 0, 0) : __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q, z, 0, 0, 0);
+    };
+    auto single = [](float k, float q, floatx4 z) {
+      return TOKENS ? __builtin_amdgcn_mfma_f32_16x16x4f32(q, k, z, 0, 0, 0) : __builtin_amdgcn_mfma_f32_16x16x4f32(k, q, z, 0, 0, 0);
+    };
 #pragma unroll
     for (int h = 0; h < kSub; ++h)
 #pragma unroll
@@ -372,7 +384,7 @@ struct Walk {
               const bf16x2 b = i & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
               x[i] = __builtin_bit_cast(uint32_t, b);
             }
-            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, q[r][f]), z, 0, 0, 0);
+            z = wide(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, q[r][f]), z);
           }
           z *= t.ks[h];
         } else if constexpr (EIGHT) {
@@ -381,16 +393,16 @@ struct Walk {
           for (int f = 0; f < kQ; ++f) {
             const uint32_t w = t.k[h][f / 4][f & 3];     // four codes
             const floatx2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-            z = __builtin_amdgcn_mfma_f32_16x16x4f32(lo[0], __uint_as_float(q[r][f][0]), z, 0, 0, 0);
-            y = __builtin_amdgcn_mfma_f32_16x16x4f32(lo[1], __uint_as_float(q[r][f][1]), y, 0, 0, 0);
-            z = __builtin_amdgcn_mfma_f32_16x16x4f32(hi[0], __uint_as_float(q[r][f][2]), z, 0, 0, 0);
-            y = __builtin_amdgcn_mfma_f32_16x16x4f32(hi[1], __uint_as_float(q[r][f][3]), y, 0, 0, 0);
+            z = single(lo[0], __uint_as_float(q[r][f][0]), z);
+            y = single(lo[1], __uint_as_float(q[r][f][1]), y);
+            z = single(hi[0], __uint_as_float(q[r][f][2]), z);
+            y = single(hi[1], __uint_as_float(q[r][f][3]), y);
           }
           z = (z + y) * t.ks[h];
         } else if constexpr (kHalf) {
 #pragma unroll
           for (int f = 0; f < kLoads; ++f)
-            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[h][f]), __builtin_bit_cast(bf16x8, q[r][f]), z, 0, 0, 0);
+            z = wide(__builtin_bit_cast(bf16x8, t.k[h][f]), __builtin_bit_cast(bf16x8, q[r][f]), z);
         } else {
           // (two sums side by side: half the chain, and less rounding)
           floatx4 y = {0.f, 0.f, 0.f, 0.f};
@@ -399,7 +411,7 @@ struct Walk {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               floatx4& sum = e & 1 ? y : z;
-              sum = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[h][f][e]), __uint_as_float(q[r][f][e]), sum, 0, 0, 0);
+              sum = single(__uint_as_float(t.k[h][f][e]), __uint_as_float(q[r][f][e]), sum);
             }
           z += y;
         }
@@ -661,7 +673,7 @@ __device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MOD
 
 // WHOLE: a workgroup has a context as a whole, and nothing is joined.
 template <typename T, int D, int RT, int MODE, int WAVES, bool WHOLE, bool EIGHT>
-__global__ __launch_bounds__(64 * WAVES, RT == 1 || D == 64 ? 2 : 1) void page_attn_kernel(PageAttnArgs a) {
+__global__ __launch_bounds__(64 * WAVES, WHOLE ? 2 : pages::at_once(D, RT, EIGHT)) void page_attn_kernel(PageAttnArgs a) {
   typedef Walk<T, D, RT, MODE, WAVES, EIGHT> W;
   constexpr int kRows = 16 * RT;
   __shared__ __align__(16) float s_o[WAVES][kRows][D + 4];         // (rows 4 banks apart)

@@ -19,82 +19,90 @@ struct WeighArgs {
   int row_blocks;
 };
 
+// Workgroups on a compute unit, of four waves each: three where the registers allow it.  (64 requests of 4K to 12K tokens in 8 bits, two rows
+// each, us: 132 with two, 129 with three, 139 with four, whose registers spill; tiles of 64 tokens 133 with two.  16 of 1K to 16K in bf16:
+// 73.0, 72.5 and 95; 73.1.)
+constexpr int at_once(bool eight, int row_tiles) { return eight && row_tiles == 1 ? 3 : 2; }
+
 template <typename T, int D, int RT, bool EIGHT>
 struct Weigher : Walk<T, D, RT, kSeveral, pages::kWaves, EIGHT> {
   typedef Walk<T, D, RT, kSeveral, pages::kWaves, EIGHT> W;
   typedef typename W::Tile Tile;
   static constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.925963033500e-8f;
   const WeighArgs& w_;
-  float ref[RT], ref_low[RT];                            // lse in powers of two, as two floats
-  floatx4* out;                                          // weights of token 0 of this lane's four
+  float ref[RT][4], ref_low[RT][4];                      // lse in powers of two of rows 4 quad to 4 quad + 3 (float32: as two floats)
+  int sees[RT][4];                                       // tokens that they see
+  float* out;                                            // this lane's place among the weights: token col of part `quad` of a tile
   int known;                                             // tokens weighed before
+  int tokens;                                            // that any row of the context sees
 
   __device__ __forceinline__ Weigher(const WeighArgs& args, int lane, int g) : W(args.a, lane, g), w_(args) {}
 
-  __device__ __forceinline__ void prepare(int context, int row0, int64_t begin, int64_t end) {
+  __device__ __forceinline__ void prepare(int context, int row0, int64_t begin, int64_t end, int tokens_) {
     this->start(context, row0, begin, end);
+    tokens = tokens_;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const int row = this->row_of(r);
-      const bool there = row < this->a.rows;
-      const int i = there ? row / this->a.G : 0;
-      const float l = there ? w_.lse[((int64_t)context * this->a.n_q + i) * this->a.H + this->g * this->a.G + (row - i * this->a.G)] : 0.f;
-      ref[r] = l * kLog2e;
-      ref_low[r] = __builtin_isfinite(ref[r]) ? __builtin_fmaf(l, kLog2e, -ref[r]) + l * kLog2eLow : 0.f;
-    }
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = row0 + 16 * r + 4 * this->quad + i;
+        sees[r][i] = __shfl(this->lim[r], 4 * this->quad + i, 64);
+        const int at = row / this->a.G;
+        const float l = sees[r][i] > 0 ? w_.lse[((int64_t)context * this->a.n_q + at) * this->a.H + this->g * this->a.G + (row - at * this->a.G)] : INFINITY;
+        ref[r][i] = l * kLog2e;                          // (a row that sees nothing: infinite, its weights are 0)
+        ref_low[r][i] = __builtin_isfinite(ref[r][i]) ? __builtin_fmaf(l, kLog2e, -ref[r][i]) + l * kLog2eLow : 0.f;
+      }
     known = w_.old ? w_.old[context] : 0x7fffffff;
-    out = reinterpret_cast<floatx4*>(w_.weights + ((int64_t)context * this->a.Hkv + this->g) * w_.stride) + this->quad + 4 * this->col;
+    out = w_.weights + ((int64_t)context * this->a.Hkv + this->g) * w_.stride + this->lane;
   }
 
-  // (lanes 0 and 1 of each 16 have the weights of a tile's parts)
-  __device__ __forceinline__ bool mine(int64_t at) const { return this->col < W::kSub && at + 16 * this->col < this->lim_hi; }
-  __device__ __forceinline__ void load(Tile& t, floatx4& was, int64_t at, bool first) {
+  __device__ __forceinline__ bool mine(int64_t at) const { return this->quad < W::kSub && at + this->lane < tokens; }
+  __device__ __forceinline__ void load(Tile& t, float& was, int64_t at, bool first) {
     const typename W::Where r = this->find(at);
     this->load_keys(t, r);
 #pragma unroll
     for (int h = 0; h < W::kSub; ++h) t.base[h] = r.base[h];
-    was = floatx4{0.f, 0.f, 0.f, 0.f};
-    if ((!first || w_.alpha != 0.f) && mine(at)) was = out[at / 4];
+    was = 0.f;
+    if ((!first || w_.alpha != 0.f) && mine(at)) was = out[at];
   }
-  __device__ __forceinline__ void weigh(const Tile& t, floatx4 was, int64_t at, bool first) {
-    float s[RT][W::kS], sum[W::kS];
-    this->logits(t, s);
+  __device__ __forceinline__ void weigh(const Tile& t, float was, int64_t at, bool first) {
+    float s[RT][W::kS], sum = 0.f;
+    this->template logits<true>(t, s);
+    bool whole = true;
 #pragma unroll
-    for (int i = 0; i < W::kS; ++i) {
-      sum[i] = 0.f;
+    for (int h = 0; h < W::kSub; ++h) whole = whole && t.base[h] >= 0 && t.base[h] + 16 <= this->lim_lo;
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        const float x = __builtin_fmaf(s[r][i], this->a.scale, -ref[r]) + __builtin_fmaf(s[r][i], this->a.scale_low, -ref_low[r]);
-        const bool ok = t.base[i >> 2] >= 0 && this->token(t, i) < this->lim[r];
-        sum[i] += ok ? __builtin_amdgcn_exp2f(x) : 0.f;
-      }
-      sum[i] = row_sum(sum[i]);
+    for (int h = 0; h < W::kSub; ++h) {
+      float part = 0.f;
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float z = s[r][4 * h + i];
+          float x = __builtin_fmaf(z, this->a.scale, -ref[r][i]);
+          // (bf16: 2^-24 of the logit and of lse less, beside what the products of rounded queries and keys have lost)
+          if constexpr (!W::kHalf) x += __builtin_fmaf(z, this->a.scale_low, -ref_low[r][i]);
+          float e = __builtin_amdgcn_exp2f(x);
+          // (a row that sees nothing may hold anything)
+          e = whole ? (sees[r][i] > 0 ? e : 0.f) : t.base[h] >= 0 && t.base[h] + this->col < sees[r][i] ? e : 0.f;
+          part += e;
+        }
+      typedef unsigned u2v __attribute__((ext_vector_type(2)));
+      u2v y = __builtin_amdgcn_permlane16_swap(__float_as_uint(part), __float_as_uint(part), false, false);
+      part = __uint_as_float(y.x) + __uint_as_float(y.y);
+      y = __builtin_amdgcn_permlane32_swap(__float_as_uint(part), __float_as_uint(part), false, false);
+      part = __uint_as_float(y.x) + __uint_as_float(y.y);
+      sum = h == this->quad ? part : sum;
     }
     if (!mine(at)) return;
-    const int64_t token = at + 16 * this->col + 4 * this->quad;
-    floatx4 now;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float mine = sum[i];
-#pragma unroll
-      for (int h = 1; h < W::kSub; ++h) mine = this->col == h ? sum[4 * h + i] : mine;
-      const float before = !first ? was[i] : token + i < known && w_.alpha != 0.f ? w_.alpha * was[i] : 0.f;
-      now[i] = before + w_.beta * mine;
-      if (now[i] != now[i]) now[i] = NAN;
-    }
-    if (token + 4 <= this->lim_hi) {
-      out[at / 4] = now;
-    } else {
-      float* w = reinterpret_cast<float*>(out + at / 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (token + i < this->lim_hi) w[i] = now[i];
-    }
+    const float before = !first ? was : at + this->lane < known && w_.alpha != 0.f ? w_.alpha * was : 0.f;
+    const float now = before + w_.beta * sum;
+    out[at] = now != now ? NAN : now;
   }
   __device__ __forceinline__ void run(int64_t at, bool first) {
     if (at >= this->end) return;
     Tile t0, t1;
-    floatx4 w0, w1;
+    float w0, w1;
     load(t0, w0, at, first);
     while (true) {
       int64_t next = at + W::kStep;
@@ -110,7 +118,7 @@ struct Weigher : Walk<T, D, RT, kSeveral, pages::kWaves, EIGHT> {
 };
 
 template <typename T, int D, int RT, bool EIGHT>
-__global__ __launch_bounds__(64 * pages::kWaves, 2) void page_weigh_kernel(WeighArgs args) {
+__global__ __launch_bounds__(64 * pages::kWaves, at_once(EIGHT, RT)) void page_weigh_kernel(WeighArgs args) {
   typedef Weigher<T, D, RT, EIGHT> W;
   const PageAttnArgs& a = args.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -128,8 +136,7 @@ __global__ __launch_bounds__(64 * pages::kWaves, 2) void page_weigh_kernel(Weigh
       const int64_t begin = g0 * pages::kGrain, end = g1 == here.grains ? tokens : g1 * pages::kGrain;
       // (each wave's tokens are its own, and so are their weights: the second block of rows finds what the first one stored)
       for (int block = 0; block < args.row_blocks; ++block) {
-        w.prepare(here.x, block * 16 * RT, begin, end);
-        w.lim_hi = (int)tokens;                          // (of all rows)
+        w.prepare(here.x, block * 16 * RT, begin, end, (int)tokens);
         w.run(begin + wave * W::W::kTokens, block == 0);
       }
     }
@@ -157,7 +164,7 @@ qcf_status launch_page_weigh(const qcf_layer_desc& L, const qcf_page_cache& c, c
   w.stride = (int64_t)c.max_pages * c.page_size;
   w.row_blocks = (rows + 16 * row_tiles - 1) / (16 * row_tiles);
   const int64_t ranges = ((int64_t)B * ((w.stride + pages::kGrain - 1) / pages::kGrain) + w.a.least - 1) / w.a.least;
-  w.a.slots = (int)std::min<int64_t>(ranges, std::max(1, 2 * compute_unit_count() / L.n_kv_heads));
+  w.a.slots = (int)std::min<int64_t>(ranges, std::max(1, at_once(scales != nullptr, row_tiles) * compute_unit_count() / L.n_kv_heads));
   const dim3 grid((unsigned)((int64_t)w.a.slots * w.a.inner)), block(64 * pages::kWaves);
 #define QCF_LAUNCH(T, D, RT, EIGHT) page_weigh_kernel<T, D, RT, EIGHT><<<grid, block, 0, st>>>(w)
 #define QCF_ROWS(T, D, EIGHT) do { if (row_tiles == 1) QCF_LAUNCH(T, D, 1, EIGHT); else QCF_LAUNCH(T, D, 2, EIGHT); } while (0)

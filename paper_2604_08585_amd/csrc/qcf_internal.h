@@ -379,6 +379,7 @@ qcf_status launch_page_weigh(const qcf_layer_desc& L, const qcf_page_cache& c, c
                              float* weights, hipStream_t st);
 qcf_status launch_page_evict(const qcf_layer_desc& L, const qcf_page_cache& c, const float* scales, int32_t B, const int32_t* len,
                              const float* weights, int32_t n_keep, int32_t n_first, int32_t n_last, const qcf_page_cache& to,
-                             float* to_scales, int32_t* kept, float* to_weights, int32_t* to_len, hipStream_t st);
+                             float* to_scales, int32_t* kept, float* to_weights, int32_t* to_len, void* ws, hipStream_t st);
+size_t page_evict_workspace(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B);
 
 }  // namespace qcf

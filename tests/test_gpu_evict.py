@@ -150,13 +150,14 @@ def _evict(p, to, lens, w, keep, first, last, to_len=None):
     return kept, to_w, to_len
 
 
+@pytest.mark.parametrize("wide", [False, True])               # (a wide table: the choice is divided over the GPU)
 @pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("case", EVICTIONS)
-def test_eviction(case, eight):
+def test_eviction(case, eight, wide):
     dtype, H, Hkv, D, page, new_page, order, lens, keep, first, last = case
     rng = np.random.default_rng(44)
     B = len(lens)
-    p = _paged(eight, rng, shape(H, Hkv, D, dtype), page, lens, order)
+    p = _paged(eight, rng, shape(H, Hkv, D, dtype), page, lens, order, width=40960 // page if wide else None)
     t = _paged(eight, rng, shape(H, Hkv, D, dtype), new_page, [keep] * B, order)              # other pools, for pages of another size
     say("evict", dtype, H, Hkv, D, page, "->", new_page, "8 bits" if eight else "", "lens", lens[:8], "keep", keep)
     tokens = p.table.shape[1] * page
@@ -198,6 +199,43 @@ def test_eviction(case, eight):
                 assert np.array_equal(got[which][page_id, at], before[which][page_id, at])
         for x in t.table[b, -(-n // new_page):]:
             assert np.array_equal(to_np(t.bd)[x], b0[x])
+
+
+@pytest.mark.parametrize("B,Hkv,tokens,keep,first,last,kind", [
+    (1, 2, 131072, 30000, 4, 1000, "heavy"), (2, 1, 50000, 4097, 3, 5, "equal"), (3, 2, 40001, 12289, 0, 0, "zeros"), (1, 1, 70000, 69999, 1, 1, "heavy"),
+    (2, 2, 45000, 8192, 4096, 4096, "heavy"), (1, 2, 33000, 1, 0, 0, "signs"), (1, 1, 40000, 100, 100, 0, "heavy"), (2, 1, 36865, 20000, 7, 4095, "steps"),
+    (1, 3, 65536, 32768, 0, 32768, "heavy")])
+def test_choice_among_many_tokens(B, Hkv, tokens, keep, first, last, kind):
+    """Long rows, of which all of the GPU works on each: the tokens that a stable sort keeps."""
+    rng = np.random.default_rng(48)
+    page, D = 256, 64
+    width = -(-tokens // page)
+    lens = [tokens - 37 * b for b in range(B)]
+    pools = [torch.zeros(width, page, Hkv, D, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    tables = [torch.arange(n, dtype=torch.int32, device=DEV).repeat(B, 1).contiguous() for n in (width, -(-keep // page))]
+    cache, to = (qb.page_cache(*pools, None, t) for t in tables)
+    desc = qb.make_desc(shape(Hkv, Hkv, D, "bf16"))
+    w = {"heavy": lambda n: np.exp(2 * rng.standard_normal(n)), "equal": lambda n: np.full(n, 0.25), "zeros": lambda n: rng.random(n) * (rng.random(n) < 0.2),
+         "signs": lambda n: rng.standard_normal(n), "steps": lambda n: rng.integers(0, 5, n) * 2.0 ** -10}[kind]((B, Hkv, width * page)).astype(np.float32)
+    if kind == "signs":
+        w[:, :, ::1000], w[:, :, 1::1000], w[:, :, 2::1000] = -0.0, np.inf, -np.inf
+    if kind == "heavy":
+        w[0, 0, 20000:20010] = np.nan
+    say("choice", B, Hkv, tokens, keep, first, last, kind)
+    kept = torch.full((B, Hkv, keep), 77, dtype=torch.int32, device=DEV)
+    to_len = i32([0] * B)
+    for _ in range(2):                                                     # (the second call finds the first one's workspace in the allocator)
+        qb.qcf_page_evict(desc, cache, B, i32(lens), torch.from_numpy(w).to(DEV), keep, first, last, to, kept, None, to_len)
+    torch.cuda.synchronize()
+    for b in range(B):
+        for g in range(Hkv):
+            x, t = w[b, g, :lens[b]].astype(np.float64), np.arange(lens[b])
+            forced = (t < first) | (t >= lens[b] - last)
+            rank = np.where(forced, 2, np.where(np.isnan(x), 1, 0))
+            order = np.lexsort((t, -np.where(np.isnan(x) | forced, 0.0, x), -rank))
+            want = np.sort(order[:keep])
+            assert np.array_equal(kept[b, g].cpu().numpy(), want), (b, g)
+        assert to_len[b].item() == min(lens[b], keep)
 
 
 def test_eviction_within_one_pool_and_what_is_not_there():

@@ -6,7 +6,9 @@ Tolerances, derived.  A code is off by at most half a step: 2^-4 of its value, o
              first-order term), the two products and the sum by 2^-24 each; a code then by half a step of what it stands for and slack; a
              scale only where the largest element lies within slack of the border.
   attention  as for pages of the layer's type (a logit of d products in 32 bits: eps = (d + 4) 2^-24 sum |q k| / sqrt(d), and one more
-             rounding each for the two scales; weights by exp(2 eps) and 2^-22; sums of T terms T 2^-24), relative to max |v|.
+             rounding each for the two scales; weights by exp(2 eps) and 2^-22; sums of T terms T 2^-24; in bf16 a weight enters its product
+             as two terms: cut off after 8 bits, the rest, less than 2^-7 of it, to half a step of 2^-8, so 2^-15 at most; the products of
+             both are exact in 32 bits), relative to max |v|.
 """
 import math
 
@@ -200,7 +202,7 @@ def _attend_and_check(p, rng, seen, pages=None, q=None, with_lse=True):
             x = np.asarray(q[b, i], dtype=np.float64)
             terms = max((np.abs(rows[0][:, h // (H // sh.n_kv_heads)]) @ np.abs(x[h])).max() for h in range(H))
             eps, T = (D + 5) * 2.0 ** -24 * terms / math.sqrt(D), len(rows[0])
-            out = (2 * eps + 2.0 ** -22 + (T + 1) * 2.0 ** -24) * np.abs(rows[1]).max()
+            out = (2 * eps + 2.0 ** -22 + (T + 1) * 2.0 ** -24 + (2.0 ** -15 if sh.dtype == "bf16" else 0.0)) * np.abs(rows[1]).max()
             assert np.all(np.abs(got[b, i] - ref) <= HALF_STEP[sh.dtype] * np.abs(ref) + out), (b, i, np.abs(got[b, i] - ref).max(), out)
             if with_lse:
                 seeing = np.isfinite(ref_z)

@@ -38,9 +38,9 @@ def _weigh(d, c, B=1, sc=FAKE, n_q=1, q=FAKE, seen=FAKE, lse=FAKE, old=None, alp
     return qb.load_library().qcf_page_weigh(C.byref(d), C.byref(c), sc, B, n_q, q, seen, lse, old, alpha, beta, w, None)
 
 
-def _evict(d, c, B=1, sc=FAKE, lens=FAKE, w=FAKE, keep=4, first=1, last=1, to=None, to_sc=FAKE, kept=FAKE, to_w=None, to_len=FAKE, ws=None):
+def _evict(d, c, B=1, sc=FAKE, lens=FAKE, w=FAKE, keep=4, first=1, last=1, to=None, to_sc=FAKE, kept=FAKE, to_w=None, to_len=FAKE, ws=FAKE, have=1 << 50):
     return qb.load_library().qcf_page_evict(C.byref(d), C.byref(c), sc, B, lens, w, keep, first, last, C.byref(to or _raw()), to_sc, kept, to_w,
-                                            to_len, ws, 0, None)
+                                            to_len, ws, have, None)
 
 
 def _said():
@@ -92,6 +92,10 @@ def test_other_refusals():
                      (dict(to_w=FAKE + 4), b"to_weights")]:
         assert _evict(d, c, **kw) == 1 and word in _said(), kw
     assert _evict(d, c, B=65536) == 2
+    long = _raw(max_pages=1 << 16)
+    need = qb.load_library().qcf_page_evict_workspace_bytes(C.byref(d), C.byref(long), 3, 4)
+    assert need > 0 and _evict(d, long, B=3, have=need - 1) == 3 and _evict(d, long, B=3, ws=None) == 3
+    assert qb.load_library().qcf_page_evict_workspace_bytes(C.byref(d), C.byref(c), 3, 4) == 0
 
 
 def test_launches_of_more_than_2_to_the_32_threads_are_refused():
