@@ -345,17 +345,17 @@ __global__ __launch_bounds__(256) void evict_kernel(EvictArgs a) {
   }
 }
 
-// Whether the choice is divided over the GPU.
-#ifndef EV
-#define EV 32768
-#endif
-bool splits_choice(const qcf_page_cache& c) { return (int64_t)c.max_pages * c.page_size > EV; }
+// Whether the choice is divided over the GPU: six launches and five passes over the weights, so long rows and not too many of them.  Eviction
+// of 8-bit heads of 64 to an eighth, us, divided and not: 8 rows of 32768 tokens 36 and 25, 49152 38 and 43, 131072 44 and 108; 64 rows of
+// 32768 58 and 45, 49152 75 and 76, 131072 150 and 203; 256 rows of 65536 270 and 237.
+bool splits_choice(const qcf_page_cache& c, int64_t rows) { return (int64_t)c.max_pages * c.page_size > 32768 && rows <= 128; }
 
 }  // namespace
 
 size_t page_evict_workspace(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B) {
-  if (!splits_choice(c)) return 0;
-  const int64_t heads = (int64_t)B * L.n_kv_heads, segments = ((int64_t)c.max_pages * c.page_size + kSegment - 1) / kSegment;
+  const int64_t heads = (int64_t)B * L.n_kv_heads;
+  if (!splits_choice(c, heads)) return 0;
+  const int64_t segments = ((int64_t)c.max_pages * c.page_size + kSegment - 1) / kSegment;
   return (size_t)(heads * (kHist * (int64_t)sizeof(uint32_t) + (2 + segments) * (int64_t)sizeof(uint2)));
 }
 
@@ -373,7 +373,7 @@ qcf_status launch_page_evict(const qcf_layer_desc& L, const qcf_page_cache& c, c
   const int64_t heads = (int64_t)B * L.n_kv_heads, blocks = heads * a.pages;
   if (blocks > pages::kThreadsAtMost / threads || heads > pages::kThreadsAtMost / pages::kTopThreads)
     return fail(QCF_ERR_UNSUPPORTED, "page evict: too many rows");
-  if (splits_choice(c)) {
+  if (splits_choice(c, heads)) {
     TopArgs t;
     t.weights = weights; t.len = len;
     t.stride = (int64_t)c.max_pages * c.page_size;

@@ -39,7 +39,8 @@ struct Division {
   int rows;                               // rows of a context and KV head: (new rows) * heads of the group
   int row_tiles;                          // of 16 rows, in a workgroup: 1 or 2
   int row_blocks;                         // workgroups that take the rows of a context and KV head
-  int inner;                              // workgroups of a range: KV heads x row blocks
+  int inner;                              // KV heads x row blocks of a range
+  int heads;                              // KV heads that a workgroup of a range takes side by side
   int slots;                              // ranges at most
   int least;                              // grains of a range at least (a power of two)
   int pad;                                // grains that the beginning of a context counts for
@@ -51,6 +52,16 @@ struct Division {
 // us, 122 with two.  Those of 128 would spill 27 registers: 234 us, 203 with two.)
 constexpr int at_once(int head_dim, int row_tiles, bool eight) {
   return head_dim == 64 ? (eight && row_tiles == 1 ? 3 : 2) : row_tiles == 1 ? 2 : 1;
+}
+
+// KV heads whose rows lie next to each other and are read side by side, by the waves of a workgroup: 256 bytes in a row, as a row of bf16
+// has.  read: bytes of the keys and values at most; where they are few, the joins of twice as many parts cost more.  us, pages that keep a
+// token's 8-bit heads together, a head to a workgroup and side by side: heads of 128, 64 requests of 4K to 12K tokens 243 and 217, one of 128K
+// 70 and 64, of 30K (61 MB) 23.3 and 24.8; heads of 64 188 and 130, one of 30K 22.0 and 20.2, of 3K 11.8 and 14.5.
+inline int side_by_side(const qcf_layer_desc& L, const qcf_page_cache& c, int elem, double read) {
+  const int heads = 256 / L.head_dim;
+  const bool worth = read > (L.head_dim == 128 ? 4.0 : 1.0) * kShared;
+  return elem == 1 && worth && c.head_stride == L.head_dim && L.n_kv_heads % heads == 0 ? heads : 1;
 }
 
 // Whether workgroups of eight waves take whole contexts, in one launch, or four waves each range of them, in two.  The second launch
@@ -94,7 +105,9 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   d.row_tiles = d.rows > 16 && read > kShared && !(elem == 1 && L.head_dim == 128) ? 2 : 1;
   d.row_blocks = (d.rows + 16 * d.row_tiles - 1) / (16 * d.row_tiles);
   d.inner = L.n_kv_heads * d.row_blocks;
-  d.slots = at_once(L.head_dim, d.row_tiles, elem == 1) * compute_unit_count() / d.inner;       // (two waves to a SIMD, or one)
+  // (several new rows with heads of 128: 51.0 us with a head to a workgroup, 55.6, for four drafts of 16 requests of up to 8K tokens)
+  d.heads = n_keep || d.row_tiles > 1 || (n_q > 1 && L.head_dim == 128) ? 1 : side_by_side(L, c, elem, read);
+  d.slots = at_once(L.head_dim, d.row_tiles, elem == 1) * compute_unit_count() * d.heads / d.inner;       // (two waves to a SIMD, or one)
   if (d.slots < 1) d.slots = 1;
   d.most = (int64_t)d.contexts * ((longest + kGrain - 1) / kGrain);
   d.least = least_range(L);

@@ -611,11 +611,13 @@ __device__ __forceinline__ void store_row(const PageAttnArgs& a, int x, int g, i
 
 // Joins the waves of a workgroup: their sums go through LDS, scaled to the largest of their reference points, and leave as rows of
 // the output, or as partial result `part`.
-template <typename T, int D, int RT, int MODE, int WAVES, bool EIGHT>
-__device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MODE, WAVES, EIGHT>& w, float (&s_o)[WAVES][16 * RT][D + 4],
-                                       float (&s_m)[WAVES][16 * RT], float (&s_l)[WAVES][16 * RT], int in, int row0, int64_t part) {
+// (HEADS: heads of the workgroup, whose waves alternate; in and g are those of the first one)
+template <int HEADS, typename T, int D, int RT, int MODE, int WAVES, bool EIGHT>
+__device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MODE, WAVES, EIGHT>& w, float (&s_o)[WAVES * HEADS][16 * RT][D + 4],
+                                       float (&s_m)[WAVES * HEADS][16 * RT], float (&s_l)[WAVES * HEADS][16 * RT], int in, int g, int row0,
+                                       int64_t part) {
   typedef Walk<T, D, RT, MODE, WAVES, EIGHT> W;
-  constexpr int kRows = 16 * RT, kThreads = 64 * WAVES;
+  constexpr int kRows = 16 * RT, kThreads = 64 * WAVES * HEADS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
@@ -643,17 +645,17 @@ __device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MOD
   }
   __syncthreads();
   const int rows = min(kRows, a.rows - row0);
-  for (int item = tid; item < rows * (D / 4); item += kThreads) {
-    const int r = item / (D / 4), e = item % (D / 4) * 4;
-    float top = s_m[0][r];
+  for (int item = tid; item < HEADS * rows * (D / 4); item += kThreads) {
+    const int of = item / (D / 4), head = HEADS == 1 ? 0 : of / rows, r = HEADS == 1 ? of : of - head * rows, e = item % (D / 4) * 4;
+    float top = s_m[head][r];
 #pragma unroll
-    for (int i = 1; i < WAVES; ++i) top = fmaxf(top, s_m[i][r]);
+    for (int i = 1; i < WAVES; ++i) top = fmaxf(top, s_m[i * HEADS + head][r]);
     float l = 0.f;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
-      const float mi = s_m[i][r], li = s_l[i][r];
-      const floatx4 oi = *reinterpret_cast<const floatx4*>(&s_o[i][r][e]);
+      const float mi = s_m[i * HEADS + head][r], li = s_l[i * HEADS + head][r];
+      const floatx4 oi = *reinterpret_cast<const floatx4*>(&s_o[i * HEADS + head][r][e]);
       // (what saw nothing or only logits of -inf weighs nothing beside others; the latter make a row NaN that has nothing else.  Their
       // sums are 0, or NaN where a value is not finite)
       if (mi == -INFINITY) { l = top == -INFINITY ? l + li : l; o += oi; continue; }
@@ -662,30 +664,30 @@ __device__ __forceinline__ void finish(const PageAttnArgs& a, Walk<T, D, RT, MOD
       o += f * oi;
     }
     if (part >= 0) {
-      const int64_t at = (part * a.inner + in) * a.part_rows + r;
+      const int64_t at = (part * a.inner + in + head) * a.part_rows + r;
       *reinterpret_cast<floatx4*>(a.part_o + at * D + e) = o;
       if (e == 0) a.part_ml[at] = make_float2(top, l);
       continue;
     }
-    store_row<T, D>(a, w.x, w.g, row0 + r, e, top, l, o);
+    store_row<T, D>(a, w.x, g + head, row0 + r, e, top, l, o);
   }
 }
 
-// WHOLE: a workgroup has a context as a whole, and nothing is joined.
-template <typename T, int D, int RT, int MODE, int WAVES, bool WHOLE, bool EIGHT>
+// WHOLE: a workgroup has a context as a whole, and nothing is joined.  HEADS: KV heads that it takes side by side.
+template <typename T, int D, int RT, int MODE, int WAVES, bool WHOLE, bool EIGHT, int HEADS>
 __global__ __launch_bounds__(64 * WAVES, WHOLE ? 2 : pages::at_once(D, RT, EIGHT)) void page_attn_kernel(PageAttnArgs a) {
-  typedef Walk<T, D, RT, MODE, WAVES, EIGHT> W;
+  typedef Walk<T, D, RT, MODE, WAVES / HEADS, EIGHT> W;
   constexpr int kRows = 16 * RT;
   __shared__ __align__(16) float s_o[WAVES][kRows][D + 4];         // (rows 4 banks apart)
   __shared__ float s_m[WAVES][kRows], s_l[WAVES][kRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t r = blockIdx.x / a.inner;
-  const int in = (int)(blockIdx.x - r * a.inner), g = in % a.Hkv, row0 = in / a.Hkv * kRows;
-  W w(a, lane, g);
+  const int64_t r = blockIdx.x / (a.inner / HEADS);
+  const int in = (int)(blockIdx.x - r * (a.inner / HEADS)) * HEADS, g = in % a.Hkv, row0 = in / a.Hkv * kRows;
+  W w(a, lane, g + wave % HEADS);
   if constexpr (WHOLE) {
     w.start((int)r, row0, 0, list_end<MODE>(a, context_tokens(a, (int)r)));
-    w.run(wave * W::kTokens);
-    finish(a, w, s_o, s_m, s_l, in, row0, -1);
+    w.run(wave / HEADS * W::kTokens);
+    finish<HEADS>(a, w, s_o, s_m, s_l, in, g, row0, -1);
     return;
   }
   const Contexts all = contexts_of(a, lane);
@@ -698,8 +700,8 @@ __global__ __launch_bounds__(64 * WAVES, WHOLE ? 2 : pages::at_once(D, RT, EIGHT
     if (g1 > g0) {
       const int64_t tokens = here.x < 64 ? from_lane(all.tokens, here.x) : context_tokens(a, here.x);
       w.start(here.x, row0, g0 * pages::kGrain, g1 == here.grains ? list_end<MODE>(a, tokens) : g1 * pages::kGrain);
-      w.run(g0 * pages::kGrain + wave * W::kTokens);
-      finish(a, w, s_o, s_m, s_l, in, row0, g1 - g0 == here.grains ? -1 : 2 * r + (g0 == 0));
+      w.run(g0 * pages::kGrain + wave / HEADS * W::kTokens);
+      finish<HEADS>(a, w, s_o, s_m, s_l, in, g, row0, g1 - g0 == here.grains ? -1 : 2 * r + (g0 == 0));
     }
     here.start += here.grains + all.pad;
     if (here.start >= to || all.apart || ++here.x >= a.contexts) return;
@@ -769,7 +771,7 @@ __global__ __launch_bounds__(256) void page_join_kernel(PageAttnArgs a, int row_
 
 template <typename T, int D, bool EIGHT>
 qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t st) {
-  const int64_t blocks = (int64_t)(d.whole ? d.contexts : d.slots) * d.inner;
+  const int64_t blocks = d.whole ? (int64_t)d.contexts * d.inner : (int64_t)d.slots * (d.inner / d.heads);
   // groups of a joining workgroup share a row where contexts have more than four parts on average
   const bool shared = (int64_t)d.contexts * 4 < d.slots;
   const int row_steps = shared ? a.part_rows : (a.part_rows + 1024 / D - 1) / (1024 / D);
@@ -777,19 +779,22 @@ qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t s
   if (blocks > pages::kThreadsAtMost / (64 * (d.whole ? pages::kWholeWaves : pages::kWaves)) || joins > pages::kThreadsAtMost / 256)
     return fail(QCF_ERR_UNSUPPORTED, "page attention: too many rows");
   const dim3 grid((unsigned)blocks);
-#define QCF_LAUNCH(RT, MODE, WAVES, WHOLE) page_attn_kernel<T, D, RT, MODE, WAVES, WHOLE, EIGHT><<<grid, dim3(64 * WAVES), 0, st>>>(a)
-#define QCF_ROWS(MODE)                                                                          \
+#define QCF_LAUNCH(RT, MODE, WAVES, WHOLE, HEADS) \
+  page_attn_kernel<T, D, RT, MODE, WAVES, WHOLE, EIGHT, HEADS><<<grid, dim3(64 * WAVES), 0, st>>>(a)
+#define QCF_ROWS(MODE, HEADS)                                                                   \
   do {                                                                                          \
     if (d.row_tiles == 1) {                                                                     \
-      if (d.whole) QCF_LAUNCH(1, MODE, pages::kWholeWaves, true);                               \
-      else QCF_LAUNCH(1, MODE, pages::kWaves, false);                                           \
+      if (d.whole) QCF_LAUNCH(1, MODE, pages::kWholeWaves, true, 1);                            \
+      else if (HEADS > 1 && d.heads > 1) QCF_LAUNCH(1, MODE, pages::kWaves, false, HEADS);      \
+      else QCF_LAUNCH(1, MODE, pages::kWaves, false, 1);                                        \
     } else {                                                                                    \
-      QCF_LAUNCH(2, MODE, pages::kWaves, false);                                                \
+      QCF_LAUNCH(2, MODE, pages::kWaves, false, 1);                                             \
     }                                                                                           \
   } while (0)
-  if (a.list) QCF_ROWS(kList);
-  else if (a.n_q == 1) QCF_ROWS(kOne);
-  else QCF_ROWS(kSeveral);
+  constexpr int kHeads = EIGHT ? 256 / D : 1;
+  if (a.list) QCF_ROWS(kList, 1);
+  else if (a.n_q == 1) QCF_ROWS(kOne, kHeads);
+  else QCF_ROWS(kSeveral, kHeads);
 #undef QCF_ROWS
 #undef QCF_LAUNCH
   QCF_TRY_LAUNCH("page attention");

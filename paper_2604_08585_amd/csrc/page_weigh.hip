@@ -24,9 +24,9 @@ struct WeighArgs {
 // 73.0, 72.5 and 95; 73.1.)
 constexpr int at_once(bool eight, int row_tiles) { return eight && row_tiles == 1 ? 3 : 2; }
 
-template <typename T, int D, int RT, bool EIGHT>
-struct Weigher : Walk<T, D, RT, kSeveral, pages::kWaves, EIGHT> {
-  typedef Walk<T, D, RT, kSeveral, pages::kWaves, EIGHT> W;
+template <typename T, int D, int RT, bool EIGHT, int HEADS>
+struct Weigher : Walk<T, D, RT, kSeveral, pages::kWaves / HEADS, EIGHT> {
+  typedef Walk<T, D, RT, kSeveral, pages::kWaves / HEADS, EIGHT> W;
   typedef typename W::Tile Tile;
   static constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.925963033500e-8f;
   const WeighArgs& w_;
@@ -117,13 +117,14 @@ struct Weigher : Walk<T, D, RT, kSeveral, pages::kWaves, EIGHT> {
   }
 };
 
-template <typename T, int D, int RT, bool EIGHT>
+// (HEADS: KV heads that the waves take side by side)
+template <typename T, int D, int RT, bool EIGHT, int HEADS>
 __global__ __launch_bounds__(64 * pages::kWaves, at_once(EIGHT, RT)) void page_weigh_kernel(WeighArgs args) {
-  typedef Weigher<T, D, RT, EIGHT> W;
+  typedef Weigher<T, D, RT, EIGHT, HEADS> W;
   const PageAttnArgs& a = args.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t r = blockIdx.x / a.inner;
-  const int g = (int)(blockIdx.x - r * a.inner);
+  const int g = (int)(blockIdx.x - r * a.inner) * HEADS + wave % HEADS;
   W w(args, lane, g);
   const Contexts all = contexts_of(a, lane);
   const int64_t from = r * all.range, to = from + all.range;
@@ -137,7 +138,7 @@ __global__ __launch_bounds__(64 * pages::kWaves, at_once(EIGHT, RT)) void page_w
       // (each wave's tokens are its own, and so are their weights: the second block of rows finds what the first one stored)
       for (int block = 0; block < args.row_blocks; ++block) {
         w.prepare(here.x, block * 16 * RT, begin, end, (int)tokens);
-        w.run(begin + wave * W::W::kTokens, block == 0);
+        w.run(begin + wave / HEADS * W::W::kTokens, block == 0);
       }
     }
     here.start += here.grains + all.pad;
@@ -156,17 +157,22 @@ qcf_status launch_page_weigh(const qcf_layer_desc& L, const qcf_page_cache& c, c
   fill_args(w.a, L, c, scales, n_q, q, seen);
   w.a.contexts = B;
   w.a.rows = rows;
-  w.a.inner = L.n_kv_heads;
+  w.stride = (int64_t)c.max_pages * c.page_size;
+  const int heads = pages::side_by_side(L, c, scales ? 1 : 2, (double)B * (double)w.stride * L.n_kv_heads * 2 * L.head_dim);
+  w.a.inner = L.n_kv_heads / heads;
   w.a.least = pages::least_range(L);
   w.a.pad = 0;
   w.lse = lse; w.old = old; w.alpha = alpha; w.beta = beta;
   w.weights = weights;
-  w.stride = (int64_t)c.max_pages * c.page_size;
   w.row_blocks = (rows + 16 * row_tiles - 1) / (16 * row_tiles);
   const int64_t ranges = ((int64_t)B * ((w.stride + pages::kGrain - 1) / pages::kGrain) + w.a.least - 1) / w.a.least;
-  w.a.slots = (int)std::min<int64_t>(ranges, std::max(1, at_once(scales != nullptr, row_tiles) * compute_unit_count() / L.n_kv_heads));
+  w.a.slots = (int)std::min<int64_t>(ranges, std::max(1, at_once(scales != nullptr, row_tiles) * compute_unit_count() / w.a.inner));
   const dim3 grid((unsigned)((int64_t)w.a.slots * w.a.inner)), block(64 * pages::kWaves);
-#define QCF_LAUNCH(T, D, RT, EIGHT) page_weigh_kernel<T, D, RT, EIGHT><<<grid, block, 0, st>>>(w)
+#define QCF_LAUNCH(T, D, RT, EIGHT)                                                          \
+  do {                                                                                       \
+    if (heads > 1) page_weigh_kernel<T, D, RT, EIGHT, EIGHT ? 256 / D : 1><<<grid, block, 0, st>>>(w); \
+    else page_weigh_kernel<T, D, RT, EIGHT, 1><<<grid, block, 0, st>>>(w);                   \
+  } while (0)
 #define QCF_ROWS(T, D, EIGHT) do { if (row_tiles == 1) QCF_LAUNCH(T, D, 1, EIGHT); else QCF_LAUNCH(T, D, 2, EIGHT); } while (0)
 #define QCF_PAGES(T, D) do { if (scales) QCF_ROWS(T, D, true); else QCF_ROWS(T, D, false); } while (0)
   if (L.dtype == QCF_DTYPE_BF16) {

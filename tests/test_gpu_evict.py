@@ -54,14 +54,23 @@ def _weigh(p, q, seen, lse, old, alpha, beta, w):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("case", [
+    # (tables for long contexts: heads of a token that lie next to each other are read side by side)
+    ("bf16", 32, 8, 128, 16, "token", [[731], [32], [0], [2000]], [730, 0, 0, 1900]), ("bf16", 16, 4, 64, 32, "token", [[97, 98], [640, 0]], [96, 600]),
+    ("f32", 8, 4, 64, 64, "token", [[300]], None), ("f32", 4, 2, 128, 16, "token", [[5, 6, 7], [33, 0, 80]], [4, 79]),
+    ("bf16", 64, 2, 128, 16, "token", [[77, 78]], [76])])
+def test_weights_of_heads_side_by_side(case):
+    test_weights(case, True, 524288)
+
+
 @pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("case", WEIGHTS)
-def test_weights(case, eight):
+def test_weights(case, eight, room=0):
     dtype, H, Hkv, D, page, order, seen, old = case
     rng = np.random.default_rng(41)
     seen = np.array(seen, dtype=np.int32)
     B, n_q = seen.shape
-    p = _paged(eight, rng, shape(H, Hkv, D, dtype), page, np.maximum(seen.max(1), 1).tolist(), order)
+    p = _paged(eight, rng, shape(H, Hkv, D, dtype), page, np.maximum(seen.max(1), 1).tolist(), order, width=room // page // B or None)
     say("weigh", dtype, H, Hkv, D, "page", page, order, "8 bits" if eight else "", "seen", seen.tolist() if seen.size < 40 else seen.shape)
     q = normal(rng, (B, n_q, H, D), dtype, 1.5)
     k, _ = _values(p)
