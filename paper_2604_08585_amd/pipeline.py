@@ -408,33 +408,55 @@ class PagedLayer:
     ws_linear: Optional[torch.Tensor]
     ws_select: Optional[torch.Tensor]
     ws_attn: Optional[torch.Tensor]
+    # with a budget (evict):
+    budget: int = 0                # tokens that a request's heads keep
+    spare: Optional[qb.PageCache] = None           # pages of the same pools that kept tokens move to
+    weights: Optional[torch.Tensor] = None         # [B, H_kv, tokens] float32: the attention that each token got so far
+    spare_weights: Optional[torch.Tensor] = None
+    kept: Optional[torch.Tensor] = None            # [B, H_kv, budget] int32: the tokens that the last eviction kept
+    ws_evict: Optional[torch.Tensor] = None
+    more: int = 0                  # room behind a request that has been cut down
 
 
 def paged_layer(L: DeviceLayer, more: int, page_size: int = 16, new: int = 1, keep: int = 0, first: int = 1,
-                last: int = 1) -> PagedLayer:
+                last: int = 1, eight: bool = False, budget: int = 0) -> PagedLayer:
     """The fused cache of a layer in pages, with room for `more` tokens behind every request's context (which begins at position
     0).  keep > 0: each new row's attention is cut down to that many pages for each KV head, the first `first` and the last `last`
-    among them; the pages' bounds are kept for that."""
+    among them; the pages' bounds are kept for that.  eight: pages of 8-bit elements, with a scale for every 16 tokens of a head.
+    budget > 0: steps add up the attention that tokens get, and `evict` cuts every request down to that many tokens to a head, with room
+    for `more` behind them (not with keep: weights need attention over all pages)."""
     if more < 0 or not 0 <= new <= 16:
         raise ValueError(f"room for {more} tokens, steps of {new} (at most 16)")
     if keep < 0 or min(first, last) < 0 or (keep and first + last > keep):
         raise ValueError(f"{keep} pages kept, the first {first} and the last {last} among them")
+    if budget < 0 or (budget and keep):
+        raise ValueError(f"a budget of {budget} tokens, attention cut down to {keep} pages: one of the two")
     desc, dev, dt = L.desc, L.k_fused.device, L.k_fused.dtype
     H, Hkv, d = desc.n_q_heads, desc.n_kv_heads, desc.head_dim
-    counts = [-(-(n + more) // page_size) for n in L.ctx_lens]
-    width, n_pages = max(counts + [1]), max(sum(counts), 1)
-    table = np.full((L.B, width), -1, dtype=np.int32)
+    # (a budget: two tables, which take turns; both have room for a request's context and for the budget)
+    counts = [-(-(max(n, budget) + more) // page_size) for n in L.ctx_lens]
+    width, tables = max(counts + [1]), []
     at = 0
-    for b, n in enumerate(counts):
-        table[b, :n] = np.arange(at, at + n, dtype=np.int32)
-        at += n
+    for _ in range(2 if budget else 1):
+        table = np.full((L.B, width), -1, dtype=np.int32)
+        for b, n in enumerate(counts):
+            n = n if not tables else -(-(budget + more) // page_size)
+            table[b, :n] = np.arange(at, at + n, dtype=np.int32)
+            at += n
+        tables.append(torch.from_numpy(table).to(dev))
+    n_pages = max(at, 1)
     empty = lambda *s, dtype=dt: torch.empty(*s, dtype=dtype, device=dev)
-    pool = lambda: empty(n_pages, Hkv, page_size, d).transpose(1, 2)      # a head's tokens of a page together: read 4 to 5 % faster
-    cache = qb.page_cache(pool(), pool(), empty(n_pages, Hkv, 2, d) if keep else None, torch.from_numpy(table).to(dev))
+    # a head's tokens of a page together: read 4 to 5 % faster, in 8 bits 16 %
+    pool = lambda: empty(n_pages, Hkv, page_size, d, dtype=torch.float8_e4m3fn if eight else dt).transpose(1, 2)
+    k, v, bounds = pool(), pool(), empty(n_pages, Hkv, 2, d) if keep else None
+    scales = empty(n_pages, Hkv, 2, page_size // 16, dtype=torch.float32) if eight else None
+    described = lambda t: qb.page8_cache(k, v, scales, bounds, t, dt) if eight else qb.page_cache(k, v, bounds, t)
+    cache = described(tables[0])
     rows = L.B * new
     held = torch.tensor(L.ctx_lens, dtype=torch.int32, device=dev)
     step = torch.arange(new, dtype=torch.int32, device=dev)
     qkv = empty(rows, (H + 2 * Hkv) * d)
+    attn_bytes = qb.qcf_page8_attn_workspace_bytes if eight else qb.qcf_page_attn_workspace_bytes
     P = PagedLayer(
         desc=desc, B=L.B, new=new, keep=keep, first=first, last=last, cache=cache, room=[more] * L.B, held=held, seen=held[:, None] + 1 + step,
         pos=(held[:, None] + step).flatten(), row_off=torch.arange(L.B + 1, dtype=torch.int64, device=dev) * new, qkv=qkv,
@@ -443,15 +465,20 @@ def paged_layer(L: DeviceLayer, more: int, page_size: int = 16, new: int = 1, ke
         lse=empty(L.B, new, H, dtype=torch.float32),
         ws_linear=_ws(qb.qcf_linear_workspace_bytes(desc, rows, desc.d_model, (H + 2 * Hkv) * d), dev),
         ws_select=_ws(qb.qcf_page_select_workspace_bytes(desc, cache, L.B, new, keep), dev) if keep else None,
-        ws_attn=_ws(qb.qcf_page_attn_workspace_bytes(desc, cache, L.B, new, keep), dev))
-    qb.qcf_page_append(desc, cache, L.B, None, L.k_fused[:L.total_ctx], L.v_fused[:L.total_ctx], L.ctx_off, L.total_ctx,
-                       torch.zeros_like(held), None, None)
+        ws_attn=_ws(attn_bytes(desc, cache, L.B, new, keep), dev))
+    if budget:
+        P.budget, P.more, P.spare = budget, more, described(tables[1])
+        P.weights, P.spare_weights = (torch.zeros(L.B, Hkv, cache.tokens, dtype=torch.float32, device=dev) for _ in range(2))
+        P.kept = torch.full((L.B, Hkv, budget), -1, dtype=torch.int32, device=dev)
+        P.ws_evict = _ws(qb.qcf_page_evict_workspace_bytes(desc, cache, L.B, budget), dev)
+    append = qb.qcf_page8_append if eight else qb.qcf_page_append
+    append(desc, cache, L.B, None, L.k_fused[:L.total_ctx], L.v_fused[:L.total_ctx], L.ctx_off, L.total_ctx, torch.zeros_like(held), None, None)
     return P
 
 
 def decode_step(P: PagedLayer, x: torch.Tensor, w_qkv: torch.Tensor) -> torch.Tensor:
     """One layer's attention for `new` tokens behind each request: x [B * new, d_model] (normed hidden states) is projected, keys and
-    values go into the cache, rotated on the way, and the queries attend.  Returns o [B, new, H, d].  Lengths and positions live
+    values go into the cache, rotated on the way, and the queries attend (with a budget, what they attend to is added to the tokens' weights).  Returns o [B, new, H, d].  Lengths and positions live
     on the device and are not moved: call `advance` after a step's last layer, or to accept fewer tokens than were drafted.  A step
     for which a request has no room is refused; steps that a captured graph replays are not, so who replays them counts."""
     rows, dm = P.B * P.new, P.desc.d_model
@@ -463,10 +490,14 @@ def decode_step(P: PagedLayer, x: torch.Tensor, w_qkv: torch.Tensor) -> torch.Te
         raise ValueError(f"a step of {P.new} tokens to a request, room for {room} more behind request {P.room.index(room)}")
     qb.qcf_linear(P.desc, x, rows, dm, w_qkv, P.qkv.shape[1], None, P.qkv, P.ws_linear)
     q, k, v = P.parts
-    qb.qcf_page_append(P.desc, P.cache, P.B, q, k, v, P.row_off, rows, P.held, P.pos, P.q.flatten(0, 1))
+    eight = P.cache.scales is not None
+    append, attn = (qb.qcf_page8_append, qb.qcf_page8_attn) if eight else (qb.qcf_page_append, qb.qcf_page_attn)
+    append(P.desc, P.cache, P.B, q, k, v, P.row_off, rows, P.held, P.pos, P.q.flatten(0, 1))
     if P.keep:
         qb.qcf_page_select(P.desc, P.cache, P.B, P.new, P.q, P.seen, P.keep, P.first, P.last, P.pages, P.ws_select)
-    qb.qcf_page_attn(P.desc, P.cache, P.B, P.new, P.q, P.seen, P.pages, P.keep, P.o, P.lse, P.ws_attn)
+    attn(P.desc, P.cache, P.B, P.new, P.q, P.seen, P.pages, P.keep, P.o, P.lse, P.ws_attn)
+    if P.budget:
+        qb.qcf_page_weigh(P.desc, P.cache, P.B, P.new, P.q, P.seen, P.lse, P.held, 1.0, 1.0, P.weights)
     return P.o
 
 
@@ -496,3 +527,21 @@ def advance(P: PagedLayer, tokens: Union[int, Sequence[int], torch.Tensor]) -> N
             t += operator.index(tokens)
     if not capturing:
         P.room = [room - t for t, room in zip(taken, P.room)]
+
+
+def evict(P: PagedLayer, first: int = 1, last: int = 1) -> None:
+    """Every head of every request keeps the first `first`, the last `last` and the heaviest other tokens, P.budget in all (P.kept: their
+    numbers among those that were held); there is room for as many tokens behind them as paged_layer was asked for.  Positions go on.
+    Between steps, not inside a captured graph: the layer's pages and weights change places with the spare ones, and a step that was
+    captured before would go on with those that the tokens left (capture it again)."""
+    if not P.budget:
+        raise ValueError("paged_layer(budget=...) makes the pages that tokens move to")
+    if min(first, last) < 0 or first + last > P.budget:
+        raise ValueError(f"the first {first} and the last {last} tokens, {P.budget} in all")
+    if P.held.is_cuda and torch.cuda.is_current_stream_capturing():
+        raise ValueError("an eviction moves a layer to other pages and cannot be recorded into a graph")
+    qb.qcf_page_evict(P.desc, P.cache, P.B, P.held, P.weights, P.budget, first, last, P.spare, P.kept, P.spare_weights, P.held, P.ws_evict)
+    P.cache, P.spare = P.spare, P.cache
+    P.weights, P.spare_weights = P.spare_weights, P.weights
+    P.seen.copy_(P.held[:, None] + 1 + torch.arange(P.new, dtype=torch.int32, device=P.held.device))
+    P.room = [P.more] * P.B

@@ -1,0 +1,129 @@
+"""Decoding behind a fused layer in 8-bit pages and with a budget (pipeline.paged_layer, decode_step, evict) against the oracle's chain on
+what the pages hold: projection, rotation, attention, weights, the tokens that stay.
+
+Tolerances.  Keys and values are read back from the pages, so attention and weights are held to those of the values that are stored: the
+largest absolute error that the fused layer's own attention is held to (2e-2 in bf16, 1e-4 in float32).  A stored element is off by half a
+step of e4m3, 2^-4 of its value, or 2^-10 of a scale that is at most 2 / 448 of the block's largest element; in bf16 2^-8 of the projection more.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import qcf_oracle as orc
+from paper_2604_08585_amd import inputs, pipeline
+from gpu_util import DEV, quantizer, to_np
+
+pytestmark = pytest.mark.gpu
+
+
+def _held(P, b, n):
+    """Keys and values [H_kv, n, d] that request b holds."""
+    c = P.cache
+    k, v, _, table = c.tensors
+    page = c.desc.page_size
+    at = table[b].cpu().numpy()[np.arange(n) // page], np.arange(n) % page
+    out = []
+    for i, pool in enumerate((k, v)):
+        x = pool.view(torch.uint8).cpu().view(pool.dtype).float().double().numpy()[at] if c.scales is not None else to_np(pool)[at]
+        if c.scales is not None:
+            x = x * c.scales[:, :, i].double().cpu().numpy()[at[0], :, at[1] // 16][..., None]
+        out.append(x.transpose(1, 0, 2))
+    return out
+
+
+@pytest.mark.parametrize("cfg,new,eight,budget,keep", [
+    (0, 1, True, 0, 0), (0, 3, True, 0, 0), (0, 1, False, 200, 0), (0, 2, True, 64, 0), (2, 1, True, 0, 12), (2, 1, True, 500, 0), (2, 2, False, 300, 0)])
+def test_decoding(cfg, new, eight, budget, keep):
+    wl = inputs.make_config(cfg, orc.PlantOps())
+    sh = wl.shape
+    L = pipeline.upload(wl, DEV)
+    pipeline.fuse_layer(L)
+    steps = 6
+    P = pipeline.paged_layer(L, more=3 * new, new=new, eight=eight, budget=budget, keep=keep) if budget else \
+        pipeline.paged_layer(L, more=steps * new, new=new, eight=eight, keep=keep)
+    dt, quant = inputs.torch_dtype(sh.dtype), quantizer(sh.dtype)
+    rng = np.random.default_rng(50 + cfg)
+    H, Hkv, D, G = sh.n_q_heads, sh.n_kv_heads, sh.head_dim, sh.n_q_heads // sh.n_kv_heads
+    tol = 2e-2 if sh.dtype == "bf16" else 1e-4
+    w = np.asarray(wl.w_qkv, dtype=np.float64)
+    # what has gone into the pages is the fused cache, to half a step
+    torch.cuda.synchronize()
+    off = np.concatenate([[0], np.cumsum(L.ctx_lens)])
+    for b in range(L.B):
+        for x, fused in zip(_held(P, b, L.ctx_lens[b]), (to_np(L.k_fused), to_np(L.v_fused))):
+            ref = fused[off[b]:off[b + 1]].transpose(1, 0, 2)
+            assert np.all(np.abs(x - ref) <= (2.0 ** -4 * np.abs(ref) + 2.0 ** -10 * 2 / 448 * np.abs(ref).max() if eight else 0.0))
+    held, start = list(L.ctx_lens), list(L.ctx_lens)
+    weights = [np.zeros((Hkv, n)) for n in held]
+    for step in range(steps):
+        x = quant(rng.standard_normal((L.B * new, sh.d_model)))
+        o = to_np(pipeline.decode_step(P, torch.from_numpy(x).to(device=DEV, dtype=dt), L.w_qkv))
+        torch.cuda.synchronize()
+        y = quant(x @ w.T).reshape(L.B, new, H + 2 * Hkv, D)
+        for b in range(L.B):
+            k, v = _held(P, b, held[b] + new)
+            pos = start[b] + step * new + np.arange(new)
+            q = to_np(P.q)[b]
+            assert np.abs(q - quant(orc.rope_at(y[b, :, :H], pos, sh.rope_base, sh.rope_style))).max() <= tol * max(1.0, np.abs(q).max())
+            fresh = np.stack([orc.rope_at(y[b, :, H:H + Hkv], pos, sh.rope_base, sh.rope_style), y[b, :, H + Hkv:]])
+            for got, ref in zip((k, v), fresh):
+                ref = ref.transpose(1, 0, 2)
+                step_of = np.abs(got).max()
+                assert np.all(np.abs(got[:, held[b]:] - ref) <= (2.0 ** -4 if eight else 0.0) * np.abs(ref) + 2.0 ** -7 * np.abs(ref) + 2.0 ** -10 / 100 * step_of + tol)
+            weights[b] = np.concatenate([weights[b], np.zeros((Hkv, new))], axis=1)
+            for i in range(new):
+                n = held[b] + i + 1
+                for h in range(H):
+                    rows = np.arange(n)
+                    if keep:
+                        p = P.pages[b, i, h // G].cpu().numpy()
+                        rows = np.concatenate([np.arange(16 * j, min(16 * j + 16, n)) for j in p[p >= 0]])
+                    z = k[h // G][rows] @ q[i, h] / math.sqrt(D)
+                    e = np.exp(z - z.max())
+                    assert np.abs(o[b, i, h] - e @ v[h // G][rows] / e.sum()).max() <= tol, (step, b, i, h)
+                    weights[b][h // G][rows] += e / e.sum()
+            if budget:
+                got = P.weights[b, :, :held[b] + new].double().cpu().numpy()
+                # (queries and keys are the kernel's own: a logit is off by (d + 5) 2^-24 sum |q k| / sqrt(d), a weight by as much of itself)
+                terms = np.abs(k).sum(-1).max() * np.abs(q).max() / math.sqrt(D)
+                assert np.all(np.abs(got - weights[b]) <= ((D + 5) * 2.0 ** -23 * terms + 2.0 ** -18) * weights[b])
+        pipeline.advance(P, new)
+        held = [n + new for n in held]
+        if budget and step == 2:
+            before = [_held(P, b, held[b]) for b in range(L.B)]
+            was = P.weights.cpu().numpy()
+            pipeline.evict(P, 2, 16)
+            torch.cuda.synchronize()
+            for b in range(L.B):
+                want = orc.page_evict(was[b], held[b], budget, 2, 16)
+                assert np.array_equal(P.kept[b].cpu().numpy(), want)
+                n = min(held[b], budget)
+                assert P.held[b].item() == n and P.seen[b].cpu().tolist() == [n + 1 + i for i in range(new)]
+                for x, ref in zip(_held(P, b, n), before[b]):
+                    ref = np.stack([ref[g][want[g, :n]] for g in range(Hkv)])
+                    assert np.all(np.abs(x - ref) <= (2.0 ** -10 * 2 / 448 * np.abs(ref).max() if eight else 0.0))
+                weights[b] = np.stack([weights[b][g, want[g, :n]] for g in range(Hkv)])
+                held[b] = n
+            assert P.room == [3 * new] * L.B
+    if budget:
+        with pytest.raises(ValueError, match="room for"):
+            pipeline.decode_step(P, torch.from_numpy(x).to(device=DEV, dtype=dt), L.w_qkv)
+
+
+def test_an_eviction_is_not_recorded_into_a_graph():
+    wl = inputs.make_config(0, orc.PlantOps())
+    L = pipeline.upload(wl, DEV)
+    pipeline.fuse_layer(L)
+    P = pipeline.paged_layer(L, more=4, budget=32)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    x = torch.zeros(1, device=DEV)
+    with torch.cuda.graph(graph):
+        x += 1
+        with pytest.raises(ValueError, match="recorded"):
+            pipeline.evict(P)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert x.item() == 1.0
