@@ -21,7 +21,7 @@ extern "C" {
 
 /* The cache is described by a qcf_page_cache whose k and v point to codes (16-byte aligned; strides are in elements, which are bytes
  * here, and multiples of 16) and by
- *   scales  DEVICE [n_pages, H_kv, 2, page_size / 16] float32: those of a page's keys (0) and of its values (1).
+ *   scales  DEVICE [n_pages, H_kv, 2, page_size / 16] float32: those of a page's keys (0) and of its values (1); at most 2^31 of them.
  * Bounds, if there are any, have the layer's type; qcf_page_select takes such a cache as it is (it reads bounds and table only). */
 
 /* qcf_page_append for 8-bit pages: the same arguments, and scales.  Keys are turned in float32 and rounded once, to their codes.  A

@@ -724,8 +724,10 @@ qcf_status qcf_page_attn(const qcf_layer_desc* desc, const qcf_page_cache* cache
 
 // ---- 8-bit pages ---------------------------------------------------------------------
 // `scales` of a cache, and what its codes ask of the strides
-static qcf_status check_eight(const qcf_page_cache* c, const float* scales, const char* name) {
+static qcf_status check_eight(const qcf_layer_desc* desc, const qcf_page_cache* c, const float* scales, const char* name) {
   QCF_TRY(need_idx_ptr(scales, name));
+  if ((double)c->n_pages * desc->n_kv_heads * (2 * c->page_size / QCF_PAGE8_BLOCK) > 2147483647.0)
+    return fail(QCF_ERR_UNSUPPORTED, "n_pages %d: more than 2^31 scales", c->n_pages);
   if ((c->page_stride | c->slot_stride | c->head_stride) & 15)
     return fail(QCF_ERR_INVALID_ARG, "page, slot and head strides of 8-bit pages must be multiples of 16");
   return QCF_OK;
@@ -738,7 +740,7 @@ qcf_status qcf_page8_append(const qcf_layer_desc* desc, const qcf_page_cache* ca
   bool empty = true;
   QCF_TRY(check_append(desc, cache, B, q, q_stride, k, k_stride, v, v_stride, row_off_dev, total_rows, len_dev, pos_dev, q_out, &empty));
   if (empty) return QCF_OK;
-  QCF_TRY(check_eight(cache, scales, "scales"));
+  QCF_TRY(check_eight(desc, cache, scales, "scales"));
   return launch_page8_append(*desc, *cache, scales, B, q, q_stride, k, k_stride, v, v_stride, row_off_dev, total_rows, len_dev, pos_dev,
                              q_out, (hipStream_t)stream);
 }
@@ -755,7 +757,7 @@ qcf_status qcf_page8_attn(const qcf_layer_desc* desc, const qcf_page_cache* cach
   bool empty = true;
   QCF_TRY(check_page_attn(desc, cache, B, n_q, q, seen_dev, pages, n_keep, o_out, lse_out, &empty));
   if (empty) return QCF_OK;
-  QCF_TRY(check_eight(cache, scales, "scales"));
+  QCF_TRY(check_eight(desc, cache, scales, "scales"));
   QCF_TRY(need_ws(workspace, workspace_bytes, page8_attn_workspace(*desc, *cache, B, n_q, n_keep)));
   return launch_page8_attn(*desc, *cache, scales, B, n_q, q, seen_dev, pages, n_keep, o_out, lse_out, workspace, (hipStream_t)stream);
 }
@@ -769,7 +771,7 @@ qcf_status qcf_page_weigh(const qcf_layer_desc* desc, const qcf_page_cache* cach
   if (!std::isfinite(alpha) || !std::isfinite(beta)) return fail(QCF_ERR_INVALID_ARG, "alpha and beta must be finite");
   if (empty) return QCF_OK;
   QCF_TRY(check_page_pointers(cache, false));
-  if (scales) QCF_TRY(check_eight(cache, scales, "scales"));
+  if (scales) QCF_TRY(check_eight(desc, cache, scales, "scales"));
   QCF_TRY(need_ptr(q, "q"));
   QCF_TRY(need_idx_ptr(seen_dev, "seen_dev"));
   QCF_TRY(need_idx_ptr(lse, "lse"));
@@ -807,8 +809,8 @@ qcf_status qcf_page_evict(const qcf_layer_desc* desc, const qcf_page_cache* cach
   QCF_TRY(check_page_pointers(cache, false));
   QCF_TRY(check_page_pointers(to, false));
   if (scales) {
-    QCF_TRY(check_eight(cache, scales, "scales"));
-    QCF_TRY(check_eight(to, to_scales, "to_scales"));
+    QCF_TRY(check_eight(desc, cache, scales, "scales"));
+    QCF_TRY(check_eight(desc, to, to_scales, "to_scales"));
   }
   QCF_TRY(need_idx_ptr(len_dev, "len_dev"));
   QCF_TRY(need_ptr(weights, "weights"));

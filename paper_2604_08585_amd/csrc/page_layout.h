@@ -51,7 +51,7 @@ struct Division {
 // Workgroups of four waves that a compute unit holds at once.  (8-bit heads of 64 leave room for a third: 64 requests of 4K to 12K tokens 111
 // us, 122 with two.  Those of 128 would spill 27 registers: 234 us, 203 with two.)
 constexpr int at_once(int head_dim, int row_tiles, bool eight) {
-  return head_dim == 64 ? (eight && row_tiles == 1 ? 3 : 2) : row_tiles == 1 ? 2 : 1;
+  return head_dim == 64 ? (eight && row_tiles == 1 ? 3 : 2) : row_tiles == 1 || eight ? 2 : 1;
 }
 
 // KV heads whose rows lie next to each other and are read side by side, by the waves of a workgroup: 256 bytes in a row, as a row of bf16
@@ -99,10 +99,10 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   // request of 16384 tokens 18.1 and 16.0, 8 of up to 4096 16.6 and 16.4, 64 of up to 1024 19.2 and 16.6, of up to 4096 32.6 and 43.7.
   const int64_t longest = (int64_t)(n_keep && n_keep < c.max_pages ? n_keep : c.max_pages) * c.page_size;
   const double read = (double)d.contexts * (double)longest * L.n_kv_heads * 2 * L.head_dim * elem;
-  // (8-bit heads of 128: one tile always; the registers of two leave a compute unit one workgroup, which waits for its chains of products.
-  // 64 / 8 heads, us, two tiles and one: four drafts of 8 requests of 2K to 6K tokens 36.5 and 35.6, of 64 of 4K to 12K 347 and 300, of one
-  // of 128K 93 and 79; 16 drafts of 4 requests of up to 8K 65 and 60.  Heads of 64, 8 drafts of 32 requests: 63 and 74.)
-  d.row_tiles = d.rows > 16 && read > kShared && !(elem == 1 && L.head_dim == 128) ? 2 : 1;
+  // (8-bit heads of 128: from more bytes on.  64 / 8 heads, us, two tiles and one: four drafts of 8 requests of 2K to 6K tokens 37.5 and 35.2,
+  // of 64 of 4K to 12K 247 and 292, of one of 128K 73.8 and 78.5; 32 / 8 heads, 8 drafts of 16 requests of up to 8K 60.3 and 62.7.)
+  const bool wide8 = elem == 1 && L.head_dim == 128;
+  d.row_tiles = d.rows > 16 && read > (wide8 ? 8.0 : 1.0) * kShared ? 2 : 1;
   d.row_blocks = (d.rows + 16 * d.row_tiles - 1) / (16 * d.row_tiles);
   d.inner = L.n_kv_heads * d.row_blocks;
   // (several new rows with heads of 128: 51.0 us with a head to a workgroup, 55.6, for four drafts of 16 requests of up to 8K tokens)

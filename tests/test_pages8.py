@@ -92,6 +92,8 @@ def test_other_refusals():
                      (dict(to_w=FAKE + 4), b"to_weights")]:
         assert _evict(d, c, **kw) == 1 and word in _said(), kw
     assert _evict(d, c, B=65536) == 2
+    for call in (_append, _attn, _weigh, _evict):
+        assert call(d, _raw(n_pages=1 << 29)) == 2 and b"2^31 scales" in _said(), call
     long = _raw(max_pages=1 << 16)
     need = qb.load_library().qcf_page_evict_workspace_bytes(C.byref(d), C.byref(long), 3, 4)
     assert need > 0 and _evict(d, long, B=3, have=need - 1) == 3 and _evict(d, long, B=3, ws=None) == 3
@@ -99,7 +101,7 @@ def test_other_refusals():
 
 
 def test_launches_of_more_than_2_to_the_32_threads_are_refused():
-    wide = _raw(max_pages=1 << 26, n_pages=1 << 30)
+    wide = _raw(max_pages=1 << 26, n_pages=1 << 26)
     assert _append(_desc(n_q_heads=1, n_kv_heads=1), _raw(slot_stride=64), rows=1 << 30, ks=64, vs=64, q=None, out=None) == 2 and b"too many rows" in _said()
     assert _evict(_desc(), wide, B=64, keep=1 << 30, to=wide) == 2 and b"too many rows" in _said()
     d = _desc(n_q_heads=128, n_kv_heads=128)
