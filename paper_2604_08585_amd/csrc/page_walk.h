@@ -247,7 +247,7 @@ struct Walk {
     return r;
   }
   // a lane's offset stays one register, added by the load itself to what the wave shares
-  __device__ __forceinline__ static void in_32_bits(uint32_t& offset) { asm volatile("" : "+v"(offset)); }
+  __device__ __forceinline__ static void in_32_bits(uint32_t& offset) { asm("" : "+v"(offset)); }
   __device__ __forceinline__ void load_keys(Tile& t, const Where& r) const {
     const uint32_t stride = (uint32_t)a.c.slot_stride * kSize;
     uint32_t lane_at = col * stride + 16 * quad;
