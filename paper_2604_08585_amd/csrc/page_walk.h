@@ -826,7 +826,7 @@ qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t s
   constexpr int kHeads = EIGHT ? 256 / D : 1;
   if (a.list) QCF_ROWS(kList, 1);
   else if (a.n_q == 1) QCF_ROWS(kOne, kHeads);
-  else QCF_ROWS(kSeveral, kHeads);
+  else QCF_ROWS(kSeveral, D == 64 ? kHeads : 1);
 #undef QCF_ROWS
 #undef QCF_LAUNCH
   QCF_TRY_LAUNCH("page attention");

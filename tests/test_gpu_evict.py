@@ -355,14 +355,15 @@ def test_decoding_goes_on_behind_an_eviction():
                 assert np.abs(to_np(o)[b, 0, h] - ref).max() <= 2.0 ** -8 * np.abs(ref).max() + 1e-4 * np.abs(v).max()
 
 
-def test_weights_and_eviction_replay_from_a_captured_graph():
+@pytest.mark.parametrize("width", [64, 8192])                 # (8192: heads side by side, the choice divided over the GPU)
+def test_weights_and_eviction_replay_from_a_captured_graph(width):
     rng = np.random.default_rng(47)
-    p = Paged8(rng, shape(8, 2, 128, "bf16"), 16, [300, 90], width=64)
+    p = Paged8(rng, shape(8, 2, 128, "bf16"), 16, [300, 90], width=width)
     t = Paged8(rng, shape(8, 2, 128, "bf16"), 16, [64, 64])
     q = torch.from_numpy(normal(rng, (2, 1, 8, 128), "bf16")).to(device=DEV, dtype=p.dt)
     seen, lens = i32([[300], [90]]), i32([300, 90])
     o, lse = torch.empty_like(q), torch.empty(2, 1, 8, device=DEV)
-    w, to_w, kept, to_len = torch.zeros(2, 2, 1024, device=DEV), torch.zeros(2, 2, 64, device=DEV), torch.zeros(2, 2, 50, dtype=torch.int32, device=DEV), i32([0, 0])
+    w, to_w, kept, to_len = torch.zeros(2, 2, 16 * width, device=DEV), torch.zeros(2, 2, 64, device=DEV), torch.zeros(2, 2, 50, dtype=torch.int32, device=DEV), i32([0, 0])
     ws = torch.empty(max(1, qb.qcf_page8_attn_workspace_bytes(p.desc, p.cache, 2, 1, 0)), dtype=torch.uint8, device=DEV)
     ev = torch.empty(max(1, qb.qcf_page_evict_workspace_bytes(p.desc, p.cache, 2, 50)), dtype=torch.uint8, device=DEV)
 
@@ -390,3 +391,40 @@ def test_weights_and_eviction_replay_from_a_captured_graph():
         torch.cuda.synchronize()
         for got, want in zip(results(), eager[i]):
             assert torch.equal(got, want), i
+
+
+def test_calls_on_two_streams_at_once():
+    """Weights and evictions of two layers, each with buffers of its own, on two streams: the bits of the calls alone."""
+    rng = np.random.default_rng(49)
+    jobs = []
+    for eight, lens, width in ((True, [9000, 4000, 77], 2560), (False, [15000], 1024)):
+        p = _paged(eight, rng, shape(32, 8, 128, "bf16"), 16, lens, width=width)
+        t = _paged(eight, rng, shape(32, 8, 128, "bf16"), 16, [600] * len(lens))
+        q = torch.from_numpy(normal(rng, (len(lens), 1, 32, 128), "bf16")).to(device=DEV, dtype=p.dt)
+        z = lambda *n, dt=torch.float32: torch.zeros(*n, dtype=dt, device=DEV)
+        B = len(lens)
+        lse = torch.full((B, 1, 32), 9.0, device=DEV)
+        ws = torch.empty(max(1, qb.qcf_page_evict_workspace_bytes(p.desc, p.cache, B, 600)), dtype=torch.uint8, device=DEV)
+        jobs.append(dict(p=p, t=t, q=q, lens=i32(lens), lse=lse, w=z(B, 8, 16 * width), to_w=z(B, 8, t.cache.tokens), kept=z(B, 8, 600, dt=torch.int32),
+                         to_len=z(B, dt=torch.int32), ws=ws, s=torch.cuda.Stream()))
+
+    def run(j):
+        B = len(j["q"])
+        qb.qcf_page_weigh(j["p"].desc, j["p"].cache, B, 1, j["q"], j["lens"], j["lse"], None, 0.0, 1.0, j["w"])
+        qb.qcf_page_evict(j["p"].desc, j["p"].cache, B, j["lens"], j["w"], 600, 1, 64, j["t"].cache, j["kept"], j["to_w"], j["to_len"], j["ws"])
+
+    results = lambda j: [x.clone() for x in (j["w"], j["kept"], j["to_w"], j["to_len"], j["t"].kd.view(torch.uint8), j["t"].vd.view(torch.uint8))]
+    alone = []
+    for j in jobs:
+        run(j)
+        torch.cuda.synchronize()
+        alone.append(results(j))
+        j["w"].zero_(), j["kept"].zero_()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for j in jobs:
+            with torch.cuda.stream(j["s"]):
+                run(j)
+    torch.cuda.synchronize()
+    for j, want in zip(jobs, alone):
+        assert all(torch.equal(a, b) for a, b in zip(results(j), want))
