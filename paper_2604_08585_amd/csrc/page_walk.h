@@ -817,16 +817,18 @@ qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t s
   do {                                                                                          \
     if (d.row_tiles == 1) {                                                                     \
       if (d.whole) QCF_LAUNCH(1, MODE, pages::kWholeWaves, true, 1);                            \
-      else if (HEADS > 1 && d.heads > 1) QCF_LAUNCH(1, MODE, pages::kWaves, false, HEADS);      \
+      else if ((HEADS) > 1 && d.heads > 1) QCF_LAUNCH(1, MODE, pages::kWaves, false, HEADS);      \
       else QCF_LAUNCH(1, MODE, pages::kWaves, false, 1);                                        \
     } else {                                                                                    \
       QCF_LAUNCH(2, MODE, pages::kWaves, false, 1);                                             \
     }                                                                                           \
   } while (0)
-  constexpr int kHeads = EIGHT ? 256 / D : 1;
+  // (pages::side_by_side; several new rows with heads of 128 take one at a time)
+  constexpr int kHeads = EIGHT ? 256 / D : 1, kHeadsOfSeveral = D == 64 ? kHeads : 1;
+  if (d.heads != 1 && d.heads != (a.n_q == 1 ? kHeads : kHeadsOfSeveral)) return fail(QCF_ERR_UNSUPPORTED, "page attention: %d heads side by side", d.heads);
   if (a.list) QCF_ROWS(kList, 1);
   else if (a.n_q == 1) QCF_ROWS(kOne, kHeads);
-  else QCF_ROWS(kSeveral, D == 64 ? kHeads : 1);
+  else QCF_ROWS(kSeveral, kHeadsOfSeveral);
 #undef QCF_ROWS
 #undef QCF_LAUNCH
   QCF_TRY_LAUNCH("page attention");

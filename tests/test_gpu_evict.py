@@ -233,8 +233,10 @@ def test_choice_among_many_tokens(B, Hkv, tokens, keep, first, last, kind):
     say("choice", B, Hkv, tokens, keep, first, last, kind)
     kept = torch.full((B, Hkv, keep), 77, dtype=torch.int32, device=DEV)
     to_len = i32([0] * B)
-    for _ in range(2):                                                     # (the second call finds the first one's workspace in the allocator)
-        qb.qcf_page_evict(desc, cache, B, i32(lens), torch.from_numpy(w).to(DEV), keep, first, last, to, kept, None, to_len)
+    for fill in (0.0, math.nan):                                           # (what the workspace holds does not matter)
+        ws = torch.full((qb.qcf_page_evict_workspace_bytes(desc, cache, B, keep) // 4 + 1,), fill, device=DEV).view(torch.uint8)
+        kept.fill_(77)
+        qb.qcf_page_evict(desc, cache, B, i32(lens), torch.from_numpy(w).to(DEV), keep, first, last, to, kept, None, to_len, ws)
     torch.cuda.synchronize()
     for b in range(B):
         for g in range(Hkv):

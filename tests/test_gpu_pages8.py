@@ -246,6 +246,25 @@ def test_attention(case, wide):
     _attend_and_check(p, rng, seen)
 
 
+@pytest.mark.parametrize("case", ATTENTIONS)
+def test_results_do_not_depend_on_what_the_workspace_holds(case):
+    dtype, H, Hkv, D, page, order, seen = case
+    rng = np.random.default_rng(40)
+    seen = np.array(seen, dtype=np.int32)
+    B, n_q = seen.shape
+    p = Paged8(rng, shape(H, Hkv, D, dtype), page, np.maximum(seen.max(1), 1).tolist(), order, width=131072 // page)
+    q = torch.from_numpy(normal(rng, (B, n_q, H, D), dtype)).to(device=DEV, dtype=p.dt)
+    n = qb.qcf_page8_attn_workspace_bytes(p.desc, p.cache, B, n_q, 0)
+    got = []
+    for fill in (0.0, math.nan, 1e19):
+        ws = torch.full((n // 4 + 1,), fill, device=DEV).view(torch.uint8)
+        o, lse = torch.full_like(q, 7.0), torch.full((B, n_q, H), 7.0, device=DEV)
+        qb.qcf_page8_attn(p.desc, p.cache, B, n_q, q, i32(seen), None, 0, o, lse, ws)
+        torch.cuda.synchronize()
+        got.append((o, lse))
+    assert all(torch.equal(o, got[0][0]) and torch.equal(z, got[0][1]) for o, z in got[1:])
+
+
 @pytest.mark.parametrize("width", [9, 8192])
 def test_attention_does_not_read_what_is_not_seen(width):
     """NaN codes behind `seen`, in page 0 (read in the place of absent pages) and in pages of no request; scales there that are NaN or
