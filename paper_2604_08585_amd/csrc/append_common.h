@@ -19,6 +19,7 @@ struct AppendArgs {
   void* q_out;
   qcf_page_cache c;
   int B, H, Hkv, log2_page;
+  int log2_unit;                  // tokens of a unit: a page's, or fewer
   double neg2_over_d_log2base;
 };
 
@@ -47,7 +48,7 @@ __device__ __forceinline__ u32x4 rounded(const float* f) {
 __device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 __device__ __forceinline__ float largest(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// Request of a unit: units of request b start at row_off[b] / page + 2 b (pages::append_units), so that no sum over the requests
+// Request of a unit (a page that gets rows): units of request b start at row_off[b] / page + 2 b (pages::append_units), so that no sum over the requests
 // stands in front of the rows.  Every wave looks for the last request that starts at or before the unit; offsets and lengths of the
 // first 64 are on their way together.
 struct Request {
@@ -56,7 +57,7 @@ struct Request {
 };
 __device__ __forceinline__ Request request_of(const AppendArgs& a, int64_t unit, int lane) {
   auto clamped = [&](int64_t off) { return min(max(off, (int64_t)0), a.total_rows); };
-  auto first = [&](int b, int64_t off) { return (off >> a.log2_page) + 2 * (int64_t)b; };
+  auto first = [&](int b, int64_t off) { return (off >> a.log2_unit) + 2 * (int64_t)b; };
   const int mine = min(lane, a.B - 1);
   const int64_t off = clamped(a.row_off[mine]), next = clamped(a.row_off[mine + 1]);
   const int len = a.len[mine];
@@ -99,7 +100,7 @@ inline AppendArgs append_args(const qcf_layer_desc& L, const qcf_page_cache& c, 
   a.row_off = row_off; a.total_rows = total_rows; a.len = len; a.pos = pos; a.q_out = q_out;
   a.c = c;
   a.B = B; a.H = L.n_q_heads; a.Hkv = L.n_kv_heads;
-  a.log2_page = __builtin_ctz((unsigned)c.page_size);
+  a.log2_page = a.log2_unit = __builtin_ctz((unsigned)c.page_size);
   a.neg2_over_d_log2base = -2.0 / L.head_dim * std::log2(L.rope_base);
   return a;
 }

@@ -19,9 +19,11 @@ __device__ __forceinline__ float2 exact_turn(double positions, double turns) {
   return make_float2(__builtin_fmaf(-sn, d, cn), __builtin_fmaf(cn, d, sn));
 }
 
-// One workgroup per (page that gets rows, `heads` KV heads of it).  A wave takes a block of 16 tokens of a head as a whole, keys and
+// One workgroup per (unit that gets rows, `heads` KV heads of it): a block of 16 tokens, or, where the pages have bounds, a page.  A wave takes a block of 16 tokens of a head as a whole, keys and
 // values: it turns the keys, finds both largest elements, hence the scales, and stores the codes.  Where the block has tokens already
-// and its scale grows, these are rounded again.  (heads: 1, 2 or 4; the waves of a head take its blocks in turn.)
+// and its scale grows, these are rounded again.  (heads: 1, 2 or 4; the waves of a head take its blocks in turn.)  Bound by memory where many
+// rows come (36K rows, 32 / 8 heads of 128: 158 us, 5.1 TB/s of what is read and written, a copy's rate), by the chain offsets -> table and
+// positions -> factors -> largest elements -> codes where few do (8 rows 6.1 us).
 template <typename T, int D, int STYLE>
 __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, float* __restrict__ scales, int heads) {
   constexpr int VEC = Elem<T>::kVec, TPR = D / 2 / VEC, PAIRS = D / 2, ROWS = 4096 / D;
@@ -37,8 +39,8 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, float* 
   const Request rq = request_of(a, unit, lane);
   const double turns = exp2(a.neg2_over_d_log2base * (double)(tid % PAIRS)) * 0.15915494309189533577;
   const int64_t page = a.c.page_size, len = rq.len;
-  const int64_t p = (len >> a.log2_page) + unit - rq.unit0;
-  const int64_t t0 = max(p * page, len), t1 = min((p + 1) * page, len + (rq.r1 - rq.r0));
+  const int64_t begin = ((len >> a.log2_unit) + unit - rq.unit0) << a.log2_unit, p = begin >> a.log2_page;
+  const int64_t t0 = max(begin, len), t1 = min(begin + ((int64_t)1 << a.log2_unit), len + (rq.r1 - rq.r0));
   if (t0 >= t1) return;
   const int64_t phys = p >= 0 && p < a.c.max_pages ? a.c.table[(int64_t)rq.b * a.c.max_pages + p] : -1;
   const bool there = phys >= 0 && phys < a.c.n_pages;
@@ -201,10 +203,10 @@ qcf_status launch_page8_append(const qcf_layer_desc& L, const qcf_page_cache& c,
                                int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                const int64_t* row_off, int64_t total_rows, const int32_t* len, const int32_t* pos, void* q_out,
                                hipStream_t st) {
-  const AppendArgs a = append_args(L, c, B, q, q_stride, k, k_stride, v, v_stride, row_off, total_rows, len, pos, q_out);
-  const int64_t units = pages::append_units(c, B, total_rows);
-  int heads = 1;
-  while (heads < kWaves && L.n_kv_heads % (2 * heads) == 0 && units * (L.n_kv_heads / (2 * heads)) >= compute_unit_count()) heads *= 2;
+  AppendArgs a = append_args(L, c, B, q, q_stride, k, k_stride, v, v_stride, row_off, total_rows, len, pos, q_out);
+  if (!c.bounds) a.log2_unit = __builtin_ctz((unsigned)kBlock);
+  const int64_t units = pages::append8_units(c, B, total_rows);
+  const int heads = pages::append8_heads(L, c, B, total_rows);
   const int64_t blocks = units * (L.n_kv_heads / heads);
   if (blocks > pages::kThreadsAtMost / kThreads) return fail(QCF_ERR_UNSUPPORTED, "page append: too many rows");
 #define QCF_LAUNCH(T, D, S) append8_kernel<T, D, S><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, scales, heads)

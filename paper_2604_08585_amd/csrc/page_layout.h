@@ -5,7 +5,7 @@
 #include <stddef.h>
 #include <algorithm>
 
-#include "qcf_pages.h"
+#include "qcf_pages8.h"
 
 #ifdef __HIP__
 #define QCF_BOTH __host__ __device__ inline
@@ -160,6 +160,22 @@ inline int append_heads(const qcf_layer_desc& L, const qcf_page_cache& c, int64_
     heads *= 2;
   const int64_t groups = units * (L.n_kv_heads / heads);
   if (heads > 1 && 2 * groups > 5 * cus && groups < 4 * cus) heads /= 2;
+  return heads;
+}
+
+// Units of an append to 8-bit pages: blocks of 16 tokens; where the pages have bounds, which one workgroup joins, pages.  (24K rows of 16
+// requests in pages of 256, 32 / 8 heads of 128: 118 us, 133 in parts of 64 tokens, 145 in pages.)
+inline int append8_tokens(const qcf_page_cache& c) { return c.bounds ? c.page_size : QCF_PAGE8_BLOCK; }
+inline int64_t append8_units(const qcf_page_cache& c, int32_t B, int64_t total_rows) { return total_rows / append8_tokens(c) + 2 * (int64_t)B; }
+// KV heads of its workgroup: they share (cos, sin) and whole rows; fewer give a short call, and long pages, more workgroups.  us with one, two
+// and four (32 / 8 heads of 128, blocks): 36K rows 191, 156, 158; 256 requests of one row 18.5, 12.8, 10.7; 32 of 50 to 100 17.2, 15.1, 15.2 (two by this
+// rule); 500 rows 9.6, 9.6, 10.4 (one); pages with 256 rows, 24K of them 145, 173, 233 (one), with 64, 6K of them 42.8, 42.3, 55.7 (one).
+inline int append8_heads(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int64_t total_rows) {
+  const int tokens = append8_tokens(c);
+  const int64_t workgroups = (total_rows / tokens + B) * L.n_kv_heads;               // that get rows, about, one head each
+  const int64_t wanted = (int64_t)(tokens > QCF_PAGE8_BLOCK && total_rows > 16 * (int64_t)B ? 8 : 2) * compute_unit_count();
+  int heads = 1;
+  while (heads < kWaves && L.n_kv_heads % (2 * heads) == 0 && workgroups / (2 * heads) >= wanted) heads *= 2;
   return heads;
 }
 

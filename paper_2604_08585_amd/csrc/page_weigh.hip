@@ -1,9 +1,10 @@
 // What the tokens of a cache in pages get of their requests' attention, added up step by step.
 //
-// The softmax's sums are known (lse), so a token's weights need its logits and nothing of other tokens: one pass over the keys.  A wave
-// takes 32 tokens (16 in float32) at a time as in the attention, whose division of the contexts this has too; a lane owns a row and four
-// tokens of each 16, the sum over the rows goes over the 16 lanes of a quad.  Bound by memory: the keys, and 8 bytes of weights to a token
-// and KV head.
+// w_t = alpha w_t + beta sum_rows exp(z_t - lse): the softmax's sums are known, so a token's weights need its logits and nothing of other tokens,
+// and one pass over the keys is all.  A wave takes 32 tokens (16 in float32) at a time as in the attention, whose division of the contexts
+// this has too, with the product's operands the other way round: a lane owns a token and four rows of each 16, so that the sum over the
+// rows is three additions and two exchanges between lanes (136 us with a row to a lane, four exchanges to each token; 129).  Bound by memory: the
+// keys, and 8 bytes of weights to a token and KV head: 16 requests of 1K to 16K tokens in bf16 72 us, 4.7 TB/s; 64 of 4K to 12K in 8 bits 130, 4.5.
 #include "page_walk.h"
 
 namespace qcf {
