@@ -88,22 +88,24 @@ def _check_append(p, want, q64, q_out, largest, rotated):
         assert np.array_equal(b[pages], bounds[pages], equal_nan=True)
 
 
+@pytest.mark.parametrize("bounds", [True, False])             # (a workgroup to a page, or to a block of it)
 @pytest.mark.parametrize("case", APPENDS)
-def test_append(case):
+def test_append(case, bounds):
     dtype, H, Hkv, D, style, page, order, requests, rotated = case
     rng = np.random.default_rng(21)
     lens, new = [h for h, _ in requests], [n for _, n in requests]
-    p = Paged8(rng, shape(H, Hkv, D, dtype, style), page, [h + n for h, n in requests], order)
+    p = Paged8(rng, shape(H, Hkv, D, dtype, style), page, [h + n for h, n in requests], order, bounds=bounds)
     _check_append(p, *_append(p, rng, lens, new, rotated), rotated)
 
 
+@pytest.mark.parametrize("bounds", [True, False])
 @pytest.mark.parametrize("size", [2.0 ** -40, 1e-3, 30.0, 1e4])
-def test_scales_that_grow_and_scales_that_stay(size):
+def test_scales_that_grow_and_scales_that_stay(size, bounds):
     """Rows far smaller or larger than what their block holds: the block's tokens stay as they are, or are rounded again."""
     for dtype, D, page, order in [("bf16", 128, 16, "token"), ("f32", 64, 64, "head"), ("f32", 128, 32, "token"), ("bf16", 64, 128, "head")]:
         rng = np.random.default_rng(22)
         lens, new = [5, 15, 47, 16, 1, 30], [1, 1, 3, 2, 15, 40]
-        p = Paged8(rng, shape(4, 2, D, dtype), page, [h + n for h, n in zip(lens, new)], order)
+        p = Paged8(rng, shape(4, 2, D, dtype), page, [h + n for h, n in zip(lens, new)], order, bounds=bounds)
         _check_append(p, *_append(p, rng, lens, new, False, size=size), False)
 
 
@@ -114,14 +116,15 @@ def test_append_at_far_positions(dtype, far):
     _check_append(p, *_append(p, rng, [3], [37], True, far), True)
 
 
-def test_steps_of_one_token_fill_a_page():
+@pytest.mark.parametrize("bounds", [True, False])
+def test_steps_of_one_token_fill_a_page(bounds):
     """A page token by token, then again from its middle (drafts that were not accepted): the oracle's bits after every step."""
     rng = np.random.default_rng(24)
     sh = shape(8, 2, 128, "bf16")
-    p = Paged8(rng, sh, 16, [0, 0], spare=5)
+    p = Paged8(rng, sh, 16, [0, 0], spare=5, bounds=bounds)
     p.table = np.array([[3], [1]], dtype=np.int32)
     p.scales[:] = np.nan                                                         # (a new page may hold anything)
-    p.upload()
+    p.upload(bounds)
     held = 0
     for step in range(24):
         lens = [held, held]
@@ -135,13 +138,14 @@ def test_steps_of_one_token_fill_a_page():
         held = 7 if step == 14 else held + 1
 
 
-def test_append_drops_what_has_no_page_and_takes_special_values():
+@pytest.mark.parametrize("bounds", [True, False])
+def test_append_drops_what_has_no_page_and_takes_special_values(bounds):
     rng = np.random.default_rng(25)
     for dtype, D in [("bf16", 128), ("f32", 64)]:
         sh = shape(4, 2, D, dtype)
         p = Paged8(rng, sh, 16, [64, 64, 20], spare=2)
         p.table[0, 1], p.table[1, 2] = -1, 10 ** 6                               # pages that are not there
-        p.upload()
+        p.upload(bounds)
         lens, new = [10, 30, 60], [30, 40, 9]                                    # the second and the third run beyond the table
         M = sum(new)
         rows = normal(rng, (M + 2, 8 * D), dtype)
@@ -166,13 +170,43 @@ def test_append_without_queries_or_bounds_and_queries_in_place():
     assert torch.equal(p.kd.view(torch.uint8), plain.kd.view(torch.uint8)) and torch.equal(p.sd, plain.sd) and torch.equal(q, out)
 
 
-def test_append_of_many_requests():
+@pytest.mark.parametrize("bounds", [True, False])
+def test_append_of_many_requests(bounds):
     rng = np.random.default_rng(27)
     lens = rng.integers(0, 40, 700).tolist()
     new = [int(n) if n < 5 else 0 for n in rng.integers(0, 7, 700)]
     new[333] = 50
-    p = Paged8(rng, shape(2, 1, 64, "f32"), 16, [h + n for h, n in zip(lens, new)])
+    p = Paged8(rng, shape(2, 1, 64, "f32"), 16, [h + n for h, n in zip(lens, new)], bounds=bounds)
     _check_append(p, *_append(p, rng, lens, new, True), True)
+
+
+def test_lengths_below_nothing_and_rows_behind_the_last_request():
+    """Rows that would be tokens before the first are not stored, their queries are turned; offsets beyond the rows are cut off."""
+    rng = np.random.default_rng(28)
+    for bounds in (True, False):
+        sh = shape(4, 2, 64, "bf16")
+        p = Paged8(rng, sh, 32, [64, 64], bounds=bounds)
+        k, v, q = (torch.from_numpy(normal(rng, (40, n, 64), "bf16")).to(device=DEV, dtype=p.dt) for n in (2, 2, 4))
+        pos, out = i32(np.arange(40) + 100), torch.full_like(q, 7.0)
+        qb.qcf_page8_append(p.desc, p.cache, 2, q, k, v, i64([0, 30, 90]), 38, i32([-21, 31]), pos, out)
+        torch.cuda.synchronize()
+        want = orc.rope_at(to_np(q)[:38], np.arange(38) + 100, sh.rope_base, 0)
+        assert np.abs(to_np(out)[:38] - want).max() <= 2.0 ** -8 * np.abs(want).max() + 1e-5 and (out[38:] == 7.0).all()
+        kc, vc, s = p.got()
+        turned = orc.rope_at(to_np(k)[:38], np.arange(38) + 100, sh.rope_base, 0)
+        # request 0: rows 21 to 29 are tokens 0 to 8; request 1: rows 30 to 37 are tokens 31 to 38
+        for b, first, rows in ((0, 0, range(21, 30)), (1, 31, range(30, 38))):
+            for i, m in enumerate(rows):
+                page, slot = p.table[b, (first + i) // 32], (first + i) % 32
+                for g in range(2):
+                    sv, sk = s[page, g, 1, slot // 16], s[page, g, 0, slot // 16]
+                    assert np.array_equal(vc[page, slot, g], orc.e4m3(to_np(v)[m, g] / sv))
+                    assert np.abs(kc[page, slot, g] * sk - turned[m, g]).max() <= 2.0 ** -4 * np.abs(turned[m, g]).max() + 1e-5
+        used = {(p.table[b, t // 32], t % 32) for b, ts in ((0, range(9)), (1, range(31, 39))) for t in ts}
+        for page in range(len(kc)):
+            for slot in range(32):
+                if (page, slot) not in used and (page, slot // 16) != (p.table[1, 0], 1):       # (that block's scale may have grown)
+                    assert np.array_equal(kc[page, slot], p.codes[0][page, slot]) and np.array_equal(vc[page, slot], p.codes[1][page, slot])
 
 
 # ------------------------------------------------------------------ attention
