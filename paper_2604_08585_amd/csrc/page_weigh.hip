@@ -20,10 +20,10 @@ struct WeighArgs {
   int row_blocks;
 };
 
-// Workgroups on a compute unit, of four waves each: three where the registers allow it.  (64 requests of 4K to 12K tokens in 8 bits, two rows
-// each, us: 132 with two, 129 with three, 139 with four, whose registers spill; tiles of 64 tokens 133 with two.  16 of 1K to 16K in bf16:
-// 73.0, 72.5 and 95; 73.1.)
-constexpr int at_once(bool eight, int row_tiles) { return eight && row_tiles == 1 ? 3 : 2; }
+// Workgroups on a compute unit, of four waves each: as many as the registers allow.  (us, 8 bits, 64 requests of 4K to 12K tokens: heads of 128
+// 132 with two, 129 with three, 139 with four, whose registers spill, 133 with two and tiles of 64 tokens; heads of 64 92 with two, 79.9 with
+// three, 76.0 with four.  16 of 1K to 16K in bf16: 73.0, 72.5 and 95.)
+constexpr int at_once(bool eight, int row_tiles, int head_dim) { return !eight || row_tiles > 1 ? 2 : head_dim == 64 ? 4 : 3; }
 
 template <typename T, int D, int RT, bool EIGHT, int HEADS>
 struct Weigher : Walk<T, D, RT, kSeveral, pages::kWaves / HEADS, EIGHT> {
@@ -120,7 +120,7 @@ struct Weigher : Walk<T, D, RT, kSeveral, pages::kWaves / HEADS, EIGHT> {
 
 // (HEADS: KV heads that the waves take side by side)
 template <typename T, int D, int RT, bool EIGHT, int HEADS>
-__global__ __launch_bounds__(64 * pages::kWaves, at_once(EIGHT, RT)) void page_weigh_kernel(WeighArgs args) {
+__global__ __launch_bounds__(64 * pages::kWaves, at_once(EIGHT, RT, D)) void page_weigh_kernel(WeighArgs args) {
   typedef Weigher<T, D, RT, EIGHT, HEADS> W;
   const PageAttnArgs& a = args.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -167,7 +167,7 @@ qcf_status launch_page_weigh(const qcf_layer_desc& L, const qcf_page_cache& c, c
   w.weights = weights;
   w.row_blocks = (rows + 16 * row_tiles - 1) / (16 * row_tiles);
   const int64_t ranges = ((int64_t)B * ((w.stride + pages::kGrain - 1) / pages::kGrain) + w.a.least - 1) / w.a.least;
-  w.a.slots = (int)std::min<int64_t>(ranges, std::max(1, at_once(scales != nullptr, row_tiles) * compute_unit_count() / w.a.inner));
+  w.a.slots = (int)std::min<int64_t>(ranges, std::max(1, at_once(scales != nullptr, row_tiles, L.head_dim) * compute_unit_count() / w.a.inner));
   const dim3 grid((unsigned)((int64_t)w.a.slots * w.a.inner)), block(64 * pages::kWaves);
 #define QCF_LAUNCH(T, D, RT, EIGHT)                                                          \
   do {                                                                                       \
