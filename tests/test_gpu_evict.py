@@ -159,22 +159,22 @@ def _evict(p, to, lens, w, keep, first, last, to_len=None):
     return kept, to_w, to_len
 
 
-@pytest.mark.parametrize("wide", [False, True])               # (a wide table: the choice is divided over the GPU)
+@pytest.mark.parametrize("wide,bounds", [(False, True), (True, True), (False, False), (True, False)])     # (a wide table: the choice is divided)
 @pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("case", EVICTIONS)
-def test_eviction(case, eight, wide):
+def test_eviction(case, eight, wide, bounds):
     dtype, H, Hkv, D, page, new_page, order, lens, keep, first, last = case
     rng = np.random.default_rng(44)
     B = len(lens)
     p = _paged(eight, rng, shape(H, Hkv, D, dtype), page, lens, order, width=40960 // page if wide else None)
-    t = _paged(eight, rng, shape(H, Hkv, D, dtype), new_page, [keep] * B, order)              # other pools, for pages of another size
+    t = _paged(eight, rng, shape(H, Hkv, D, dtype), new_page, [keep] * B, order, bounds=bounds)       # other pools, for pages of another size
     say("evict", dtype, H, Hkv, D, page, "->", new_page, "8 bits" if eight else "", "lens", lens[:8], "keep", keep)
     tokens = p.table.shape[1] * page
     w = np.exp(2 * rng.standard_normal((B, Hkv, tokens))).astype(np.float32)
     w[rng.random(w.shape) < 0.3] = 0.0                                                        # ties
     w[0, 0, 3:5] = np.nan
     before = t.got() if eight else (to_np(t.kd), to_np(t.vd))
-    b0 = to_np(t.bd)
+    b0 = to_np(t.bd) if bounds else None
     kept, to_w, to_len = _evict(p, t.cache, lens, torch.from_numpy(w).to(DEV), keep, first, last)
     k, v = _values(p)
     got = t.got() if eight else (to_np(t.kd), to_np(t.vd))
@@ -197,7 +197,7 @@ def test_eviction(case, eight, wide):
                     rows = orc.e4m3(rows / np.repeat(s, 16)[:n, None]) if n else rows
                 assert np.array_equal(got[which][dst, at, g], rows), (b, g, which)
             stored = got[0][dst, at, g] * (np.repeat(s0, 16)[:n, None] if eight and (s0 := got[2][dst[::16], g, 0, at[::16] // 16]) is not None else 1.0)
-            for page_of in range(-(-n // new_page)):
+            for page_of in range(-(-n // new_page) if bounds else 0):
                 mine = stored[page_of * new_page:(page_of + 1) * new_page]
                 bound = to_np(t.bd)[t.table[b, page_of], g]
                 assert np.array_equal(bound, np.stack([mine.min(0), mine.max(0)])), (b, g, page_of)
@@ -206,7 +206,7 @@ def test_eviction(case, eight, wide):
             page_id, at = t.table[b, j // new_page], j % new_page
             for which in range(2):
                 assert np.array_equal(got[which][page_id, at], before[which][page_id, at])
-        for x in t.table[b, -(-n // new_page):]:
+        for x in t.table[b, -(-n // new_page):] if bounds else ():
             assert np.array_equal(to_np(t.bd)[x], b0[x])
 
 
