@@ -802,8 +802,6 @@ qcf_status qcf_page_evict(const qcf_layer_desc* desc, const qcf_page_cache* cach
   if (n_first < 0 || n_last < 0) return fail(QCF_ERR_INVALID_ARG, "negative size");
   if ((int64_t)n_first + n_last > n_keep)
     return fail(QCF_ERR_INVALID_ARG, "n_first %d + n_last %d > n_keep %d", n_first, n_last, n_keep);
-  if (n_keep > (int64_t)to->max_pages * to->page_size)
-    return fail(QCF_ERR_INVALID_ARG, "n_keep %d, room for %lld tokens in the new table", n_keep, (long long)to->max_pages * to->page_size);
   if ((scales == nullptr) != (to_scales == nullptr)) return fail(QCF_ERR_INVALID_ARG, "scales and to_scales must both be given, or both be NULL");
   if (B == 0) return QCF_OK;
   QCF_TRY(check_page_pointers(cache, false));

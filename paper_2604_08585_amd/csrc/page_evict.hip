@@ -248,7 +248,10 @@ __global__ __launch_bounds__(256) void evict_kernel(EvictArgs a) {
     const int p = t >> a.log2_from;
     return t >= 0 && p < a.from.max_pages ? a.from.table[b * a.from.max_pages + p] : -1;
   };
-  auto new_page = [&](int j0) { return j0 < a.n_keep ? a.to.table[b * a.to.max_pages + (j0 >> a.log2_to)] : -1; };
+  auto new_page = [&](int j0) {
+    const int p = j0 >> a.log2_to;
+    return j0 < a.n_keep && p < a.to.max_pages ? a.to.table[b * a.to.max_pages + p] : -1;
+  };
   const int end = min(first + a.tokens, a.n_keep);
   for (int j0 = first + wave * kBlock; j0 < end; j0 += waves * kBlock) {
     const int t = number(j0), from = page_of(t), to = new_page(j0);
@@ -259,7 +262,7 @@ __global__ __launch_bounds__(256) void evict_kernel(EvictArgs a) {
     const int s = t & (a.from.page_size - 1), slot = j0 & (a.to.page_size - 1);
     const bool found = from >= 0 && from < a.from.n_pages, there = to >= 0 && to < a.to.n_pages;
     const int64_t src = found ? (from * a.from.page_stride + s * a.from.slot_stride + g * a.from.head_stride) * kSize : -1;
-    if (a.to_weights && lane < count)
+    if (a.to_weights && lane < count && j0 >> a.log2_to < a.to.max_pages)
       a.to_weights[(head * a.to.max_pages << a.log2_to) + j0 + lane] = found ? a.weights[(head * a.from.max_pages << a.log2_from) + t] : 0.f;
     if (there) {
       float scale[2] = {0.f, 0.f};

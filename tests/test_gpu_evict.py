@@ -285,6 +285,31 @@ def test_eviction_within_one_pool_and_what_is_not_there():
                         assert np.abs(y[dst, j % 16, g] - ref).max() <= (2.0 ** -4 * np.abs(ref).max() if eight else 0.0)
 
 
+def test_more_tokens_to_keep_than_the_new_table_has_room_for():
+    """n_keep beyond the room: requests that hold less move as a whole; what has no room is dropped, with its weights."""
+    for eight, bounds in ((False, True), (True, False), (True, True)):
+        rng = np.random.default_rng(50)
+        p = _paged(eight, rng, shape(4, 2, 64, "bf16"), 16, [40, 100])
+        t = _paged(eight, rng, shape(4, 2, 64, "bf16"), 16, [48, 48], bounds=bounds)            # three pages each
+        w = rng.random((2, 2, p.table.shape[1] * 16)).astype(np.float32)
+        behind = torch.full((2 * 2 * 48 + 64,), 7.0, device=DEV)                                # (weights, and what lies behind them)
+        kept, to_len = torch.full((2, 2, 70), 77, dtype=torch.int32, device=DEV), i32([0, 0])
+        qb.qcf_page_evict(p.desc, p.cache, 2, i32([40, 100]), torch.from_numpy(w).to(DEV), 70, 1, 5, t.cache, kept, behind[:192].view(2, 2, 48), to_len)
+        torch.cuda.synchronize()
+        assert to_len.cpu().tolist() == [40, 70] and (behind[192:] == 7.0).all()
+        to_w = behind[:192].view(2, 2, 48).cpu().numpy()
+        k = _values(p)[0]
+        got = orc.page8_values(t.got()[:2], t.got()[2])[0] if eight else to_np(t.kd)
+        for b, n in ((0, 40), (1, 70)):
+            want = orc.page_evict(w[b], [40, 100][b], 70, 1, 5)
+            assert np.array_equal(kept[b].cpu().numpy(), want)
+            for g in range(2):
+                m = min(n, 48)
+                assert np.array_equal(to_w[b, g, :m], w[b, g, want[g, :m]]) and np.all(to_w[b, g, m:] == 7.0)
+                rows = k[p.table[b, want[g, :m] // 16], want[g, :m] % 16, g]
+                assert np.abs(got[t.table[b, np.arange(m) // 16], np.arange(m) % 16, g] - rows).max() <= (2.0 ** -4 * np.abs(rows).max() if eight else 0.0)
+
+
 def test_decoding_goes_on_behind_an_eviction():
     """append, attention, weights and eviction in turn, in both formats: after each eviction attention is that over the kept tokens, each
     head its own, and the weights of kept tokens go on."""

@@ -86,7 +86,7 @@ def test_other_refusals():
                      (dict(beta=float("inf")), b"finite"), (dict(sc=FAKE + 1), b"scales")]:
         assert _weigh(d, c, **kw) == 1 and word in _said(), kw
     assert _weigh(d, c, n_q=17) == 2 and _weigh(d, c, B=65536) == 2
-    for kw, word in [(dict(B=-1), b"negative"), (dict(keep=0), b"positive"), (dict(keep=81), b"room"), (dict(first=3, last=2), b"n_keep"),
+    for kw, word in [(dict(B=-1), b"negative"), (dict(keep=0), b"positive"), (dict(first=3, last=2), b"n_keep"),
                      (dict(first=-1), b"negative"), (dict(sc=None), b"both"), (dict(to_sc=None), b"both"), (dict(lens=None), b"len_dev"),
                      (dict(w=None), b"weights"), (dict(kept=None), b"kept"), (dict(to_len=None), b"to_len"), (dict(to_w=FAKE), b"other memory"),
                      (dict(to_w=FAKE + 4), b"to_weights")]:
