@@ -33,9 +33,10 @@ def _held(P, b, n):
     return out
 
 
-@pytest.mark.parametrize("cfg,new,eight,budget,keep", [
-    (0, 1, True, 0, 0), (0, 3, True, 0, 0), (0, 1, False, 200, 0), (0, 2, True, 64, 0), (2, 1, True, 0, 12), (2, 1, True, 500, 0), (2, 2, False, 300, 0)])
-def test_decoding(cfg, new, eight, budget, keep):
+@pytest.mark.parametrize("cfg,new,eight,budget,keep,evict_after", [
+    (0, 1, True, 0, 0, ()), (0, 3, True, 0, 0, ()), (0, 1, False, 200, 0, (2,)), (0, 2, True, 64, 0, (2,)), (0, 1, True, 40, 0, (1, 3, 4)),
+    (0, 1, False, 30, 0, (0, 1, 4)), (2, 1, True, 0, 12, ()), (2, 1, True, 500, 0, (2,)), (2, 2, False, 300, 0, (2,))])
+def test_decoding(cfg, new, eight, budget, keep, evict_after):
     wl = inputs.make_config(cfg, orc.PlantOps())
     sh = wl.shape
     L = pipeline.upload(wl, DEV)
@@ -91,7 +92,7 @@ def test_decoding(cfg, new, eight, budget, keep):
                 assert np.all(np.abs(got - weights[b]) <= ((D + 5) * 2.0 ** -23 * terms + 2.0 ** -18) * weights[b])
         pipeline.advance(P, new)
         held = [n + new for n in held]
-        if budget and step == 2:
+        if step in evict_after:
             before = [_held(P, b, held[b]) for b in range(L.B)]
             was = P.weights.cpu().numpy()
             pipeline.evict(P, 2, 16)
@@ -107,7 +108,7 @@ def test_decoding(cfg, new, eight, budget, keep):
                 weights[b] = np.stack([weights[b][g, want[g, :n]] for g in range(Hkv)])
                 held[b] = n
             assert P.room == [3 * new] * L.B
-    if budget:
+    if evict_after == (2,):
         with pytest.raises(ValueError, match="room for"):
             pipeline.decode_step(P, torch.from_numpy(x).to(device=DEV, dtype=dt), L.w_qkv)
 

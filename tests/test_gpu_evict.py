@@ -455,3 +455,47 @@ def test_calls_on_two_streams_at_once():
     torch.cuda.synchronize()
     for j, want in zip(jobs, alone):
         assert all(torch.equal(a, b) for a, b in zip(results(j), want))
+
+
+def test_two_graphs_that_share_workspaces_take_turns():
+    """Two captured steps over different requests, attention divided and the choice too, replayed in turn with eager calls between them."""
+    rng = np.random.default_rng(51)
+    jobs = []
+    for lens in ([3000, 50], [700, 900, 4000]):
+        B = len(lens)
+        p = Paged8(rng, shape(32, 8, 128, "bf16"), 16, lens, width=4096)
+        t = Paged8(rng, shape(32, 8, 128, "bf16"), 16, [256] * B)
+        q = torch.from_numpy(normal(rng, (B, 1, 32, 128), "bf16")).to(device=DEV, dtype=p.dt)
+        z = lambda *n, dt=torch.float32: torch.zeros(*n, dtype=dt, device=DEV)
+        jobs.append(dict(p=p, t=t, q=q, lens=i32(lens), o=torch.empty_like(q), lse=z(B, 1, 32), w=z(B, 8, 65536), to_w=z(B, 8, 256),
+                         kept=z(B, 8, 200, dt=torch.int32), to_len=z(B, dt=torch.int32)))
+    need = max(max(qb.qcf_page8_attn_workspace_bytes(j["p"].desc, j["p"].cache, len(j["q"]), 1, 0),
+                   qb.qcf_page_evict_workspace_bytes(j["p"].desc, j["p"].cache, len(j["q"]), 200)) for j in jobs)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+
+    def run(j):
+        p, B = j["p"], len(j["q"])
+        qb.qcf_page8_attn(p.desc, p.cache, B, 1, j["q"], j["lens"], None, 0, j["o"], j["lse"], ws)
+        qb.qcf_page_weigh(p.desc, p.cache, B, 1, j["q"], j["lens"], j["lse"], None, 0.0, 1.0, j["w"])
+        qb.qcf_page_evict(p.desc, p.cache, B, j["lens"], j["w"], 200, 1, 20, j["t"].cache, j["kept"], j["to_w"], j["to_len"], ws)
+
+    results = lambda j: [x.clone() for x in (j["o"], j["lse"], j["w"], j["kept"], j["to_w"], j["to_len"], j["t"].kd.view(torch.uint8), j["t"].sd)]
+    graphs, want = [], []
+    for j in jobs:
+        run(j)
+        torch.cuda.synchronize()
+        want.append(results(j))
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run(j)
+        graphs.append(g)
+    for turn in range(3):
+        for i in (0, 1):
+            jobs[i]["o"].fill_(2.0), jobs[i]["kept"].fill_(2), jobs[i]["w"].fill_(2.0)
+            jobs[i]["w"][want[i][2] == 0] = 0.0
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(results(jobs[i]), want[i])), (turn, i)
+            run(jobs[1 - i])
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(results(jobs[1 - i]), want[1 - i])), (turn, i)
