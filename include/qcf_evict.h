@@ -39,7 +39,8 @@ qcf_status qcf_page_weigh(const qcf_layer_desc* desc, const qcf_page_cache* cach
  * weights), and to_len[b] (may be len) the number of tokens.  Slots of `to` behind them are left as they were.
  * `to` may lie in the same pools and have pages of another size; the pages that it lists must be none of the pages that `cache` lists for
  * these requests, and each once only.  Tokens of pages that are not there must not be among the first len[b] (they move as zeros);
- * what pages of `to` that are not there should get is dropped, and what goes beyond its max_pages (to_len counts it).  Bounds of `to`, if it has any, are made anew; `cache` needs none.
+ * what pages of `to` that are not there should get is dropped, and what goes beyond its max_pages (to_len counts it).  Bounds of `to`,
+ * if it has any, are made anew; `cache` needs none.
  * 8-bit pages (scales and to_scales, both or neither): a block of `to` gets the scale that qcf_page8_append would give its tokens. */
 size_t qcf_page_evict_workspace_bytes(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_keep);
 qcf_status qcf_page_evict(const qcf_layer_desc* desc, const qcf_page_cache* cache, const float* scales, int32_t B,

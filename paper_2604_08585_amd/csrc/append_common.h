@@ -48,8 +48,8 @@ __device__ __forceinline__ u32x4 rounded(const float* f) {
 __device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 __device__ __forceinline__ float largest(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// Request of a unit (a page that gets rows): units of request b start at row_off[b] / page + 2 b (pages::append_units), so that no sum over the requests
-// stands in front of the rows.  Every wave looks for the last request that starts at or before the unit; offsets and lengths of the
+// Request of a unit (a page that gets rows): units of request b start at row_off[b] / page + 2 b (pages::append_units), so that no sum
+// over the requests stands in front of the rows.  Every wave looks for the last request that starts at or before the unit; offsets and lengths of the
 // first 64 are on their way together.
 struct Request {
   int b;

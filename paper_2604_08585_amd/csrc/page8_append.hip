@@ -19,10 +19,10 @@ __device__ __forceinline__ float2 exact_turn(double positions, double turns) {
   return make_float2(__builtin_fmaf(-sn, d, cn), __builtin_fmaf(cn, d, sn));
 }
 
-// One workgroup per (unit that gets rows, `heads` KV heads of it): a block of 16 tokens, or, where the pages have bounds, a page.  A wave takes a block of 16 tokens of a head as a whole, keys and
-// values: it turns the keys, finds both largest elements, hence the scales, and stores the codes.  Where the block has tokens already
-// and its scale grows, these are rounded again.  (heads: 1, 2 or 4; the waves of a head take its blocks in turn.)  Bound by memory where many
-// rows come (36K rows, 32 / 8 heads of 128: 158 us, 5.1 TB/s of what is read and written, a copy's rate), by the chain offsets -> table and
+// One workgroup per (unit that gets rows, `heads` KV heads of it): a block of 16 tokens, or, where the pages have bounds, a page.  A wave
+// takes a block for one head as a whole, keys and values: it turns the keys, finds both largest elements, hence the scales, and stores
+// the codes.  Where the block has tokens already and its scale grows, these are rounded again.  (heads: 1, 2 or 4; the waves of a head
+// take its blocks in turn.)  Bound by memory where many rows come (36K rows, 32 / 8 heads of 128: 158 us, 5.1 TB/s of what is read and written, a copy's rate), by the chain offsets -> table and
 // positions -> factors -> largest elements -> codes where few do (8 rows 6.1 us).
 template <typename T, int D, int STYLE>
 __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, float* __restrict__ scales, int heads) {

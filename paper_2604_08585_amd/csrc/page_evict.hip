@@ -143,7 +143,8 @@ __global__ __launch_bounds__(kThreadsOf) void top_count_kernel(TopArgs a) {
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const bool mine = (there >> i & 1) && (LEVEL == 0 || key[i] >> kShift[LEVEL == 0 ? 0 : LEVEL - 1] == prefix >> kShift[LEVEL == 0 ? 0 : LEVEL - 1]);
+    constexpr int kFound = kShift[LEVEL == 0 ? 0 : LEVEL - 1];
+    const bool mine = (there >> i & 1) && (LEVEL == 0 || key[i] >> kFound == prefix >> kFound);
     const uint32_t digit = key[i] >> kShift[LEVEL] & (kBins - 1);
     // (keys that are all alike, weights of 0 above all, are counted at once)
     const uint64_t all = __ballot(mine);
@@ -328,7 +329,11 @@ __global__ __launch_bounds__(256) void evict_kernel(EvictArgs a) {
               Vec16<T>::unpack(x[0][it], f);
             }
 #pragma unroll
-            for (int e = 0; e < kIn; ++e) { lo[BOUNDS ? e : 0] = least(lo[BOUNDS ? e : 0], f[e]); hi[BOUNDS ? e : 0] = largest(hi[BOUNDS ? e : 0], f[e]); }
+            for (int e = 0; e < kIn; ++e) {
+              const int i = BOUNDS ? e : 0;
+              lo[i] = least(lo[i], f[e]);
+              hi[i] = largest(hi[i], f[e]);
+            }
           }
         }
       }

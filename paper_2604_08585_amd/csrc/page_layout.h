@@ -168,8 +168,8 @@ inline int append_heads(const qcf_layer_desc& L, const qcf_page_cache& c, int64_
 inline int append8_tokens(const qcf_page_cache& c) { return c.bounds ? c.page_size : QCF_PAGE8_BLOCK; }
 inline int64_t append8_units(const qcf_page_cache& c, int32_t B, int64_t total_rows) { return total_rows / append8_tokens(c) + 2 * (int64_t)B; }
 // KV heads of its workgroup: they share (cos, sin) and whole rows; fewer give a short call, and long pages, more workgroups.  us with one, two
-// and four (32 / 8 heads of 128, blocks): 36K rows 191, 156, 158; 256 requests of one row 18.5, 12.8, 10.7; 32 of 50 to 100 17.2, 15.1, 15.2 (two by this
-// rule); 500 rows 9.6, 9.6, 10.4 (one); pages with 256 rows, 24K of them 145, 173, 233 (one), with 64, 6K of them 42.8, 42.3, 55.7 (one).
+// and four (32 / 8 heads of 128, blocks): 36K rows 191, 156, 158; 256 requests of one row 18.5, 12.8, 10.7; 32 of 50 to 100 17.2, 15.1,
+// 15.2 (two by this rule); 500 rows 9.6, 9.6, 10.4 (one); pages with 256 rows, 24K of them 145, 173, 233 (one), with 64, 6K of them 42.8, 42.3, 55.7 (one).
 inline int append8_heads(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t B, int64_t total_rows) {
   const int tokens = append8_tokens(c);
   const int64_t workgroups = (total_rows / tokens + B) * L.n_kv_heads;               // that get rows, about, one head each

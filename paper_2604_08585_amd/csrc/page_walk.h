@@ -69,6 +69,11 @@ __device__ __forceinline__ uint32_t wave_incl(uint32_t x) {
   x += dpp<0x142, 0xa>(x);
   return x + dpp<0x143, 0xc>(x);
 }
+// the lower or upper two of four codes as bf16, exactly
+template <bool UPPER>
+__device__ __forceinline__ uint32_t two_bf16(uint32_t codes) {
+  return __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, UPPER));
+}
 __device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 
 // The contexts in grains, end to end, `pad` of them in front of each: what a workgroup that has begun one context pays for another.
@@ -150,11 +155,11 @@ struct Window {
 };
 
 // T: type of the queries and outputs, and of the pages; EIGHT: the pages have e4m3 codes, and a scale to every 16 tokens of a head.
-template <typename T, int D, int RT, int MODE, int WAVES, bool EIGHT = false, int SUB = sizeof(T) == 2 ? 2 : 1>
+template <typename T, int D, int RT, int MODE, int WAVES, bool EIGHT = false>
 struct Walk {
   static constexpr bool kHalf = sizeof(T) == 2;
   static constexpr int kSize = EIGHT ? 1 : (int)sizeof(T);             // bytes of a stored element
-  static constexpr int kSub = SUB;             // parts of 16 tokens of a tile; a part lies in one page
+  static constexpr int kSub = kHalf ? 2 : 1;             // parts of 16 tokens of a tile; a part lies in one page
   static constexpr int kTokens = 16 * kSub, kS = 4 * kSub;             // tokens of a tile, logits of a lane
   static constexpr int kQ = kHalf ? D / 32 : D / 16;                   // 16-byte vectors of a lane's part of a query
   static constexpr int kLoads = D * kSize / 64;                        // 16-byte loads of a lane for 16 tokens' keys
@@ -223,7 +228,7 @@ struct Walk {
       for (int h = 0; h < kSub; ++h) {
         const int mine = first + 16 * h, i = (mine >> a.log2_page) - w.first, slot = mine & mask;
         const int scale = __builtin_amdgcn_readlane(w.scale, i);
-        const uint64_t rows = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)w.high, i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)w.low, i);
+        const uint64_t rows = (uint64_t)from_lane(w.high, i) << 32 | from_lane(w.low, i);
         const int token = MODE == kList ? (__builtin_amdgcn_readlane(w.page, i) << a.log2_page) + slot : mine;
         r.base[h] = scale >= 0 && mine < (int)end ? token : -1;
         r.off[h] = (int64_t)(rows + (uint32_t)slot * (uint32_t)a.c.slot_stride);
@@ -339,8 +344,7 @@ struct Walk {
           if constexpr (EIGHT) {
             // elements e and e + 1 of two tokens side by side, then two codes at a time
             const uint32_t pair = __builtin_amdgcn_perm(t.v[2 * i + 1][e / 4], t.v[2 * i][e / 4], e & 2 ? 0x07030602u : 0x05010400u);
-            const bf16x2 x = e & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(pair, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(pair, 1.f, false);
-            vt[i] = __builtin_bit_cast(uint32_t, x);
+            vt[i] = e & 1 ? two_bf16<true>(pair) : two_bf16<false>(pair);
           } else {
             vt[i] = __builtin_amdgcn_perm(t.v[2 * i + 1][e / 2], t.v[2 * i][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
           }
@@ -356,7 +360,8 @@ struct Walk {
       for (int j = 0; j < kV; ++j)
 #pragma unroll
         for (int e = 0; e < kE; e += 2) {
-          const floatx2 x = e & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)t.v[j][e / 4], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)t.v[j][e / 4], false);
+          const int w = (int)t.v[j][e / 4];
+          const floatx2 x = e & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8(w, true) : __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
 #pragma unroll
           for (int r = 0; r < N; ++r) {
             c[r][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[0], p[r][j], c[r][e], 0, 0, 0);
@@ -413,8 +418,7 @@ struct Walk {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const uint32_t w = t.k[h][f / 2][2 * (f & 1) + i / 2];
-              const bf16x2 b = i & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
-              x[i] = __builtin_bit_cast(uint32_t, b);
+              x[i] = i & 1 ? two_bf16<true>(w) : two_bf16<false>(w);
             }
             z = wide(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, q[r][f]), z);
           }
@@ -825,7 +829,8 @@ qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t s
   } while (0)
   // (pages::side_by_side; several new rows with heads of 128 take one at a time)
   constexpr int kHeads = EIGHT ? 256 / D : 1, kHeadsOfSeveral = D == 64 ? kHeads : 1;
-  if (d.heads != 1 && d.heads != (a.n_q == 1 ? kHeads : kHeadsOfSeveral)) return fail(QCF_ERR_UNSUPPORTED, "page attention: %d heads side by side", d.heads);
+  if (d.heads != 1 && d.heads != (a.n_q == 1 ? kHeads : kHeadsOfSeveral))
+    return fail(QCF_ERR_UNSUPPORTED, "page attention: %d heads side by side", d.heads);
   if (a.list) QCF_ROWS(kList, 1);
   else if (a.n_q == 1) QCF_ROWS(kOne, kHeads);
   else QCF_ROWS(kSeveral, kHeadsOfSeveral);

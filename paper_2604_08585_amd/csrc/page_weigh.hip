@@ -48,8 +48,8 @@ struct Weigher : Walk<T, D, RT, kSeveral, pages::kWaves / HEADS, EIGHT> {
       for (int i = 0; i < 4; ++i) {
         const int row = row0 + 16 * r + 4 * this->quad + i;
         sees[r][i] = __shfl(this->lim[r], 4 * this->quad + i, 64);
-        const int at = row / this->a.G;
-        const float l = sees[r][i] > 0 ? w_.lse[((int64_t)context * this->a.n_q + at) * this->a.H + this->g * this->a.G + (row - at * this->a.G)] : INFINITY;
+        const int at = row / this->a.G, head = this->g * this->a.G + (row - at * this->a.G);
+        const float l = sees[r][i] > 0 ? w_.lse[((int64_t)context * this->a.n_q + at) * this->a.H + head] : INFINITY;
         ref[r][i] = l * kLog2e;                          // (a row that sees nothing: infinite, its weights are 0)
         ref_low[r][i] = __builtin_isfinite(ref[r][i]) ? __builtin_fmaf(l, kLog2e, -ref[r][i]) + l * kLog2eLow : 0.f;
       }

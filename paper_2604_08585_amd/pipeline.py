@@ -477,10 +477,11 @@ def paged_layer(L: DeviceLayer, more: int, page_size: int = 16, new: int = 1, ke
 
 
 def decode_step(P: PagedLayer, x: torch.Tensor, w_qkv: torch.Tensor) -> torch.Tensor:
-    """One layer's attention for `new` tokens behind each request: x [B * new, d_model] (normed hidden states) is projected, keys and
-    values go into the cache, rotated on the way, and the queries attend (with a budget, what they attend to is added to the tokens' weights).  Returns o [B, new, H, d].  Lengths and positions live
-    on the device and are not moved: call `advance` after a step's last layer, or to accept fewer tokens than were drafted.  A step
-    for which a request has no room is refused; steps that a captured graph replays are not, so who replays them counts."""
+    """One layer's attention for `new` tokens behind each request: x [B * new, d_model] (normed hidden states) is projected,
+    keys and values go into the cache, rotated on the way, and the queries attend (with a budget, what they attend to is added
+    to the tokens' weights).  Returns o [B, new, H, d].  Lengths and positions live on the device and are not moved: call
+    `advance` after a step's last layer, or to accept fewer tokens than were drafted.  A step for which a request has no room is
+    refused; steps that a captured graph replays are not, so who replays them counts."""
     rows, dm = P.B * P.new, P.desc.d_model
     if x.shape != (rows, dm) or w_qkv.shape != (P.qkv.shape[1], dm) or x.dtype != P.qkv.dtype or w_qkv.dtype != P.qkv.dtype:
         raise ValueError(f"x {tuple(x.shape)} and w_qkv {tuple(w_qkv.shape)} for {P.B} requests of {P.new} rows of {dm}, "
