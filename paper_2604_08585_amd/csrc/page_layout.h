@@ -72,15 +72,25 @@ inline int side_by_side(const qcf_layer_desc& L, const qcf_page_cache& c, int el
 // 13.1, 2048 16.3 and 11.1.  In float32, heads of 64: 2 of 512 10.8 and 9.7, 4 of up to 512 10.9 and 12.3, 1024 15.9 and 10.5.  Over eight
 // shapes, 1 to 64 requests and 256 to 8192 tokens the rule is 0.5 % behind the better of the two on average (272 KB in place of 290:
 // 0.6 %, 350: 0.9 %); at its border it takes the worse one by up to 11 % (19 % in float32), and by 25 % for 2048 workgroups of up to 256 tokens.
-// 8-bit pages: a wave's tile takes about as long whatever its width, so that the rule goes by tokens.  us, whole and divided, bf16 heads of
-// 128: 8 workgroups of 1024 tokens 11.2 and 11.9, 2048 12.2 and 11.9; 192 of up to 2048 22.5 and 25.8, 4096 42.2 and 40.6; 512 of up to 2048
-// 50.1 and 52.5, 4096 88.8 and 88.2.  Heads of 64: 8 of 1024 8.8 and 11.1, 2048 12.7 and 11.4; 64 of up to 2048 17.0 and 16.3; 192 of up to 2048
-// 17.8 and 20.5, 4096 30.4 and 26.7, 8192 58.6 and 43.9; 512 of up to 8192 91.3 and 97.4.  float32, heads of 64: 2 of 512 9.2 and 10.9, 1024 13.9
-// and 11.0; 16 of up to 512 10.7 and 11.4, 1024 17.2 and 11.7.
-inline bool takes_whole(const qcf_layer_desc& L, int64_t workgroups, int64_t longest, int elem) {
+// 8-bit pages: a wave's tile takes about as long whatever its width, so that the rule goes by tokens; and where there are more workgroups
+// than compute units, whose second round leaves some idle, it divides from fewer on.  us, whole and divided, lengths from a quarter of the
+// longest on.  One new row, bf16, heads of 128: 8 workgroups of 1024 tokens 11.2 and 11.9, 2048 12.2 and 11.9; 192 of up to 2000 21.3 and
+// 23.3, 4000 36.0 and 35.9; 320 of up to 1000 22.2 and 21.7, 4000 62.7 and 53.4; 512 of up to 1000 26.2 and 29.8, 8000 147 and 133; 1024 of up
+// to 1000 52.5 and 54.3, 2000 81.9 and 80.6.  Heads of 64: 8 of 1024 8.8 and 11.1, 2048 12.7 and 11.4; 128 of up to 3000 20.8 and 20.6; 320 of
+// up to 2000 20.7 and 21.9, 4000 37.0 and 32.0; 1024 of up to 2000 44.4 and 50.2, 8000 149 and 141.  float32, half as many tokens: heads of 64,
+// 320 of up to 500 16.1 and 18.3, 1500 34.8 and 29.8; of 128, 1024 of up to 500 54.4 and 58.4, 1000 91.6 and 84.8.
+// Several new rows, which a join takes longer for: 512 workgroups, heads of 128, of up to 2000 51.7 and 57.0, 4000 86.1 and 88.6; 320 of up
+// to 4000 67.8 and 63.0; heads of 64, 512 of up to 4000 49.0 and 52.5.
+// Heads that only ranges take side by side, one row: heads of 128, 256 of up to 5000 63.9 and 54.2, 320 of up to 4000 73.2 and 53.2, 2048 of
+// up to 300 56.5 and 49.0; of 64, 256 of up to 2500 26.5 and 26.2, 320 of up to 1000 16.9 and 18.8, 1024 of up to 1000 33.3 and 31.5, 4000 120
+// and 88.9.  At its borders the rule takes the worse one by up to 5 % (float32, heads of 64: 15 %).
+inline bool takes_whole(const qcf_layer_desc& L, int64_t workgroups, int64_t longest, int elem, int heads, bool several) {
   if (elem == 1) {
-    const int64_t alone = std::max<int64_t>(30, 200 - workgroups * 154 / compute_unit_count());
-    return longest * alone <= (L.dtype == QCF_DTYPE_BF16 ? 1400 : 700) * 200;
+    const bool one_round = workgroups <= compute_unit_count(), wide = L.head_dim == 128;
+    int64_t most = one_round ? 1400 * 200 / (200 - workgroups * 154 / compute_unit_count())
+                             : several ? (wide ? 3072 : 4096) : wide ? 1024 : 3072;
+    if (heads > 1 && !several) most = std::min<int64_t>(most, one_round ? 2048 : wide ? 0 : 1024);
+    return (L.dtype == QCF_DTYPE_BF16 ? longest : 2 * longest) <= most;
   }
   const int64_t bytes = longest * 2 * L.head_dim * elem;
   const int64_t alone = std::max<int64_t>(30, 200 - workgroups * 256 / compute_unit_count());      // of 200
@@ -114,7 +124,7 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   // (four drafts of 8 requests of 2K to 6K tokens, 32 rows, before later steps, which brought 47 to 44 us: 53.0 us without, 48.1 with 12,
   // 47.1 with 18, 50.0 with 28; two workgroups on a compute unit cover for each other, 0 to 9 are the same there)
   d.pad = d.contexts > 1 && d.row_tiles == 2 ? 16 : 0;
-  d.whole = d.row_tiles == 1 && takes_whole(L, (int64_t)d.contexts * d.inner, longest, elem);
+  d.whole = d.row_tiles == 1 && takes_whole(L, (int64_t)d.contexts * d.inner, longest, elem, d.heads, n_q > 1 && !n_keep);
   const int64_t ranges = (d.most + d.least - 1) / d.least;
   if (d.slots > ranges) d.slots = (int)ranges;
   return d;

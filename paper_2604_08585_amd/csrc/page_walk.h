@@ -543,8 +543,11 @@ struct Walk {
     const int64_t shared = MODE == kSeveral && lim_lo < lim_hi ? min(end, (int64_t)(lim_lo & -kTokens)) : end;
     auto nothing = [] {};
     at = tile_at(at, shared);
-    if constexpr (RT == 2 && D == 128) {
-      // (no registers for a second tile: the next keys are asked for once the logits are there, the next values after the products)
+    if constexpr ((RT == 2 || (EIGHT && WAVES < pages::kWaves)) && D == 128) {
+      // (two tiles of rows leave no registers for a second tile of tokens: the next keys are asked for once the logits are there, the
+      // next values after the products.  8-bit heads side by side, whose waves ask for the same tokens at once, gain by it too: 64
+      // requests of 4K to 12K tokens 205 us, 216 with a second tile, one of 128K 60.9 and 65.0; a head to a workgroup gains nothing,
+      // 202 and 200, and several rows lose, 35.4 and 34.2)
       if (at < shared) {
         Tile t;
         load(t, at);

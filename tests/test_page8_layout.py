@@ -71,11 +71,22 @@ def test_heads_side_by_side_where_there_is_much_to_read():
     assert division(6, 3, 128, "bf16", 64, 1, 131072)["heads"] == 1                                # (three heads: no pairs)
 
 
-@pytest.mark.parametrize("dtype,workgroups,longest", [("bf16", 1, 1400), ("f32", 1, 704), ("bf16", 64, 1728), ("bf16", 192, 3294), ("bf16", 512, 9333)])
-def test_whole_contexts_up_to_a_number_of_tokens(dtype, workgroups, longest):
+@pytest.mark.parametrize("dtype,D,workgroups,longest", [("bf16", 64, 1, 1400), ("f32", 64, 1, 704), ("bf16", 64, 64, 1728), ("bf16", 64, 192, 3294), ("f32", 64, 192, 1647),
+                                                        ("bf16", 128, 192, 3294), ("bf16", 64, 512, 3072), ("bf16", 128, 264, 1024), ("f32", 128, 512, 512)])
+def test_whole_contexts_up_to_a_number_of_tokens(dtype, D, workgroups, longest):
     B = max(1, workgroups // 8)
-    shape = (32, 8, 64) if workgroups >= 8 else (4, 1, 64)
-    assert division(*shape, dtype, B, 1, longest - 64)["whole"] and not division(*shape, dtype, B, 1, longest + 64)["whole"]
+    shape = (32, 8, D) if workgroups >= 8 else (4, 1, D)
+    assert division(*shape, dtype, B, 1, longest - 64, adjacent=False)["whole"] and not division(*shape, dtype, B, 1, longest + 64, adjacent=False)["whole"]
+
+
+def test_whole_contexts_of_several_rows_and_of_heads_side_by_side():
+    assert division(32, 8, 128, "bf16", 64, 4, 3000)["whole"] and not division(32, 8, 128, "bf16", 64, 4, 3200)["whole"]
+    # (kept pages: a row of its own, whatever their number)
+    assert division(32, 8, 128, "bf16", 16, 4, 5000, n_keep=64)["whole"] and not division(32, 8, 128, "bf16", 16, 4, 5000, n_keep=65)["whole"]
+    for D, B, longest in ((64, 32, 2048), (64, 64, 1024)):
+        below, above = division(32, 8, D, "bf16", B, 1, longest), division(32, 8, D, "bf16", B, 1, longest + 16)
+        assert below["heads"] == above["heads"] == 4 and below["whole"] and not above["whole"]
+    assert division(32, 8, 128, "bf16", 64, 1, 1000)["heads"] == 2 and not division(32, 8, 128, "bf16", 64, 1, 1000)["whole"]
 
 
 def test_two_tiles_of_rows_where_there_is_much_to_read():
