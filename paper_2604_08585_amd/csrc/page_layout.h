@@ -56,8 +56,9 @@ constexpr int at_once(int head_dim, int row_tiles, bool eight) {
 
 // KV heads whose rows lie next to each other and are read side by side, by the waves of a workgroup: 256 bytes in a row, as a row of bf16
 // has.  read: bytes of the keys and values at most; where they are few, the joins of twice as many parts cost more.  us, pages that keep a
-// token's 8-bit heads together, a head to a workgroup and side by side: heads of 128, 64 requests of 4K to 12K tokens 243 and 217, one of 128K
-// 70 and 64, of 30K (61 MB) 23.3 and 24.8; heads of 64 188 and 130, one of 30K 22.0 and 20.2, of 3K 11.8 and 14.5.
+// token's 8-bit heads together, a head to a workgroup and side by side: heads of 128, 64 requests of 4K to 12K tokens 243 and 205, one of 128K
+// 70 and 61, of 30K (61 MB) 23.0 and 22.6, four new rows 249 and 220, 70 and 65, 8 requests of up to 6K 31.1 and 31.6;
+// heads of 64 188 and 130, one of 30K 22.0 and 20.2, of 3K 11.8 and 14.5.
 inline int side_by_side(const qcf_layer_desc& L, const qcf_page_cache& c, int elem, double read) {
   const int heads = 256 / L.head_dim;
   const bool worth = read > (L.head_dim == 128 ? 4.0 : 1.0) * kShared;
@@ -83,13 +84,16 @@ inline int side_by_side(const qcf_layer_desc& L, const qcf_page_cache& c, int el
 // to 4000 67.8 and 63.0; heads of 64, 512 of up to 4000 49.0 and 52.5.
 // Heads that only ranges take side by side, one row: heads of 128, 256 of up to 5000 63.9 and 54.2, 320 of up to 4000 73.2 and 53.2, 2048 of
 // up to 300 56.5 and 49.0; of 64, 256 of up to 2500 26.5 and 26.2, 320 of up to 1000 16.9 and 18.8, 1024 of up to 1000 33.3 and 31.5, 4000 120
-// and 88.9.  At its borders the rule takes the worse one by up to 5 % (float32, heads of 64: 15 %).
+// and 88.9.  Four rows, heads of 128: 256 of up to 2500 37.9 and 42.9, 4000 54.1 and 54.9; 512 of up to 1000 34.2 and 36.9, 3000 79.6 and
+// 76.3; 2048 of up to 300 76.3 and 71.7, 2000 198 and 181.  At its borders the rule takes the worse one by up to 5 % (float32, heads of 64:
+// 15 %).
 inline bool takes_whole(const qcf_layer_desc& L, int64_t workgroups, int64_t longest, int elem, int heads, bool several) {
   if (elem == 1) {
-    const bool one_round = workgroups <= compute_unit_count(), wide = L.head_dim == 128;
-    int64_t most = one_round ? 1400 * 200 / (200 - workgroups * 154 / compute_unit_count())
-                             : several ? (wide ? 3072 : 4096) : wide ? 1024 : 3072;
+    const int64_t units = compute_unit_count();
+    const bool one_round = workgroups <= units, wide = L.head_dim == 128;
+    int64_t most = one_round ? 1400 * 200 / (200 - workgroups * 154 / units) : several ? (wide ? 3072 : 4096) : wide ? 1024 : 3072;
     if (heads > 1 && !several) most = std::min<int64_t>(most, one_round ? 2048 : wide ? 0 : 1024);
+    if (heads > 1 && several && wide) most = std::min(most, one_round ? 4096 : 2048 * units / workgroups);
     return (L.dtype == QCF_DTYPE_BF16 ? longest : 2 * longest) <= most;
   }
   const int64_t bytes = longest * 2 * L.head_dim * elem;
@@ -115,8 +119,7 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   d.row_tiles = d.rows > 16 && read > (wide8 ? 8.0 : 1.0) * kShared ? 2 : 1;
   d.row_blocks = (d.rows + 16 * d.row_tiles - 1) / (16 * d.row_tiles);
   d.inner = L.n_kv_heads * d.row_blocks;
-  // (several new rows with heads of 128: 51.0 us with a head to a workgroup, 55.6, for four drafts of 16 requests of up to 8K tokens)
-  d.heads = n_keep || d.row_tiles > 1 || (n_q > 1 && L.head_dim == 128) ? 1 : side_by_side(L, c, elem, read);
+  d.heads = n_keep || d.row_tiles > 1 ? 1 : side_by_side(L, c, elem, read);
   d.slots = at_once(L.head_dim, d.row_tiles, elem == 1) * compute_unit_count() * d.heads / d.inner;       // (two waves to a SIMD, or one)
   if (d.slots < 1) d.slots = 1;
   d.most = (int64_t)d.contexts * ((longest + kGrain - 1) / kGrain);

@@ -546,8 +546,8 @@ struct Walk {
     if constexpr ((RT == 2 || (EIGHT && WAVES < pages::kWaves)) && D == 128) {
       // (two tiles of rows leave no registers for a second tile of tokens: the next keys are asked for once the logits are there, the
       // next values after the products.  8-bit heads side by side, whose waves ask for the same tokens at once, gain by it too: 64
-      // requests of 4K to 12K tokens 205 us, 216 with a second tile, one of 128K 60.9 and 65.0; a head to a workgroup gains nothing,
-      // 202 and 200, and several rows lose, 35.4 and 34.2)
+      // requests of 4K to 12K tokens 205 us, 216 with a second tile, one of 128K 60.9 and 65.0; a head to a workgroup gains
+      // nothing, 202 and 200, and four drafts of eight requests there lose, 35.4 and 34.2)
       if (at < shared) {
         Tile t;
         load(t, at);
@@ -830,13 +830,12 @@ qcf_status launch(const PageAttnArgs& a, const pages::Division& d, hipStream_t s
       QCF_LAUNCH(2, MODE, pages::kWaves, false, 1);                                             \
     }                                                                                           \
   } while (0)
-  // (pages::side_by_side; several new rows with heads of 128 take one at a time)
-  constexpr int kHeads = EIGHT ? 256 / D : 1, kHeadsOfSeveral = D == 64 ? kHeads : 1;
-  if (d.heads != 1 && d.heads != (a.n_q == 1 ? kHeads : kHeadsOfSeveral))
+  constexpr int kHeads = EIGHT ? 256 / D : 1;            // (pages::side_by_side)
+  if (d.heads != 1 && d.heads != kHeads)
     return fail(QCF_ERR_UNSUPPORTED, "page attention: %d heads side by side", d.heads);
   if (a.list) QCF_ROWS(kList, 1);
   else if (a.n_q == 1) QCF_ROWS(kOne, kHeads);
-  else QCF_ROWS(kSeveral, kHeadsOfSeveral);
+  else QCF_ROWS(kSeveral, kHeads);
 #undef QCF_ROWS
 #undef QCF_LAUNCH
   QCF_TRY_LAUNCH("page attention");

@@ -267,6 +267,10 @@ ATTENTIONS = [
     ("bf16", 32, 32, 128, 16, "token", [[97 * i % 1300] for i in range(80)]),
     ("f32", 16, 16, 64, 32, "token", [[61 * i % 500, 7 * i] for i in range(70)]),
     ("bf16", 2, 1, 64, 64, "token", [[30001]]),
+    # several rows of heads that ranges read side by side, in one tile of rows and in two
+    ("bf16", 16, 4, 128, 16, "token", [[700, 701, 640, 0], [1, 2, 3, 4], [33, 32, 31, 2000]]),
+    ("f32", 4, 2, 128, 32, "token", [[64, 65, 66, 67, 68], [0, 0, 0, 0, 1000]]),
+    ("bf16", 64, 8, 128, 64, "token", [[4000, 100, 4001]]),
 ]
 
 

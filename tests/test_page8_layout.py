@@ -56,7 +56,7 @@ def test_what_a_division_promises(H, Hkv, D):
         assert d["inner"] == Hkv * d["row_blocks"] and d["inner"] % d["heads"] == 0 and Hkv % d["heads"] == 0
         assert d["row_blocks"] * 16 * d["row_tiles"] >= d["rows"] > (d["row_blocks"] - 1) * 16 * d["row_tiles"]
         # heads side by side: only where their rows lie next to each other, in kernels that there are
-        assert d["heads"] in (1, 256 // D) and (d["heads"] == 1 or (adjacent and not keep and d["row_tiles"] == 1 and (n_q == 1 or D == 64)))
+        assert d["heads"] in (1, 256 // D) and (d["heads"] == 1 or (adjacent and not keep and d["row_tiles"] == 1))
         # as many workgroups as the GPU holds at once, or one range
         assert d["slots"] == 1 or d["slots"] * d["inner"] // d["heads"] <= d["at_once"] * 256
         assert d["parts"] == 2 * d["slots"] * d["inner"] * d["part_rows"]
@@ -80,7 +80,9 @@ def test_whole_contexts_up_to_a_number_of_tokens(dtype, D, workgroups, longest):
 
 
 def test_whole_contexts_of_several_rows_and_of_heads_side_by_side():
-    assert division(32, 8, 128, "bf16", 64, 4, 3000)["whole"] and not division(32, 8, 128, "bf16", 64, 4, 3200)["whole"]
+    for adjacent, B, longest in ((False, 64, 3072), (True, 64, 1024), (True, 32, 4096)):
+        below, above = (division(32, 8, 128, "bf16", B, 4, n, adjacent=adjacent) for n in (longest, longest + 16))
+        assert below["heads"] == above["heads"] == 1 + adjacent and below["whole"] and not above["whole"]
     # (kept pages: a row of its own, whatever their number)
     assert division(32, 8, 128, "bf16", 16, 4, 5000, n_keep=64)["whole"] and not division(32, 8, 128, "bf16", 16, 4, 5000, n_keep=65)["whole"]
     for D, B, longest in ((64, 32, 2048), (64, 64, 1024)):
