@@ -24,7 +24,7 @@ extern "C" {
  *   scales  DEVICE [n_pages, H_kv, 2, page_size / 16] float32: those of a page's keys (0) and of its values (1); at most 2^31 of them.
  * Bounds, if there are any, have the layer's type; qcf_page_select takes such a cache as it is (it reads bounds and table only). */
 
-/* qcf_page_append for 8-bit pages: the same arguments, and scales.  Keys are turned in float32 and rounded once, to their codes.  A
+/* qcf_page_append for 8-bit pages: the same arguments, and scales.  Keys are turned in 64 bits and rounded once, to their codes.  A
  * block's scale is the least power of two s, not less than 2^-100, with |x| <= 448 s for all elements that were stored into it since
  * its first slot was written.  Where rows make the scale of a block grow that has tokens in front of them, these are rounded again, to
  * the new scale (a value changes only where it comes beneath 2^-6 of it).  Elements that are not finite or beyond 2^100 are stored as

@@ -1,4 +1,6 @@
 // Decoding over a cache in 8-bit pages: new rows into their pages.
+#include <type_traits>
+
 #include "qcf_internal.h"
 #include "page_layout.h"
 #include "append_common.h"
@@ -9,28 +11,48 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 
-// (cos, sin) of `positions` times a frequency in turns, to the last bit or so: a code's rounding turns an error of its element into a
-// whole step where the element lies between two codes.  What the fraction of a turn loses as a float comes back in first order.
-__device__ __forceinline__ float2 exact_turn(double positions, double turns) {
-  const double t = positions * turns, r = t - __builtin_rint(t);
-  const float f = (float)r, d = (float)(r - (double)f) * 6.283185307f;
-  float sn, cn;
-  sincospif(2.f * f, &sn, &cn);
-  return make_float2(__builtin_fmaf(-sn, d, cn), __builtin_fmaf(cn, d, sn));
+// (cos, sin) of `positions` times a frequency in turns, in 64 bits: a rotated key is rounded to a code as the formula has it.  (In float32
+// 32 to 40 of 34 million codes were a whole step off, elements within an error of 2^-24 of the middle between two codes.)  The angle is
+// reduced to an eighth of a turn around a quarter; Taylor's series are 2^-45 off there.  (731 rows 10.2 us, 9.6 in
+// float32; 8 rows 6.7 in the kernel, 6.0; 36K 159 both ways.)
+__device__ __forceinline__ double2 exact_turn(double positions, double turns) {
+  const double t = positions * turns, r = t - __builtin_rint(t), quarters = __builtin_rint(4.0 * r);
+  const double x = (r - 0.25 * quarters) * 6.283185307179586477, y = x * x;
+  double sn = 1.0 / 6227020800, cn = -1.0 / 87178291200;                 // 1 / 13!, -1 / 14!
+  constexpr double kSin[] = {-1.0 / 39916800, 1.0 / 362880, -1.0 / 5040, 1.0 / 120, -1.0 / 6, 1.0};
+  constexpr double kCos[] = {1.0 / 479001600, -1.0 / 3628800, 1.0 / 40320, -1.0 / 720, 1.0 / 24, -0.5, 1.0};
+#pragma unroll
+  for (int i = 0; i < 6; ++i) sn = __builtin_fma(sn, y, kSin[i]);
+#pragma unroll
+  for (int i = 0; i < 7; ++i) cn = __builtin_fma(cn, y, kCos[i]);
+  sn *= x;
+  const int q = (int)quarters & 3;
+  const double c = q & 1 ? sn : cn, s = q & 1 ? cn : sn;
+  return make_double2(q == 1 || q == 2 ? -c : c, q & 2 ? -s : s);
+}
+
+// x as a float of 21 bits that lies on the same side of every code, and of every middle between two, as x does: what these bits cannot hold
+// makes the last one odd.
+__device__ __forceinline__ float odd(double x) {
+  const uint64_t bits = (uint64_t)__double_as_longlong(x);
+  const uint32_t high = (uint32_t)(bits >> 32) | min((uint32_t)bits, 1u);
+  return (float)__longlong_as_double((int64_t)((uint64_t)high << 32));
 }
 
 // One workgroup per (unit that gets rows, `heads` KV heads of it): a block of 16 tokens, or, where the pages have bounds, a page.  A wave
 // takes a block for one head as a whole, keys and values: it turns the keys, finds both largest elements, hence the scales, and stores
 // the codes.  Where the block has tokens already and its scale grows, these are rounded again.  (heads: 1, 2 or 4; the waves of a head
-// take its blocks in turn.)  Bound by memory where many rows come (36K rows, 32 / 8 heads of 128: 158 us, 5.1 TB/s of what is read and written, a copy's rate), by the chain offsets -> table and
-// positions -> factors -> largest elements -> codes where few do (8 rows 6.1 us).
+// take its blocks in turn.)  Bound by memory where many rows come (36K rows, 32 / 8 heads of 128: 159 us, 5.1 TB/s of what
+// is read and written, a copy's rate), by the chain offsets -> table and positions -> factors -> largest elements -> codes where few do (8
+// rows 6.7 us).
 template <typename T, int D, int STYLE>
 __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, float* __restrict__ scales, int heads) {
   constexpr int VEC = Elem<T>::kVec, TPR = D / 2 / VEC, PAIRS = D / 2, ROWS = 4096 / D;
   constexpr int RPI = 64 / TPR, ITS = kBlock / RPI;                      // rows of a block side by side in a wave, and how often
   constexpr int kWords = VEC / 4;                                        // words of half a lane's codes
   typedef uint32_t codes_t __attribute__((ext_vector_type(kWords)));
-  __shared__ float2 s_turn[ROWS][PAIRS];
+  // (the pairs of a lane TPR apart, rows 16 * TPR bytes more than theirs: lanes read what lies side by side, in banks of their own)
+  __shared__ __align__(16) double2 s_turn[ROWS][PAIRS + TPR];
   __shared__ float s_bound[2][kWaves][D];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int parts = a.Hkv / heads;
@@ -53,13 +75,20 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, float* 
     Vec16<T>::unpack(*reinterpret_cast<const u32x4*>(src + e0), f);
     Vec16<T>::unpack(*reinterpret_cast<const u32x4*>(src + e1), f + VEC);
   };
-  auto turn = [&](int j, float* f) {
+  // (exact: of a key, which will be coded)
+  auto turn = [&](auto exact, int j, float* f) {
     if (!a.pos) return;
     float o[2 * VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
       const int ia = STYLE == 0 ? i : 2 * i, ib = STYLE == 0 ? i + VEC : 2 * i + 1;
-      turn_pair(f[ia], f[ib], s_turn[j][i0 + i], o[ia], o[ib]);
+      const double2 w = s_turn[j][i * TPR + place];
+      if constexpr (exact.value) {
+        o[ia] = odd(f[ia] * w.x - f[ib] * w.y);
+        o[ib] = odd(f[ib] * w.x + f[ia] * w.y);
+      } else {
+        turn_pair(f[ia], f[ib], make_float2((float)w.x, (float)w.y), o[ia], o[ib]);
+      }
     }
 #pragma unroll
     for (int e = 0; e < 2 * VEC; ++e) f[e] = o[e];
@@ -84,8 +113,16 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, float* 
     const int first = max(slot0, c0), last = min(slot1, c0 + ROWS);       // slots of the chunk that get rows
     if (a.pos) {
       if (c0 > slot0) __syncthreads();
-      for (int s = first + tid / PAIRS; s < last; s += kThreads / PAIRS)
-        s_turn[s - c0][tid % PAIRS] = exact_turn((double)a.pos[row0 + s], turns);
+      // (a block's at a time: positions and factors on their way together; rows behind the last one are that one again)
+      constexpr int kStep = kThreads / PAIRS, kAt = kBlock / kStep;
+      for (int s0 = first + tid / PAIRS; s0 < last; s0 += kBlock) {
+        int32_t pos[kAt];
+#pragma unroll
+        for (int i = 0; i < kAt; ++i) pos[i] = a.pos[row0 + min(s0 + i * kStep, last - 1)];
+#pragma unroll
+        for (int i = 0; i < kAt; ++i)
+          s_turn[min(s0 + i * kStep, last - 1) - c0][tid % VEC * TPR + tid % PAIRS / VEC] = exact_turn((double)pos[i], turns);
+      }
       __syncthreads();
     }
     for (int b0 = (first / kBlock + turn_of) * kBlock; there && b0 < last; b0 += turns_of * kBlock) {
@@ -109,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, float* 
         for (int it = 0; it < ITS; ++it) {
           const int s = b0 + it * RPI + lane / TPR;
           const bool mine = s >= first && s < last;
-          if (which == 0) turn(min(max(s, first), last - 1) - c0, f[it]);
+          if (which == 0) turn(std::true_type{}, min(max(s, first), last - 1) - c0, f[it]);
 #pragma unroll
           for (int e = 0; e < 2 * VEC; ++e) {
             if (!storable(f[it][e])) f[it][e] = NAN;
@@ -159,7 +196,7 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(AppendArgs a, float* 
         const int j = at / q_vecs, h = (at - j * q_vecs) / TPR, s = first + j;
         float f[2 * VEC];
         read(q + (row0 + s) * a.q_stride + h * D, f);
-        turn(s - c0, f);
+        turn(std::false_type{}, s - c0, f);
         T* dst = q_out + ((row0 + s) * a.H + h) * D;
         *reinterpret_cast<u32x4*>(dst + e0) = rounded<T>(f);
         *reinterpret_cast<u32x4*>(dst + e1) = rounded<T>(f + VEC);

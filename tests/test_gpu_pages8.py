@@ -109,6 +109,18 @@ def test_scales_that_grow_and_scales_that_stay(size, bounds):
         _check_append(p, *_append(p, rng, lens, new, False, size=size), False)
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,D,style", [("bf16", 8, 8, 128, 0), ("bf16", 8, 8, 64, 1), ("f32", 4, 4, 128, 1), ("f32", 8, 8, 64, 0)])
+def test_rotated_keys_get_the_codes_of_the_formula(dtype, H, Hkv, D, style):
+    """A key turned in 64 bits is at most 2^-41 of its pair off (positions below 2000, angles to 2^-52 of theirs); of a million elements, with
+    middles between codes at least 2^-4 of them apart, 2^-16 may be expected to lie that close to one: all codes are the oracle's."""
+    rng = np.random.default_rng(41)
+    p = Paged8(rng, shape(H, Hkv, D, dtype, style), 32, [1203, 900, 5], "token", bounds=True)
+    (codes, scales, bounds), _, _, _ = _append(p, rng, [3, 0, 0], [1200, 900, 5], True)
+    k, v, s = p.got()
+    assert np.array_equal(k, codes[0], equal_nan=True) and np.array_equal(v, codes[1], equal_nan=True) and np.array_equal(s, scales)
+    assert np.array_equal(to_np(p.bd), bounds, equal_nan=True)
+
+
 @pytest.mark.parametrize("dtype,far", [("f32", 3000000), ("bf16", 2000000000), ("f32", -100000)])
 def test_append_at_far_positions(dtype, far):
     rng = np.random.default_rng(23)
