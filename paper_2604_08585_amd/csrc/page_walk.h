@@ -297,9 +297,8 @@ struct Walk {
     return at;
   }
 
-  // bf16 terms of a weight in its product with the values (8 bits: two, 2^-17 of it are lost, beside codes that are off by 2^-4 of what was
-  // stored; four drafts of 8 requests of 2K to 6K tokens 38.7 us with three, 36.5 with two)
-  static constexpr int kTerms = EIGHT ? 2 : 3;
+  // bf16 terms of a weight in its product with the values: the whole float, whatever the values are stored in
+  static constexpr int kTerms = 3;
   // products of the tile's values with the weights, added to c
   template <int N>
   __device__ __forceinline__ void values(const Tile& t, const float (&p_)[N][kS], floatx4 (&c)[N][kE]) const {
