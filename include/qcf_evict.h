@@ -8,6 +8,7 @@
  *   call order for one layer:
  *     every step  qcf_page_append -> qcf_page_attn (with lse) -> qcf_page_weigh
  *     now and then  qcf_page_evict
+ *   (rows that may still be rejected, drafts, are weighed once it is known which of them stay, with a `seen` of 0 for the others)
  *
  * Both calls take pages of the layer's type (scales NULL) or 8-bit pages (qcf_pages8.h).  Weights are dense:
  *   weights  DEVICE [B, H_kv, max_pages * page_size] float32, token t of request b at its own place whatever page it is in.

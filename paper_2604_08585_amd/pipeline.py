@@ -411,11 +411,22 @@ class PagedLayer:
     # with a budget (evict):
     budget: int = 0                # tokens that a request's heads keep
     spare: Optional[qb.PageCache] = None           # pages of the same pools that kept tokens move to
-    weights: Optional[torch.Tensor] = None         # [B, H_kv, tokens] float32: the attention that each token got so far
+    settled: Optional[torch.Tensor] = None         # [B, H_kv, tokens] float32: the attention that each token got from rows that were accepted
+    pending: Optional[torch.Tensor] = None         # [B, new] int32: tokens that the rows of the last step see, 0 once `advance` has decided on them
     spare_weights: Optional[torch.Tensor] = None
     kept: Optional[torch.Tensor] = None            # [B, H_kv, budget] int32: the tokens that the last eviction kept
     ws_evict: Optional[torch.Tensor] = None
     more: int = 0                  # room behind a request that has been cut down
+
+    @property
+    def weights(self) -> Optional[torch.Tensor]:
+        """[B, H_kv, tokens] float32, a copy: the attention that each token got so far, that of a step on which `advance` has not decided
+        yet with it."""
+        if not self.budget:
+            return None
+        w = self.settled.clone()
+        qb.qcf_page_weigh(self.desc, self.cache, self.B, self.new, self.q, self.pending, self.lse, self.held, 1.0, 1.0, w)
+        return w
 
 
 def paged_layer(L: DeviceLayer, more: int, page_size: int = 16, new: int = 1, keep: int = 0, first: int = 1,
@@ -423,8 +434,9 @@ def paged_layer(L: DeviceLayer, more: int, page_size: int = 16, new: int = 1, ke
     """The fused cache of a layer in pages, with room for `more` tokens behind every request's context (which begins at position
     0).  keep > 0: each new row's attention is cut down to that many pages for each KV head, the first `first` and the last `last`
     among them; the pages' bounds are kept for that.  eight: pages of 8-bit elements, with a scale for every 16 tokens of a head.
-    budget > 0: steps add up the attention that tokens get, and `evict` cuts every request down to that many tokens to a head, with room
-    for `more` behind them (not with keep: weights need attention over all pages)."""
+    budget > 0: the attention that accepted rows give to tokens is added up, from 0 on (the prompt's own rows are not among them), and
+    `evict` cuts every request down to that many tokens to a head, with room for `more` behind them (not with keep: weights need attention
+    over all pages)."""
     if more < 0 or not 0 <= new <= 16:
         raise ValueError(f"room for {more} tokens, steps of {new} (at most 16)")
     if keep < 0 or min(first, last) < 0 or (keep and first + last > keep):
@@ -468,7 +480,8 @@ def paged_layer(L: DeviceLayer, more: int, page_size: int = 16, new: int = 1, ke
         ws_attn=_ws(attn_bytes(desc, cache, L.B, new, keep), dev))
     if budget:
         P.budget, P.more, P.spare = budget, more, described(tables[1])
-        P.weights, P.spare_weights = (torch.zeros(L.B, Hkv, cache.tokens, dtype=torch.float32, device=dev) for _ in range(2))
+        P.settled, P.spare_weights = (torch.zeros(L.B, Hkv, cache.tokens, dtype=torch.float32, device=dev) for _ in range(2))
+        P.pending = torch.zeros_like(P.seen)
         P.kept = torch.full((L.B, Hkv, budget), -1, dtype=torch.int32, device=dev)
         P.ws_evict = _ws(qb.qcf_page_evict_workspace_bytes(desc, cache, L.B, budget), dev)
     append = qb.qcf_page8_append if eight else qb.qcf_page_append
@@ -478,10 +491,11 @@ def paged_layer(L: DeviceLayer, more: int, page_size: int = 16, new: int = 1, ke
 
 def decode_step(P: PagedLayer, x: torch.Tensor, w_qkv: torch.Tensor) -> torch.Tensor:
     """One layer's attention for `new` tokens behind each request: x [B * new, d_model] (normed hidden states) is projected,
-    keys and values go into the cache, rotated on the way, and the queries attend (with a budget, what they attend to is added
-    to the tokens' weights).  Returns o [B, new, H, d].  Lengths and positions live on the device and are not moved: call
-    `advance` after a step's last layer, or to accept fewer tokens than were drafted.  A step for which a request has no room is
-    refused; steps that a captured graph replays are not, so who replays them counts."""
+    keys and values go into the cache, rotated on the way, and the queries attend.  Returns o [B, new, H, d].  Lengths and
+    positions live on the device and are not moved: call `advance` after a step's last layer, or to accept fewer tokens than
+    were drafted (with a budget, it is `advance` that adds the accepted rows' attention to the tokens' weights: a step may be run
+    again before it).  A step for which a request has no room is refused; steps that a captured graph replays are not, so who
+    replays them counts."""
     rows, dm = P.B * P.new, P.desc.d_model
     if x.shape != (rows, dm) or w_qkv.shape != (P.qkv.shape[1], dm) or x.dtype != P.qkv.dtype or w_qkv.dtype != P.qkv.dtype:
         raise ValueError(f"x {tuple(x.shape)} and w_qkv {tuple(w_qkv.shape)} for {P.B} requests of {P.new} rows of {dm}, "
@@ -498,14 +512,16 @@ def decode_step(P: PagedLayer, x: torch.Tensor, w_qkv: torch.Tensor) -> torch.Te
         qb.qcf_page_select(P.desc, P.cache, P.B, P.new, P.q, P.seen, P.keep, P.first, P.last, P.pages, P.ws_select)
     attn(P.desc, P.cache, P.B, P.new, P.q, P.seen, P.pages, P.keep, P.o, P.lse, P.ws_attn)
     if P.budget:
-        qb.qcf_page_weigh(P.desc, P.cache, P.B, P.new, P.q, P.seen, P.lse, P.held, 1.0, 1.0, P.weights)
+        P.pending.copy_(P.seen)
     return P.o
 
 
 def advance(P: PagedLayer, tokens: Union[int, Sequence[int], torch.Tensor]) -> None:
     """Every request holds `tokens` tokens more, at most the `new` of a step (fewer: the others' slots are written again); a
     sequence of one number for each request where they accept different ones.  The numbers are the host's, which counts the room.
-    (One number recorded into a graph moves lengths and positions at every replay, and what is left of the room not at all.)"""
+    (One number recorded into a graph moves lengths and positions at every replay, and what is left of the room not at all.)
+    With a budget, the attention of the accepted rows of the last step is added to the tokens' weights; with this call the others
+    are rejected."""
     if isinstance(tokens, torch.Tensor) and tokens.is_cuda:
         raise ValueError("advance counts the room on the host: pass the accepted tokens as numbers, not as a CUDA tensor")
     several = np.ndim(tokens) > 0
@@ -520,6 +536,15 @@ def advance(P: PagedLayer, tokens: Union[int, Sequence[int], torch.Tensor]) -> N
         if capturing:
             raise ValueError("the numbers of several requests come from the host and cannot be recorded into a graph")
         more = torch.tensor(taken, dtype=torch.int32, device=P.held.device)
+    if getattr(P, "budget", 0):
+        if several:
+            P.pending.masked_fill_(torch.arange(P.new, dtype=torch.int32, device=P.held.device) >= more[:, None], 0)
+        else:
+            P.pending[:, operator.index(tokens):].zero_()
+        if any(taken):
+            qb.qcf_page_weigh(P.desc, P.cache, P.B, P.new, P.q, P.pending, P.lse, P.held, 1.0, 1.0, P.settled)
+        P.pending.zero_()
+    if several:
         P.held += more
         P.seen += more[:, None]
         P.pos += more.repeat_interleave(P.new)
@@ -541,8 +566,9 @@ def evict(P: PagedLayer, first: int = 1, last: int = 1) -> None:
         raise ValueError(f"the first {first} and the last {last} tokens, {P.budget} in all")
     if P.held.is_cuda and torch.cuda.is_current_stream_capturing():
         raise ValueError("an eviction moves a layer to other pages and cannot be recorded into a graph")
-    qb.qcf_page_evict(P.desc, P.cache, P.B, P.held, P.weights, P.budget, first, last, P.spare, P.kept, P.spare_weights, P.held, P.ws_evict)
+    qb.qcf_page_evict(P.desc, P.cache, P.B, P.held, P.settled, P.budget, first, last, P.spare, P.kept, P.spare_weights, P.held, P.ws_evict)
     P.cache, P.spare = P.spare, P.cache
-    P.weights, P.spare_weights = P.spare_weights, P.weights
+    P.settled, P.spare_weights = P.spare_weights, P.settled
+    P.pending.zero_()
     P.seen.copy_(P.held[:, None] + 1 + torch.arange(P.new, dtype=torch.int32, device=P.held.device))
     P.room = [P.more] * P.B
