@@ -257,9 +257,9 @@ __global__ __launch_bounds__(256) void evict_kernel(EvictArgs a) {
   for (int j0 = first + wave * kBlock; j0 < end; j0 += waves * kBlock) {
     const int t = number(j0), from = page_of(t), to = new_page(j0);
     const int count = (int)__popcll(__ballot(t >= 0) & 0xffffu);
-    if (count == 0 && j0 > 0) break;                     // (of the wave)
     // (the entry behind a full block: the next block's first)
-    if (g == 0 && lane == 0 && (count < kBlock || entry(j0 + kBlock) < 0)) a.to_len[b] = j0 + count;
+    if (g == 0 && lane == 0 && (count > 0 || j0 == 0) && (count < kBlock || entry(j0 + kBlock) < 0)) a.to_len[b] = j0 + count;
+    if (count == 0) break;                               // (of the wave: a block without tokens has no scale either)
     const int s = t & (a.from.page_size - 1), slot = j0 & (a.to.page_size - 1);
     const bool found = from >= 0 && from < a.from.n_pages, there = to >= 0 && to < a.to.n_pages;
     const int64_t src = found ? (from * a.from.page_stride + s * a.from.slot_stride + g * a.from.head_stride) * kSize : -1;
