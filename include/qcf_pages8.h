@@ -34,9 +34,9 @@ qcf_status qcf_page8_append(const qcf_layer_desc* desc, const qcf_page_cache* ca
                             const int64_t* row_off_dev, int64_t total_rows, const int32_t* len_dev, const int32_t* pos_dev, void* q_out,
                             void* stream);
 
-/* qcf_page_attn over 8-bit pages: the same arguments, and scales (any positive finite ones).  Products and sums are taken in 32 bits,
- * codes enter them exactly; a code that is NaN makes the rows NaN that see it.  The scale of a block none of whose tokens a row sees
- * may be anything. */
+/* qcf_page_attn over 8-bit pages: the same arguments, and scales (any from 2^-100 to 2^92, the least and the largest that are stored by
+ * qcf_page8_append: beyond them sums may overflow, below them lose bits).  Products and sums are taken in 32 bits, codes enter them
+ * exactly; a code that is NaN makes the rows NaN that see it.  The scale of a block none of whose tokens a row sees may be anything. */
 size_t qcf_page8_attn_workspace_bytes(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_q, int32_t n_keep);
 qcf_status qcf_page8_attn(const qcf_layer_desc* desc, const qcf_page_cache* cache, const float* scales, int32_t B, int32_t n_q,
                           const void* q, const int32_t* seen_dev, const int32_t* pages, int32_t n_keep, void* o_out, float* lse_out,
