@@ -28,7 +28,8 @@ extern "C" {
  * block's scale is the least power of two s, not less than 2^-100, with |x| <= 448 s for all elements that were stored into it since
  * its first slot was written.  Where rows make the scale of a block grow that has tokens in front of them, these are rounded again, to
  * the new scale (a value changes only where it comes beneath 2^-6 of it).  Elements that are not finite or beyond 2^100 are stored as
- * NaN and do not count for the scale.  Bounds are those of the stored values. */
+ * NaN and do not count for the scale.  Bounds contain the stored values, and are theirs but where older tokens were rounded again, which may
+ * have come closer to 0 than they were: there they may be wider, until slot 0 of the page is written. */
 qcf_status qcf_page8_append(const qcf_layer_desc* desc, const qcf_page_cache* cache, float* scales, int32_t B, const void* q,
                             int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                             const int64_t* row_off_dev, int64_t total_rows, const int32_t* len_dev, const int32_t* pos_dev, void* q_out,

@@ -48,3 +48,35 @@ def test_turned_keys_get_the_codes_of_the_formula(dtype, H, Hkv, D, style, bound
         assert np.array_equal(to_np(p.bd), limits)
     ref = orc.rope_at(q, pos, p.sh.rope_base, style)
     assert np.all(np.abs(to_np(q_out) - ref) <= HALF_STEP[dtype] * np.abs(ref) + 2.0 ** -21 * 2 * np.abs(rows).max())
+
+
+@pytest.mark.parametrize("dtype,D,page,order", [("bf16", 128, 16, "token"), ("f32", 64, 64, "head"), ("bf16", 64, 256, "token")])
+def test_bounds_contain_what_is_stored(dtype, D, page, order):
+    """Steps of rows that grow and shrink, whose blocks are rounded again and again: least and largest stored key of a page lie within its
+    bounds at all times, and are its bounds where the page was written at once.  (Sizes far enough apart for older tokens to lose bits.)"""
+    rng = np.random.default_rng(85)
+    sh = shape(4, 2, D, dtype)
+    p = Paged8(rng, sh, page, [200, 200], order)
+    held, wider = [0, 0], 0
+    for step in range(24):
+        new = [int(n) for n in rng.integers(0, 14, 2)] if step else [40, 0]
+        size = float(2.0 ** rng.uniform(-20, 20))
+        rows = normal(rng, (sum(new) + 1, 8 * D), dtype, size)
+        pos = np.concatenate([np.arange(n) + h for h, n in zip(held, new)] + [[0]]).astype(np.int32)
+        _append(p, rng, held, new, rows, pos if step % 2 else None)
+        held = [h + n for h, n in zip(held, new)]
+        if max(held) > 186:
+            break
+        codes_k, _, scales = p.got()
+        k, b = orc.page8_values((codes_k, codes_k), scales)[0], to_np(p.bd)
+        for r in range(2):
+            for i in range(-(-held[r] // page)):
+                n = min(page, held[r] - i * page)
+                x = k[p.table[r, i], :n]
+                for g in range(2):
+                    lo, hi = b[p.table[r, i], g]
+                    assert np.all(lo <= x[:, g].min(0)) and np.all(hi >= x[:, g].max(0)), (step, r, i, g)
+                    wider += int(np.any(lo < x[:, g].min(0)) or np.any(hi > x[:, g].max(0)))
+                    if step == 0:
+                        assert np.array_equal(lo, x[:, g].min(0)) and np.array_equal(hi, x[:, g].max(0))
+    print("pages and heads whose bounds are wider than what is stored:", wider, flush=True)
