@@ -42,7 +42,10 @@ qcf_status qcf_page_weigh(const qcf_layer_desc* desc, const qcf_page_cache* cach
  * these requests, and each once only.  Tokens of pages that are not there must not be among the first len[b] (they move as zeros);
  * what pages of `to` that are not there should get is dropped, and what goes beyond its max_pages (to_len counts it).  Bounds of `to`,
  * if it has any, are made anew; `cache` needs none.
- * 8-bit pages (scales and to_scales, both or neither): a block of `to` gets the scale that qcf_page8_append would give its tokens. */
+ * 8-bit pages (scales and to_scales, both or neither): a block of `to` gets the scale that qcf_page8_append would give its tokens.
+ * The choice is divided by the room of the table and not by the lengths, which the host does not know: in six launches, where a table has
+ * room for more than 32768 tokens and B * H_kv is at most 128.  8 KV heads of 128 in 8 bits, requests of 2000 tokens to 1024: one takes
+ * 13 us with room for 32768, 30 with more; 16 take 22, 47 with room for 33024 and 117 with room for 131072. */
 size_t qcf_page_evict_workspace_bytes(const qcf_layer_desc* desc, const qcf_page_cache* cache, int32_t B, int32_t n_keep);
 qcf_status qcf_page_evict(const qcf_layer_desc* desc, const qcf_page_cache* cache, const float* scales, int32_t B,
                           const int32_t* len_dev, const float* weights, int32_t n_keep, int32_t n_first, int32_t n_last,

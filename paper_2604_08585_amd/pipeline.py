@@ -539,7 +539,7 @@ def advance(P: PagedLayer, tokens: Union[int, Sequence[int], torch.Tensor]) -> N
     if getattr(P, "budget", 0):
         if several:
             P.pending.masked_fill_(torch.arange(P.new, dtype=torch.int32, device=P.held.device) >= more[:, None], 0)
-        else:
+        elif operator.index(tokens) < P.new:
             P.pending[:, operator.index(tokens):].zero_()
         if any(taken):
             qb.qcf_page_weigh(P.desc, P.cache, P.B, P.new, P.q, P.pending, P.lse, P.held, 1.0, 1.0, P.settled)
