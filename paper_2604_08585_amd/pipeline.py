@@ -549,8 +549,7 @@ def advance(P: PagedLayer, tokens: Union[int, Sequence[int], torch.Tensor]) -> N
         P.seen += more[:, None]
         P.pos += more.repeat_interleave(P.new)
     else:
-        for t in (P.held, P.seen, P.pos):
-            t += operator.index(tokens)
+        torch._foreach_add_([P.held, P.seen, P.pos], operator.index(tokens))         # (one launch)
     if not capturing:
         P.room = [room - t for t, room in zip(taken, P.room)]
 
