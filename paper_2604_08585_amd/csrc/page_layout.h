@@ -48,17 +48,17 @@ struct Division {
   bool whole;                             // a workgroup to every context, KV head and row block: nothing is divided
 };
 
-// Workgroups of four waves that a compute unit holds at once.  (8-bit heads of 64 leave room for a third: 64 requests of 4K to 12K tokens 111
-// us, 122 with two.  Those of 128 would spill 27 registers: 234 us, 203 with two.)
+// Workgroups of four waves that a compute unit holds at once.  (8-bit heads of 64 leave room for a third: 64 requests of 4K to 12K tokens 113
+// us, 123 with two.  Those of 128 would spill registers: 234 us, 203 with two.)
 constexpr int at_once(int head_dim, int row_tiles, bool eight) {
   return head_dim == 64 ? (eight && row_tiles == 1 ? 3 : 2) : row_tiles == 1 || eight ? 2 : 1;
 }
 
 // KV heads whose rows lie next to each other and are read side by side, by the waves of a workgroup: 256 bytes in a row, as a row of bf16
 // has.  read: bytes of the keys and values at most; where they are few, the joins of twice as many parts cost more.  us, pages that keep a
-// token's 8-bit heads together, a head to a workgroup and side by side: heads of 128, 64 requests of 4K to 12K tokens 243 and 205, one of 128K
-// 70 and 61, of 30K (61 MB) 23.0 and 22.6, four new rows 249 and 220, 70 and 65, 8 requests of up to 6K 31.1 and 31.6;
-// heads of 64 188 and 130, one of 30K 22.0 and 20.2, of 3K 11.8 and 14.5.
+// token's 8-bit heads together, a head to a workgroup and side by side: heads of 128, 64 requests of 4K to 12K tokens 239 and 206, one of 128K
+// 70 and 61, of 30K (61 MB) 23.3 and 22.9, four new rows 250 and 221, 71 and 65, 8 requests of up to 6K 32.1 and 32.5;
+// heads of 64 191 and 130, one of 30K 22.3 and 20.5, of 3K 11.9 and 14.5.
 inline int side_by_side(const qcf_layer_desc& L, const qcf_page_cache& c, int elem, double read) {
   const int heads = 256 / L.head_dim;
   const bool worth = read > (L.head_dim == 128 ? 4.0 : 1.0) * kShared;
@@ -75,17 +75,17 @@ inline int side_by_side(const qcf_layer_desc& L, const qcf_page_cache& c, int el
 // 0.6 %, 350: 0.9 %); at its border it takes the worse one by up to 11 % (19 % in float32), and by 25 % for 2048 workgroups of up to 256 tokens.
 // 8-bit pages: a wave's tile takes about as long whatever its width, so that the rule goes by tokens; and where there are more workgroups
 // than compute units, whose second round leaves some idle, it divides from fewer on.  us, whole and divided, lengths from a quarter of the
-// longest on.  One new row, bf16, heads of 128: 8 workgroups of 1024 tokens 11.2 and 11.9, 2048 12.2 and 11.9; 192 of up to 2000 21.3 and
-// 23.3, 4000 36.0 and 35.9; 320 of up to 1000 22.2 and 21.7, 4000 62.7 and 53.4; 512 of up to 1000 26.2 and 29.8, 8000 147 and 133; 1024 of up
-// to 1000 52.5 and 54.3, 2000 81.9 and 80.6.  Heads of 64: 8 of 1024 8.8 and 11.1, 2048 12.7 and 11.4; 128 of up to 3000 20.8 and 20.6; 320 of
-// up to 2000 20.7 and 21.9, 4000 37.0 and 32.0; 1024 of up to 2000 44.4 and 50.2, 8000 149 and 141.  float32, half as many tokens: heads of 64,
-// 320 of up to 500 16.1 and 18.3, 1500 34.8 and 29.8; of 128, 1024 of up to 500 54.4 and 58.4, 1000 91.6 and 84.8.
-// Several new rows, which a join takes longer for: 512 workgroups, heads of 128, of up to 2000 51.7 and 57.0, 4000 86.1 and 88.6; 320 of up
-// to 4000 67.8 and 63.0; heads of 64, 512 of up to 4000 49.0 and 52.5.
-// Heads that only ranges take side by side, one row: heads of 128, 256 of up to 5000 63.9 and 54.2, 320 of up to 4000 73.2 and 53.2, 2048 of
-// up to 300 56.5 and 49.0; of 64, 256 of up to 2500 26.5 and 26.2, 320 of up to 1000 16.9 and 18.8, 1024 of up to 1000 33.3 and 31.5, 4000 120
-// and 88.9.  Four rows, heads of 128: 256 of up to 2500 37.9 and 42.9, 4000 54.1 and 54.9; 512 of up to 1000 34.2 and 36.9, 3000 79.6 and
-// 76.3; 2048 of up to 300 76.3 and 71.7, 2000 198 and 181.  At its borders the rule takes the worse one by up to 5 % (float32, heads of 64:
+// longest on.  One new row, bf16, heads of 128: 8 workgroups of up to 1024 tokens 11.0 and 11.3, 2048 15.0 and 11.2; 192 of up to 2000 22.0
+// and 23.8, 4000 39.7 and 36.4; 320 of up to 1000 22.9 and 22.2, 4000 64.4 and 53.9; 512 of up to 1000 26.8 and 30.3, 8000 150 and 134; 1024 of
+// up to 1000 53.4 and 54.9, 2000 84.0 and 80.9.  Heads of 64: 8 of 1024 8.7 and 10.7, 2048 11.8 and 11.0; 128 of up to 3000 22.2 and 20.9; 320
+// of up to 2000 21.7 and 22.3, 4000 38.8 and 32.6; 1024 of up to 2000 45.7 and 50.9, 8000 151 and 141.  float32, half as many tokens: heads of
+// 64, 320 of up to 500 16.1 and 18.3, 1500 34.8 and 29.8; of 128, 1024 of up to 500 54.4 and 58.4, 1000 91.6 and 84.8.
+// Several new rows, which a join takes longer for: 512 workgroups, heads of 128, of up to 2000 53.2 and 58.2, 4000 88.1 and 89.4; 320 of up
+// to 4000 70.0 and 64.1; heads of 64, 512 of up to 4000 50.3 and 53.7.
+// Heads that only ranges take side by side, one row: heads of 128, 256 of up to 5000 63.7 and 54.6, 320 of up to 4000 73.9 and 53.8, 2048 of
+// up to 300 57.9 and 47.4; of 64, 256 of up to 2500 26.4 and 25.8, 320 of up to 1000 17.4 and 19.0, 1024 of up to 1000 33.9 and 32.0, 4000 120
+// and 89.1.  Four rows, heads of 128: 256 of up to 2500 38.2 and 43.4, 4000 54.6 and 55.3; 512 of up to 1000 34.8 and 37.5, 3000 80.6 and
+// 76.9; 2048 of up to 300 78.9 and 73.2, 2000 200 and 182.  At its borders the rule takes the worse one by up to 6 % (float32, heads of 64:
 // 15 %).
 inline bool takes_whole(const qcf_layer_desc& L, int64_t workgroups, int64_t longest, int elem, int heads, bool several) {
   if (elem == 1) {
@@ -113,8 +113,8 @@ inline Division divide(const qcf_layer_desc& L, const qcf_page_cache& c, int32_t
   // request of 16384 tokens 18.1 and 16.0, 8 of up to 4096 16.6 and 16.4, 64 of up to 1024 19.2 and 16.6, of up to 4096 32.6 and 43.7.
   const int64_t longest = (int64_t)(n_keep && n_keep < c.max_pages ? n_keep : c.max_pages) * c.page_size;
   const double read = (double)d.contexts * (double)longest * L.n_kv_heads * 2 * L.head_dim * elem;
-  // (8-bit heads of 128: from more bytes on.  64 / 8 heads, us, two tiles and one: four drafts of 8 requests of 2K to 6K tokens 37.5 and 35.2,
-  // of 64 of 4K to 12K 247 and 292, of one of 128K 73.8 and 78.5; 32 / 8 heads, 8 drafts of 16 requests of up to 8K 60.3 and 62.7.)
+  // (8-bit heads of 128: from more bytes on.  64 / 8 heads, us, two tiles and one: four drafts of 8 requests of 2K to 6K tokens 38.4 and 36.6,
+  // of 64 of 4K to 12K 262 and 301, of one of 128K 76.4 and 80.6; 32 / 8 heads, 8 drafts of 16 requests of up to 8K 60.0 and 63.9.)
   const bool wide8 = elem == 1 && L.head_dim == 128;
   d.row_tiles = d.rows > 16 && read > (wide8 ? 8.0 : 1.0) * kShared ? 2 : 1;
   d.row_blocks = (d.rows + 16 * d.row_tiles - 1) / (16 * d.row_tiles);

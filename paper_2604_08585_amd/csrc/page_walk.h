@@ -545,8 +545,8 @@ struct Walk {
     if constexpr ((RT == 2 || (EIGHT && WAVES < pages::kWaves)) && D == 128) {
       // (two tiles of rows leave no registers for a second tile of tokens: the next keys are asked for once the logits are there, the
       // next values after the products.  8-bit heads side by side, whose waves ask for the same tokens at once, gain by it too: 64
-      // requests of 4K to 12K tokens 205 us, 216 with a second tile, one of 128K 60.9 and 65.0; a head to a workgroup gains
-      // nothing, 202 and 200, and four drafts of eight requests there lose, 35.4 and 34.2)
+      // requests of 4K to 12K tokens 207 us, 217 with a second tile, one of 128K 61.5 and 65.7; a head to a workgroup gains
+      // little, 200 and 204, and four drafts of eight requests there lose, 35.7 and 34.7)
       if (at < shared) {
         Tile t;
         load(t, at);
