@@ -557,8 +557,8 @@ def advance(P: PagedLayer, tokens: Union[int, Sequence[int], torch.Tensor]) -> N
 def evict(P: PagedLayer, first: int = 1, last: int = 1) -> None:
     """Every head of every request keeps the first `first`, the last `last` and the heaviest other tokens, P.budget in all (P.kept: their
     numbers among those that were held); there is room for as many tokens behind them as paged_layer was asked for.  Positions go on.
-    Between steps (rows that `advance` has not taken are gone), not inside a captured graph: the layer's pages and weights change places with the spare ones, and a step that was
-    captured before would go on with those that the tokens left (capture it again)."""
+    Between steps (rows that `advance` has not taken are gone), not inside a captured graph: the layer's pages and weights change places
+    with the spare ones, and a step that was captured before would go on with those that the tokens left (capture it again)."""
     if not P.budget:
         raise ValueError("paged_layer(budget=...) makes the pages that tokens move to")
     if min(first, last) < 0 or first + last > P.budget:
